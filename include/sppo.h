@@ -368,8 +368,8 @@ sppo_status sppo_attn_bwd_chunk_noalloc(int64_t batch, int64_t seq_len, int64_t 
 sppo_status sppo_get_offsets(const sppo_ctx* ctx, int64_t* out, int32_t capacity);
 
 /* Message for the last failure of this context ("" if none); with
- * ctx == NULL, the message of the last failed sppo_create or context-free
- * attention call on this thread. */
+ * ctx == NULL, the message of the last failed sppo_create, context-free
+ * attention call or training operator on this thread. */
 const char* sppo_last_error(const sppo_ctx* ctx);
 
 /* Static name of a status code. */
@@ -456,6 +456,148 @@ sppo_status sppo_transpose_bf16(const void* in, void* out, int64_t rows, int64_t
  * the fused QKV projection's output (B = 1). */
 sppo_status sppo_pack_qkv_grad(int64_t rows, int32_t wq, int32_t wkv, const void* dq, const float* dk,
                                const float* dv, int64_t row0, void* out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Training operators beside the layer's: dropout, the norms, gate and
+ * residual at a block's ends, and the token embedding.  Context-free like
+ * the calls above (device pointers, validated on the host, nothing enqueued
+ * on failure, the message in sppo_last_error(NULL) on the calling thread),
+ * and free of any allocation or synchronisation, so they can be captured
+ * into a graph.  `dtype` is the element type of every activation and of the
+ * embedding table; parameters, statistics and parameter gradients are fp32.
+ * Activations are row-major with a leading dimension in elements.  Widths
+ * and leading dimensions are multiples of 8, activation, table and gradient
+ * table pointers 16-byte aligned, the other pointers aligned to their type.
+ * An output may be the same buffer as an input only where it says so.  A
+ * workspace is the call's own until its work on the stream is done: calls
+ * that may run at the same time (two streams, two graphs) need one each.
+ * ---------------------------------------------------------------------- */
+
+/* Dropout without a stored mask.  Whether an element is kept depends on
+ * (seed, offset, its position in the whole sequence) alone, so the backward
+ * and a recomputed forward draw the mask again, and the chunks of a sequence
+ * draw the mask that the whole sequence would:
+ *   t = row0 + r (r: row of the call), e = t * W + c (c < W: column, W the
+ *   row's width), u = 16-bit half word e % 8 (low half of word 0 first) of
+ *   Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as
+ *   easy as 1, 2, 3", SC 2011) with counter words (e / 8 low, e / 8 high,
+ *   offset low, offset high) and key (seed low, seed high);
+ *   kept when u >= T, T = round(65536 p), and then scaled by
+ *   65536 / (65536 - T), the inverse of the probability that is drawn.
+ * A dropped element is zero whatever its value (NaN and infinities too).
+ * Calls that need independent masks (other operators, other steps) take
+ * other offsets.  offset_dev: NULL, or a device uint64 added to offset when
+ * the kernel runs, so that a replayed graph draws new masks; it is to hold
+ * the same value in a step's forward and backward. */
+typedef struct {
+  float p;                    /* 0 <= p < 1, T < 65536                      */
+  uint64_t seed;
+  uint64_t offset;
+  const uint64_t* offset_dev;
+  int64_t row0;               /* global index of the call's first row, >= 0 */
+} sppo_drop;
+
+/* y = res + keep * x (res NULL: y = keep * x) for rows x cols elements;
+ * applied to a gradient it is the backward.  y may be x or res (with the
+ * same leading dimension).  Errors: INVALID_ARG, UNSUPPORTED
+ * ((row0 + rows) * cols >= 2^63), HIP. */
+sppo_status sppo_dropout(sppo_dtype dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx, const void* res,
+                         int64_t ldres, const sppo_drop* drop, void* y, int64_t ldy, void* stream);
+
+/* What joins a block's output b to the residual stream x, in one pass:
+ *   n = N_post(b)                      (post NONE: n = b)
+ *   h = residual_scale x + branch_scale keep (gate n)
+ *   z = N_pre(h)                       (pre NONE: no z)
+ * N is LayerNorm (LAYER: (v - mean) rstd gamma + beta, biased variance) or
+ * RMSNorm (RMS: v rstd gamma + beta, rstd = 1/sqrt(mean(v^2) + eps)); beta
+ * may be NULL (zero).  gate: fp32, one value per channel [H] (a parameter)
+ * or per row [rows].  keep: the dropout above, W = H, or none.  H % 8 == 0,
+ * H <= 8192.  Everything between the loads and the stores is fp32: z and
+ * its statistics come from h before it is rounded. */
+typedef enum { SPPO_NORM_NONE = 0, SPPO_NORM_LAYER = 1, SPPO_NORM_RMS = 2 } sppo_norm;
+typedef enum { SPPO_GATE_NONE = 0, SPPO_GATE_CHANNEL = 1, SPPO_GATE_TOKEN = 2 } sppo_gate;
+typedef struct {
+  int32_t H;
+  sppo_dtype dtype;
+  sppo_norm post, pre;
+  sppo_gate gate_kind;
+  float eps;                /* > 0 where there is a norm                    */
+  float residual_scale, branch_scale;  /* finite                            */
+  const float* post_gamma;  /* [H], needed unless post is NONE              */
+  const float* post_beta;   /* [H] or NULL                                  */
+  const float* gate;        /* [H] or [rows], needed unless gate is NONE    */
+  const float* pre_gamma;   /* [H], needed unless pre is NONE               */
+  const float* pre_beta;    /* [H] or NULL                                  */
+} sppo_block_norm;
+
+/* Row statistics, fp32 [rows]: written by the forward, read by the
+ * backward.  Each is needed where its norm is there (the means for LAYER
+ * only) and ignored otherwise. */
+typedef struct {
+  float* post_mean;
+  float* post_rstd;
+  float* pre_mean;
+  float* pre_rstd;
+} sppo_block_norm_stats;
+
+/* Parameter gradients, fp32 ([H]; gate as the gate).  NULL: not wanted.
+ * One without its parameter is ignored. */
+typedef struct {
+  float* post_gamma;
+  float* post_beta;
+  float* gate;
+  float* pre_gamma;
+  float* pre_beta;
+} sppo_block_norm_grads;
+
+/* drop: NULL for none.  z: needed unless pre is NONE.  h may be x or b, and
+ * z may be b (with the same leading dimension; h and z differ). */
+sppo_status sppo_block_norm_fwd(const sppo_block_norm* bn, int64_t rows, const sppo_drop* drop, const void* x,
+                                int64_t ldx, const void* b, int64_t ldb, void* h, int64_t ldh, void* z, int64_t ldz,
+                                const sppo_block_norm_stats* stats, void* stream);
+
+/* Backward: dz is z's gradient, dh the gradient that reaches h from
+ * elsewhere (the residual stream; NULL: none, where there is a z).  With
+ * D = dh + N_pre'(dz):
+ *   dx = residual_scale D,  m = branch_scale keep D,  dgate = sum m n,
+ *   db = N_post'(gate m),  and the norms' parameter gradients.
+ * The [H] gradients are overwritten (accumulate = 0) or added to, their sums
+ * over rows taken in a fixed order (the same bits every time); a gate
+ * gradient per row is always written.  b is needed unless post is NONE and
+ * no gate gradient is wanted, h where there is a z.  dx may be dh or dz, db
+ * may be b, dz or h (with the same leading dimension; dx and db differ).
+ * workspace: sppo_block_norm_bwd_workspace bytes (0 for an invalid bn; it
+ * does not shrink as rows grow), 16-byte aligned. */
+size_t sppo_block_norm_bwd_workspace(const sppo_block_norm* bn, int64_t rows);
+sppo_status sppo_block_norm_bwd(const sppo_block_norm* bn, int64_t rows, const sppo_drop* drop, const void* b,
+                                int64_t ldb, const void* h, int64_t ldh, const sppo_block_norm_stats* stats,
+                                const void* dz, int64_t lddz, const void* dh, int64_t lddh, void* dx, int64_t lddx,
+                                void* db, int64_t lddb, const sppo_block_norm_grads* grads, int32_t accumulate,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* y[r] = keep * (scale * table[ids[r]]), table [V, H] with row stride ldt;
+ * ids [rows] of id_type.  An id outside [0, V) (padding, another rank's part
+ * of a split vocabulary) gives a row of zeros, and nothing is read for it.
+ * drop: NULL for none (W = H).  rows <= 2^28, V < 2^31, H <= 2^20
+ * (UNSUPPORTED otherwise). */
+typedef enum { SPPO_I32 = 0, SPPO_I64 = 1 } sppo_id_type;
+sppo_status sppo_embedding_fwd(sppo_dtype dtype, sppo_id_type id_type, int64_t rows, int32_t H, int64_t V,
+                               const void* ids, const void* table, int64_t ldt, float scale, const sppo_drop* drop,
+                               void* y, int64_t ldy, void* stream);
+
+/* Its gradient, by sorted tokens: dtable[v] (fp32 [V, H], row stride lddt)
+ * = scale * sum over the rows r with ids[r] == v of keep * dy[r].
+ * accumulate 0 overwrites all V rows (rows without a token become zero), 1
+ * adds to the rows that have tokens and leaves the others as they are.  The
+ * sums run in a fixed order, so results are the same bits every time.  Ids
+ * outside [0, V) contribute nothing.  workspace:
+ * sppo_embedding_bwd_workspace bytes (0 for invalid sizes; it does not
+ * shrink as rows grow), 16-byte aligned. */
+size_t sppo_embedding_bwd_workspace(int64_t rows, int32_t H);
+sppo_status sppo_embedding_bwd(sppo_dtype dtype, sppo_id_type id_type, int64_t rows, int32_t H, int64_t V,
+                               const void* ids, const void* dy, int64_t lddy, float scale, const sppo_drop* drop,
+                               float* dtable, int64_t lddt, int32_t accumulate, void* workspace,
+                               size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

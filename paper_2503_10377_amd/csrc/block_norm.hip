@@ -1,0 +1,498 @@
+// The end of a transformer block in one pass: the norm after the block's
+// branch, its gate, dropout, the scaled residual add and the norm in front of
+// the next block; and the backward of all of it.
+//   n = N_post(b);  h = alpha x + s keep (gate n);  z = N_pre(h)
+// Done by separate kernels, n and h would travel to memory and back.  One row
+// is held by a team of threads in registers (TEAM threads, PER groups of
+// eight columns each); both norms' sums stay within the team.
+#include "row_common.h"
+
+namespace sppo {
+namespace {
+
+constexpr int kNone = 0, kLayer = 1, kRms = 2;
+constexpr int kChannel = 1, kToken = 2;
+
+// Mean and 1 / sqrt(var + eps) of the row that the team holds in v.  Each wave
+// takes the mean of its own columns and the squares around it; the waves'
+// pairs are then joined (M2 = sum M2_w + n_w (mean_w - mean)^2), so one
+// exchange serves both moments and nothing cancels.  red: an LDS image for
+// this call alone until the next barrier but one (callers alternate two).
+template <int TEAM, int PER>
+__device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int tid, bool rms, float eps, float* red,
+                                            float& mean, float& rstd) {
+  constexpr int NW = TEAM / 64;
+  const int wv = tid >> 6;
+  auto columns = [&](int w) {  // of wave w
+    int n = 0;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int left = H - 8 * (64 * w + TEAM * p);
+      n += left <= 0 ? 0 : (left < 512 ? left : 512);
+    }
+    return n;
+  };
+  float s = 0.f, q = 0.f;
+  float m = 0.f;
+  if (!rms) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+      if (8 * (tid + TEAM * p) < H) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += v[p][e];
+      }
+    s = wave_sum(s);
+    const int n = columns(wv);
+    m = n > 0 ? s / n : 0.f;
+  }
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+    if (8 * (tid + TEAM * p) < H) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = v[p][e] - m;
+        q += d * d;
+      }
+    }
+  q = wave_sum(q);
+  if constexpr (NW > 1) {
+    if ((tid & 63) == 0) {
+      red[2 * wv] = s;
+      red[2 * wv + 1] = q;
+    }
+    __syncthreads();
+    s = q = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s += red[2 * w];
+    m = rms ? 0.f : s / H;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      q += red[2 * w + 1];
+      const int n = columns(w);
+      if (!rms && n > 0) {
+        const float d = red[2 * w] / n - m;
+        q += n * d * d;
+      }
+    }
+  }
+  mean = m;
+  rstd = 1.f / sqrtf(q / H + eps);
+}
+
+// Forward.  NT threads, teams of TEAM (the workgroup, or one wave of it).
+template <typename T, int NT, int TEAM, int PER>
+__global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
+  static_assert(TEAM == NT || TEAM == 64, "");
+  __shared__ float red[2][2 * (NT / 64)];
+  const int H = a.H, tid = threadIdx.x % TEAM;
+  const int64_t row = (int64_t)blockIdx.x * (NT / TEAM) + threadIdx.x / TEAM;
+  if (TEAM < NT && row >= a.rows) return;
+  const Dropper drop(a.drop);
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  const T* b = static_cast<const T*>(a.b) + row * a.ldb;
+  Eight<T> xr[PER], br[PER];
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int c = 8 * (tid + TEAM * p);
+    if (c < H) {
+      br[p].load(b + c);
+      xr[p].load(x + c);
+    }
+  }
+  float v[PER][8];
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+    if (8 * (tid + TEAM * p) < H) br[p].get(v[p]);
+  float mean = 0.f, rstd = 1.f;
+  if (a.post != kNone) {
+    row_moments<TEAM, PER>(v, H, tid, a.post == kRms, a.eps, red[0], mean, rstd);
+    if (tid == 0) {
+      if (a.post == kLayer) a.post_mean[row] = mean;
+      a.post_rstd[row] = rstd;
+    }
+  }
+  const float scale = a.gate_kind == kToken ? a.bscale * a.gate[row] : a.bscale;
+  const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int c = 8 * (tid + TEAM * p);
+    if (c < H) {
+      float w[8];
+      if (a.post != kNone) {
+        load8f(a.post_gamma + c, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] = (v[p][e] - mean) * rstd * w[e];
+        if (a.post_beta) {
+          load8f(a.post_beta + c, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[p][e] += w[e];
+        }
+      }
+      if (a.gate_kind == kChannel) {
+        load8f(a.gate + c, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] *= w[e];
+      }
+      drop.apply(g0 + c / 8, v[p]);
+      xr[p].get(w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[p][e] = a.alpha * w[e] + scale * v[p][e];
+      Eight<T>::store(static_cast<T*>(a.h) + row * a.ldh + c, v[p]);
+    }
+  }
+  if (a.pre == kNone) return;
+  row_moments<TEAM, PER>(v, H, tid, a.pre == kRms, a.eps, red[1], mean, rstd);
+  if (tid == 0) {
+    if (a.pre == kLayer) a.pre_mean[row] = mean;
+    a.pre_rstd[row] = rstd;
+  }
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int c = 8 * (tid + TEAM * p);
+    if (c < H) {
+      float w[8];
+      load8f(a.pre_gamma + c, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[p][e] = (v[p][e] - mean) * rstd * w[e];
+      if (a.pre_beta) {
+        load8f(a.pre_beta + c, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] += w[e];
+      }
+      Eight<T>::store(static_cast<T*>(a.z) + row * a.ldz + c, v[p]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ backward
+// With xh, bh the normalised h and b, m = s keep D, k = the row's gate (1
+// unless the gate is per row) and the column sums over rows
+//   S0 = sum dz xh, S1 = sum dz, S2 = sum k m bh, S3 = sum k m
+// (no post norm: S2 = sum k m b), the parameter gradients are
+//   dgamma_pre = S0, dbeta_pre = S1, dgamma_post = gate S2, dbeta_post = gate S3,
+//   dgate (per channel) = gamma_post S2 + beta_post S3 (no post norm: S2),
+// so the gate per channel needs no sum of its own.
+struct Slots {
+  bool on[4];
+  int at[4];
+  int n;
+};
+__host__ __device__ inline Slots bn_slots(const BlockNormArgs& a) {
+  Slots s;
+  const bool chan = a.gate_kind == kChannel && a.d_gate;
+  s.on[0] = a.pre != kNone && a.d_pre_gamma;
+  s.on[1] = a.pre != kNone && a.pre_beta && a.d_pre_beta;
+  s.on[2] = chan || (a.post != kNone && a.d_post_gamma);
+  s.on[3] = a.post != kNone && a.post_beta && (chan || a.d_post_beta);
+  s.n = 0;
+  for (int i = 0; i < 4; ++i) {
+    s.at[i] = s.n;
+    s.n += s.on[i];
+  }
+  return s;
+}
+
+// The team's sums of N values per thread, in every thread.
+template <int TEAM, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  if constexpr (TEAM > 64) {
+    constexpr int NW = TEAM / 64;
+    if ((tid & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[(tid >> 6) * N + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = red[i];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v[i] += red[w * N + i];
+    }
+  }
+}
+
+template <typename T, int NT, int TEAM, int PER>
+__global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
+  static_assert(TEAM == NT || TEAM == 64, "");
+  constexpr int TEAMS = NT / TEAM;
+  // The team's exchanges alternate between two images: a wave writes one only
+  // past the barrier that ended the reads of its last use.
+  __shared__ float red[2][3 * (NT / 64)];
+  int ph = 0;
+  const int H = a.H, tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+  const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block;
+  const int64_t r1 = r0 + a.rows_per_block < a.rows ? r0 + a.rows_per_block : a.rows;
+  const Dropper drop(a.drop);
+  const Slots slots = bn_slots(a);
+  const bool pre = a.pre != kNone, post = a.post != kNone;
+  const bool need_b = a.b != nullptr;
+  float sum[4][PER][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[i][p][e] = 0.f;
+  for (int64_t row = r0 + team; row < r1; row += TEAMS) {
+    Eight<T> hr[PER], br[PER], zr[PER], dr[PER];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      hr[p].zero(); br[p].zero(); zr[p].zero(); dr[p].zero();
+      if (c < H) {
+        if (pre) {
+          hr[p].load(static_cast<const T*>(a.h) + row * a.ldh + c);
+          zr[p].load(static_cast<const T*>(a.dz) + row * a.lddz + c);
+        }
+        if (a.dh) dr[p].load(static_cast<const T*>(a.dh) + row * a.lddh + c);
+        if (need_b) br[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
+      }
+    }
+    float D[PER][8];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) dr[p].get(D[p]);
+    if (pre) {
+      const float mean = a.pre == kLayer ? a.pre_mean[row] : 0.f, rstd = a.pre_rstd[row];
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int c = 8 * (tid + TEAM * p);
+        if (c < H) {
+          float hv[8], zv[8], gm[8];
+          hr[p].get(hv);
+          zr[p].get(zv);
+          load8f(a.pre_gamma + c, gm);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float xh = (hv[e] - mean) * rstd, g = zv[e] * gm[e];
+            s[0] += g;
+            s[1] += g * xh;
+            sum[0][p][e] += zv[e] * xh;
+            sum[1][p][e] += zv[e];
+          }
+        }
+      }
+      team_sum<TEAM>(s, tid, red[ph]);
+      ph ^= 1;
+      const float m1 = a.pre == kLayer ? s[0] / H : 0.f, m2 = s[1] / H;
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int c = 8 * (tid + TEAM * p);
+        if (c < H) {
+          float hv[8], zv[8], gm[8];
+          hr[p].get(hv);
+          zr[p].get(zv);
+          load8f(a.pre_gamma + c, gm);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) D[p][e] += rstd * (zv[e] * gm[e] - m1 - (hv[e] - mean) * rstd * m2);
+        }
+      }
+    }
+    const float mean = a.post == kLayer ? a.post_mean[row] : 0.f, rstd = post ? a.post_rstd[row] : 1.f;
+    const float k = a.gate_kind == kToken ? a.gate[row] : 1.f;
+    const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
+    float s[3] = {0.f, 0.f, 0.f};  // of m gamma gate_c, of that times bh (no post norm: of m b), of m beta
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      if (c < H) {
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = a.alpha * D[p][e];
+        Eight<T>::store(static_cast<T*>(a.dx) + row * a.lddx + c, o);
+        drop.apply(g0 + c / 8, D[p]);
+        float bv[8], gm[8], bt[8], gc[8];
+        br[p].get(bv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) gm[e] = gc[e] = 1.f, bt[e] = 0.f;
+        if (post) load8f(a.post_gamma + c, gm);
+        if (post && a.post_beta) load8f(a.post_beta + c, bt);
+        if (a.gate_kind == kChannel) load8f(a.gate + c, gc);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float m = a.bscale * D[p][e], bh = (bv[e] - mean) * rstd;
+          const float w = m * gm[e] * gc[e];
+          s[0] += w;
+          s[1] += m != 0.f ? w * bh : 0.f;  // a dropped element is zero whatever b holds
+          s[2] += m * bt[e];
+          sum[2][p][e] += m != 0.f ? k * m * bh : 0.f;
+          sum[3][p][e] += k * m;
+          D[p][e] = w;
+        }
+      }
+    }
+    if (post || a.gate_kind == kToken) {
+      team_sum<TEAM>(s, tid, red[ph]);
+      ph ^= 1;
+    }
+    if (a.gate_kind == kToken && a.d_gate && tid == 0) a.d_gate[row] = s[1] + s[2];
+    const float m1 = a.post == kLayer ? k * s[0] / H : 0.f, m2 = k * s[1] / H;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      if (c < H) {
+        if (post) {
+          float bv[8];
+          br[p].get(bv);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) D[p][e] = rstd * (k * D[p][e] - m1 - (bv[e] - mean) * rstd * m2);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) D[p][e] *= k;
+        }
+        Eight<T>::store(static_cast<T*>(a.db) + row * a.lddb + c, D[p]);
+      }
+    }
+  }
+  // The workgroup's column sums: its teams' in team order.
+  float* part = a.part + (int64_t)blockIdx.x * slots.n * H;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (!slots.on[i]) continue;
+    if constexpr (TEAMS > 1) {
+      __shared__ __attribute__((aligned(16))) float comb[TEAMS][8 * TEAM * PER];
+      __syncthreads();
+#pragma unroll
+      for (int p = 0; p < PER; ++p) Eight<float>::store(&comb[team][8 * (tid + TEAM * p)], sum[i][p]);
+      __syncthreads();
+      for (int c = threadIdx.x; c < H; c += NT) {
+        float t = comb[0][c];
+#pragma unroll
+        for (int u = 1; u < TEAMS; ++u) t += comb[u][c];
+        part[slots.at[i] * H + c] = t;
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const int c = 8 * (tid + TEAM * p);
+        if (c < H) Eight<float>::store(part + slots.at[i] * H + c, sum[i][p]);
+      }
+    }
+  }
+}
+
+// The column sums over the workgroups, and the gradients made from them.  A
+// workgroup covers 32 columns with 32 groups of rows: group t adds blocks t,
+// t + 32, ... in order, then the groups are added pairwise.
+constexpr int kRedCols = 32, kRedGroups = 32;
+__global__ __launch_bounds__(kRedCols / 4 * kRedGroups) void bn_reduce_kernel(BlockNormArgs a) {
+  __shared__ __attribute__((aligned(16))) float red[4][kRedGroups][kRedCols + 4];
+  const int lc = threadIdx.x % (kRedCols / 4) * 4, t = threadIdx.x / (kRedCols / 4);
+  const int c = blockIdx.x * kRedCols + lc, H = a.H;
+  const Slots slots = bn_slots(a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (slots.on[i] && c < H) {
+#pragma unroll 8
+      for (int b = t; b < a.nblocks; b += kRedGroups)
+        s += *reinterpret_cast<const f32x4*>(a.part + ((int64_t)b * slots.n + slots.at[i]) * H + c);
+    }
+    *reinterpret_cast<f32x4*>(&red[i][t][lc]) = s;
+  }
+  __syncthreads();
+  const int oc = blockIdx.x * kRedCols + threadIdx.x;
+  if (threadIdx.x >= kRedCols || oc >= H) return;
+  float S[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float v[kRedGroups];
+#pragma unroll
+    for (int u = 0; u < kRedGroups; ++u) v[u] = red[i][u][threadIdx.x];
+#pragma unroll
+    for (int n = kRedGroups / 2; n > 0; n /= 2) {
+#pragma unroll
+      for (int u = 0; u < n; ++u) v[u] += v[u + n];
+    }
+    S[i] = v[0];
+  }
+  const bool post = a.post != kNone, chan = a.gate_kind == kChannel;
+  auto put = [&](float* dst, float x) {
+    if (a.accumulate) dst[oc] += x;
+    else dst[oc] = x;
+  };
+  const float gate = chan ? a.gate[oc] : 1.f;
+  if (slots.on[0]) put(a.d_pre_gamma, S[0]);
+  if (slots.on[1]) put(a.d_pre_beta, S[1]);
+  if (post && a.d_post_gamma) put(a.d_post_gamma, gate * S[2]);
+  if (post && a.post_beta && a.d_post_beta) put(a.d_post_beta, gate * S[3]);
+  if (chan && a.d_gate) {
+    float g = post ? a.post_gamma[oc] * S[2] : S[2];
+    if (post && a.post_beta) g += a.post_beta[oc] * S[3];
+    put(a.d_gate, g);
+  }
+}
+
+constexpr int kMaxBlocks = 512;  // two a compute unit
+
+template <typename T, int NT, int TEAM, int PER>
+hipError_t fwd(const BlockNormArgs& a, hipStream_t stream) {
+  const int64_t teams = NT / TEAM;
+  hipLaunchKernelGGL((bn_fwd_kernel<T, NT, TEAM, PER>), dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(NT), 0,
+                     stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, int NT, int TEAM, int PER>
+hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((bn_bwd_kernel<T, NT, TEAM, PER>), dim3((unsigned)a.nblocks), dim3(NT), 0, stream, a);
+  return hipGetLastError();
+}
+
+// Rows a workgroup works on at a time: up to 1024 columns a wave holds a row.
+int teams_of(int H) { return H <= 1024 ? 4 : 1; }
+
+template <typename T>
+hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
+  if (a.H <= 512) return fwd<T, 256, 64, 1>(a, stream);
+  if (a.H <= 1024) return fwd<T, 256, 64, 2>(a, stream);
+  if (a.H <= 2048) return fwd<T, 256, 256, 1>(a, stream);
+  if (a.H <= 4096) return fwd<T, 512, 512, 1>(a, stream);
+  return fwd<T, 1024, 1024, 1>(a, stream);
+}
+
+template <typename T>
+hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
+  if (a.H <= 512) return bwd<T, 256, 64, 1>(a, stream);
+  if (a.H <= 1024) return bwd<T, 256, 64, 2>(a, stream);
+  if (a.H <= 2048) return bwd<T, 256, 256, 1>(a, stream);
+  if (a.H <= 4096) return bwd<T, 512, 512, 1>(a, stream);
+  return bwd<T, 1024, 1024, 1>(a, stream);
+}
+
+int64_t bwd_blocks(int64_t rows, int H) {
+  const int64_t teams = teams_of(H), groups = (rows + teams - 1) / teams;
+  return groups < kMaxBlocks ? groups : kMaxBlocks;
+}
+
+}  // namespace
+
+size_t block_norm_bwd_workspace(const BlockNormArgs& a) {
+  // as if every gradient were wanted
+  BlockNormArgs b = a;
+  float any;
+  b.d_post_gamma = b.d_post_beta = b.d_gate = b.d_pre_gamma = b.d_pre_beta = &any;
+  return (size_t)bwd_blocks(a.rows, a.H) * bn_slots(b).n * (size_t)a.H * sizeof(float);
+}
+
+hipError_t launch_block_norm_fwd(const BlockNormArgs& a, hipStream_t stream) {
+  if (a.rows <= 0 || a.H <= 0 || a.H % 8 || a.H > kBnMaxH) return hipErrorInvalidValue;
+  return a.f32 ? forward<float>(a, stream) : forward<uint16_t>(a, stream);
+}
+
+hipError_t launch_block_norm_bwd(const BlockNormArgs& a, hipStream_t stream) {
+  if (a.rows <= 0 || a.H <= 0 || a.H % 8 || a.H > kBnMaxH) return hipErrorInvalidValue;
+  BlockNormArgs b = a;
+  const int64_t teams = teams_of(a.H), most = bwd_blocks(a.rows, a.H);
+  b.rows_per_block = (int)((a.rows + most * teams - 1) / (most * teams) * teams);
+  b.nblocks = (int)((a.rows + b.rows_per_block - 1) / b.rows_per_block);
+  const hipError_t e = a.f32 ? backward<float>(b, stream) : backward<uint16_t>(b, stream);
+  if (e != hipSuccess || bn_slots(a).n == 0) return e;
+  hipLaunchKernelGGL(bn_reduce_kernel, dim3((unsigned)((a.H + kRedCols - 1) / kRedCols)),
+                     dim3(kRedCols / 4 * kRedGroups), 0, stream, b);
+  return hipGetLastError();
+}
+
+}  // namespace sppo

@@ -3,32 +3,13 @@
 // recomputation, the weight transpose, and the packing of the chunk's
 // [dQ | dK | dV] rows for the QKV projection's backward.  bf16 activations,
 // fp32 statistics and parameter gradients.
-#include "sppo_kernels.h"
-#include "tile_common.h"
+#include "row_common.h"
 
 namespace sppo {
 namespace {
 
 constexpr int kLnThreads = 256;
 constexpr int kLnMaxPer = 4;  // 16-byte groups per thread: H <= 256 * 8 * 4 = 8192
-
-// Sum over the wave, in every lane: DPP within the 16-lane rows (xor 1, xor 2,
-// then mirrors, whose partners hold the other half's sum), permlane swaps
-// between them; no LDS round trips.
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  v += dpp<0xB1>(v);
-  v += dpp<0x4E>(v);
-  v += dpp<0x141>(v);
-  v += dpp<0x140>(v);
-  return sum_groups(v);
-}
-
-// Four floats of a buffer whose caller promises a float's alignment.
-using f32x4_a4 = float __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ float block_sum(float v, float* red) {
   v = wave_sum(v);
@@ -37,18 +18,6 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   if (lane == 0) red[w] = v;
   __syncthreads();
   return red[0] + red[1] + red[2] + red[3];
-}
-
-__device__ __forceinline__ void unpack8(const u32x4& x, float (&f)[8]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = __uint_as_float(x[e] << 16);
-    f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
-  const bf16x8 b = pack_bf16x8(f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]);
-  return __builtin_bit_cast(u32x4, b);
 }
 
 // y = (x - mean) * rstd * gamma + beta per row, with biased variance; TEAM

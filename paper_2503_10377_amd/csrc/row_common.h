@@ -1,0 +1,126 @@
+// Device-side helpers of the row-wise kernels: sums over a wave, eight
+// elements of a row in and out, the counter-based generator of the dropout,
+// and the division of a flat index by a row's pieces.
+#pragma once
+
+#include "sppo_kernels.h"
+#include "tile_common.h"
+
+namespace sppo {
+
+// Sum over the wave, in every lane: DPP within the 16-lane rows (xor 1, xor 2,
+// then mirrors, whose partners hold the other half's sum), permlane swaps
+// between them; no LDS round trips.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v += dpp<0xB1>(v);
+  v += dpp<0x4E>(v);
+  v += dpp<0x141>(v);
+  v += dpp<0x140>(v);
+  return sum_groups(v);
+}
+
+// Four floats of a buffer whose caller promises a float's alignment.
+using f32x4_a4 = float __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ void unpack8(const u32x4& x, float (&f)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = __uint_as_float(x[e] << 16);
+    f[2 * e + 1] = __uint_as_float(x[e] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
+  const bf16x8 b = pack_bf16x8(f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]);
+  return __builtin_bit_cast(u32x4, b);
+}
+
+// Eight consecutive elements as they lie in memory, for activations of either
+// type: bf16 in one 16-byte piece, fp32 in two.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+  u32x4 v;
+  __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void load(const uint16_t* p) { v = ld_global16(p); }
+  __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(v, f); }
+  static __device__ __forceinline__ void store(uint16_t* p, const float (&f)[8]) {
+    *reinterpret_cast<u32x4*>(p) = pack8(f);
+  }
+};
+template <>
+struct Eight<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ void zero() { v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = *reinterpret_cast<const f32x4*>(p);
+    v[1] = *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = v[e >> 2][e & 3];
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&f)[8]) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+  }
+};
+__device__ __forceinline__ void load8f(const float* p, float (&f)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4_a4*>(p + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[e + i] = v[i];
+  }
+}
+
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011): ten rounds of two
+// 32 x 32 -> 64 bit products on a 128-bit counter, with a 64-bit key.
+__device__ __forceinline__ u32x4 philox(uint64_t counter, uint64_t offset, uint64_t seed) {
+  uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32);
+  uint32_t c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)p1;
+    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)p0;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return u32x4{c0, c1, c2, c3};
+}
+
+// The dropout of a kernel's rows: eight elements (one draw) at a time.
+struct Dropper {
+  uint64_t seed, offset;
+  uint32_t t16;  // threshold in the high half word; 0: everything is kept
+  float scale;
+  __device__ __forceinline__ explicit Dropper(const DropArgs& d)
+      : seed(d.seed), offset(d.offset), t16(d.threshold << 16), scale(d.scale) {
+    if (d.offset_dev) offset += *d.offset_dev;
+  }
+  // f (the elements 8 g .. 8 g + 7 of the whole sequence) with the dropped
+  // ones zero and the others scaled.  A half word is compared in the upper
+  // half of a word: the low one shifted there, the high one where it is.
+  __device__ __forceinline__ void apply(uint64_t g, float (&f)[8]) const {
+    if (t16 == 0) return;
+    const u32x4 w = philox(g, offset, seed);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (e & 1 ? w[e >> 1] : w[e >> 1] << 16) >= t16 ? f[e] * scale : 0.f;
+  }
+};
+
+// n / d and n % d for n < 2^31 by a product with the rounded reciprocal that
+// the host made.
+__device__ __forceinline__ uint32_t fast_div(uint32_t n, const FastDiv& d) {
+  return d.shift < 0 ? n : (uint32_t)(((uint64_t)n * d.mul) >> 32) >> d.shift;
+}
+
+}  // namespace sppo

@@ -189,4 +189,123 @@ struct PackArgs {
 };
 hipError_t launch_pack_dqkv(const PackArgs& a, hipStream_t stream);
 
+// Dropout of a call's rows: threshold in [0, 65535] (0: none), the scale of
+// the kept elements, the global index of its first row.
+struct DropArgs {
+  uint64_t seed, offset;
+  const uint64_t* offset_dev;
+  uint32_t threshold;
+  float scale;
+  int64_t row0;
+};
+
+// Division of numbers below 2^31 by d >= 1 (row_common.h: fast_div): with
+// s = ceil(log2 d) and mul = ceil(2^(31 + s) / d), which is below 2^32 for
+// d > 1, n mul / 2^(31 + s) exceeds n / d by less than 2^-s <= 1 / d.
+struct FastDiv {
+  uint32_t mul;
+  int shift;  // -1: d == 1
+};
+inline FastDiv fast_divisor(uint32_t d) {
+  if (d == 1) return {0, -1};
+  int s = 0;
+  while (((uint64_t)1 << s) < d) ++s;
+  return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), s - 1};
+}
+
+// y = res + drop(x) (res NULL: drop(x)) on rows of `cols` elements, fp32 or bf16.
+struct DropoutArgs {
+  int64_t rows;
+  int cols;
+  const void* x;
+  int64_t ldx;
+  const void* res;
+  int64_t ldres;
+  void* y;
+  int64_t ldy;
+  DropArgs drop;
+  int f32;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
+// A block's end: n = N_post(b), h = alpha x + bscale keep (gate n), z =
+// N_pre(h), and its backward (norm and gate kinds as sppo_norm, sppo_gate).
+// The backward's workgroups take rows_per_block rows each and leave their
+// column sums in part [nblocks][slots][H], slots in the order of BnSlot of
+// those that are needed; a second kernel adds them in a fixed order.
+struct BlockNormArgs {
+  int64_t rows;
+  int H;
+  int post, pre, gate_kind;
+  float eps, alpha, bscale;
+  const float* post_gamma;
+  const float* post_beta;
+  const float* gate;
+  const float* pre_gamma;
+  const float* pre_beta;
+  float* post_mean;
+  float* post_rstd;
+  float* pre_mean;
+  float* pre_rstd;
+  DropArgs drop;
+  const void* x;
+  int64_t ldx;
+  const void* b;
+  int64_t ldb;
+  void* h;
+  int64_t ldh;
+  void* z;
+  int64_t ldz;
+  const void* dz;
+  int64_t lddz;
+  const void* dh;
+  int64_t lddh;
+  void* dx;
+  int64_t lddx;
+  void* db;
+  int64_t lddb;
+  float* d_post_gamma;
+  float* d_post_beta;
+  float* d_gate;
+  float* d_pre_gamma;
+  float* d_pre_beta;
+  int accumulate;
+  float* part;
+  int rows_per_block, nblocks;
+  int f32;
+};
+constexpr int kBnMaxH = 8192;
+// Bytes of the column sums that the backward leaves for up to a.rows rows.
+size_t block_norm_bwd_workspace(const BlockNormArgs& a);
+hipError_t launch_block_norm_fwd(const BlockNormArgs& a, hipStream_t stream);
+hipError_t launch_block_norm_bwd(const BlockNormArgs& a, hipStream_t stream);
+
+// Embedding lookup y[r] = drop(scale table[ids[r]]) and its gradient, dtable
+// (+)= scale * the sums of drop(dy) by token, through a workspace of
+// embedding_workspace bytes.
+struct EmbedArgs {
+  int64_t rows;
+  int H;
+  int64_t V;
+  const void* ids;
+  int id64;
+  const void* table;  // fwd
+  int64_t ldt;
+  void* y;            // fwd
+  const void* dy;     // bwd
+  int64_t ldy;        // of y or dy
+  float scale;
+  DropArgs drop;
+  float* dtable;
+  int64_t lddt;
+  int accumulate;
+  void* workspace;
+  int f32;
+};
+constexpr int64_t kMaxEmbedRows = (int64_t)1 << 28;
+constexpr int32_t kMaxEmbedH = 1 << 20;
+size_t embedding_workspace(int64_t rows, int H);
+hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t stream);
+hipError_t launch_embedding_bwd(const EmbedArgs& a, hipStream_t stream);
+
 }  // namespace sppo

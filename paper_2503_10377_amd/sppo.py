@@ -77,6 +77,42 @@ class sppo_copy_stats_t(ctypes.Structure):
     ]
 
 
+class sppo_drop(ctypes.Structure):
+    _fields_ = [
+        ("p", ctypes.c_float),
+        ("seed", ctypes.c_uint64),
+        ("offset", ctypes.c_uint64),
+        ("offset_dev", ctypes.c_void_p),
+        ("row0", ctypes.c_int64),
+    ]
+
+
+class sppo_block_norm(ctypes.Structure):
+    _fields_ = [
+        ("H", ctypes.c_int32),
+        ("dtype", ctypes.c_int),
+        ("post", ctypes.c_int),
+        ("pre", ctypes.c_int),
+        ("gate_kind", ctypes.c_int),
+        ("eps", ctypes.c_float),
+        ("residual_scale", ctypes.c_float),
+        ("branch_scale", ctypes.c_float),
+        ("post_gamma", ctypes.c_void_p),
+        ("post_beta", ctypes.c_void_p),
+        ("gate", ctypes.c_void_p),
+        ("pre_gamma", ctypes.c_void_p),
+        ("pre_beta", ctypes.c_void_p),
+    ]
+
+
+class sppo_block_norm_stats(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("post_mean", "post_rstd", "pre_mean", "pre_rstd")]
+
+
+class sppo_block_norm_grads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("post_gamma", "post_beta", "gate", "pre_gamma", "pre_beta")]
+
+
 KERNELS = ("fwd", "bwd_pre", "bwd_dkdv", "bwd_dq")
 
 
@@ -147,6 +183,24 @@ def lib() -> ctypes.CDLL:
                                              I32, I32, ctypes.c_int, ctypes.c_float, I32, VP, VP, VP, VP, VP, VP,
                                              VP, VP, VP, VP], ctypes.c_int),
             "sppo_attn_finalize_chunk": ([P, I32, VP, VP, VP, VP, VP], ctypes.c_int),
+            "sppo_dropout": ([ctypes.c_int, ctypes.c_int64, I32, VP, ctypes.c_int64, VP, ctypes.c_int64,
+                              ctypes.POINTER(sppo_drop), VP, ctypes.c_int64, VP], ctypes.c_int),
+            "sppo_block_norm_fwd": ([ctypes.POINTER(sppo_block_norm), ctypes.c_int64, ctypes.POINTER(sppo_drop), VP,
+                                     ctypes.c_int64, VP, ctypes.c_int64, VP, ctypes.c_int64, VP, ctypes.c_int64,
+                                     ctypes.POINTER(sppo_block_norm_stats), VP], ctypes.c_int),
+            "sppo_block_norm_bwd_workspace": ([ctypes.POINTER(sppo_block_norm), ctypes.c_int64], ctypes.c_size_t),
+            "sppo_block_norm_bwd": ([ctypes.POINTER(sppo_block_norm), ctypes.c_int64, ctypes.POINTER(sppo_drop), VP,
+                                     ctypes.c_int64, VP, ctypes.c_int64, ctypes.POINTER(sppo_block_norm_stats), VP,
+                                     ctypes.c_int64, VP, ctypes.c_int64, VP, ctypes.c_int64, VP, ctypes.c_int64,
+                                     ctypes.POINTER(sppo_block_norm_grads), I32, VP, ctypes.c_size_t, VP],
+                                    ctypes.c_int),
+            "sppo_embedding_fwd": ([ctypes.c_int, ctypes.c_int, ctypes.c_int64, I32, ctypes.c_int64, VP, VP,
+                                    ctypes.c_int64, ctypes.c_float, ctypes.POINTER(sppo_drop), VP, ctypes.c_int64,
+                                    VP], ctypes.c_int),
+            "sppo_embedding_bwd_workspace": ([ctypes.c_int64, I32], ctypes.c_size_t),
+            "sppo_embedding_bwd": ([ctypes.c_int, ctypes.c_int, ctypes.c_int64, I32, ctypes.c_int64, VP, VP,
+                                    ctypes.c_int64, ctypes.c_float, ctypes.POINTER(sppo_drop), VP, ctypes.c_int64,
+                                    I32, VP, ctypes.c_size_t, VP], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -438,3 +492,83 @@ def sppo_transpose_bf16(x, y, rows, cols, stream=None):
 
 def sppo_pack_qkv_grad(rows, wq, wkv, dq, dk, dv, row0, out, stream=None):
     _plain(lib().sppo_pack_qkv_grad(rows, wq, wkv, _ptr(dq), _ptr(dk), _ptr(dv), row0, _ptr(out), _stream(stream)))
+
+
+# -------------------------------------------------------- training operators
+NORMS = {"none": 0, "layer": 1, "rms": 2}
+GATES = {"none": 0, "channel": 1, "token": 2}
+DTYPES = {"bf16": SPPO_BF16, "f32": SPPO_F32, "fp32": SPPO_F32}
+ID_TYPES = {"i32": 0, "i64": 1}
+
+
+def _context_free(status: int):
+    if status != SPPO_OK:
+        raise SppoError(status, lib().sppo_last_error(None).decode())
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def drop_spec(p, seed, offset=0, row0=0, offset_dev=None) -> sppo_drop:
+    """The dropout of a call whose first row is the sequence's row ``row0``;
+    offset_dev: a device uint64 (int64 tensor) added to ``offset``."""
+    return sppo_drop(p, seed, offset, _ptr(offset_dev), row0)
+
+
+def block_norm(H, dtype="bf16", post="none", pre="none", gate_kind="none", eps=1e-5, residual_scale=1.0,
+               branch_scale=1.0, post_gamma=None, post_beta=None, gate=None, pre_gamma=None,
+               pre_beta=None) -> sppo_block_norm:
+    """The description of a block's end.  Holds addresses only: the tensors
+    must outlive its use."""
+    return sppo_block_norm(H, DTYPES.get(dtype, dtype), NORMS.get(post, post), NORMS.get(pre, pre),
+                           GATES.get(gate_kind, gate_kind), eps, residual_scale, branch_scale, _ptr(post_gamma),
+                           _ptr(post_beta), _ptr(gate), _ptr(pre_gamma), _ptr(pre_beta))
+
+
+def block_norm_stats(post_mean=None, post_rstd=None, pre_mean=None, pre_rstd=None) -> sppo_block_norm_stats:
+    return sppo_block_norm_stats(_ptr(post_mean), _ptr(post_rstd), _ptr(pre_mean), _ptr(pre_rstd))
+
+
+def block_norm_grads(post_gamma=None, post_beta=None, gate=None, pre_gamma=None,
+                     pre_beta=None) -> sppo_block_norm_grads:
+    return sppo_block_norm_grads(_ptr(post_gamma), _ptr(post_beta), _ptr(gate), _ptr(pre_gamma), _ptr(pre_beta))
+
+
+def sppo_dropout(rows, cols, x, ldx, drop, y, ldy, res=None, ldres=0, dtype="bf16", stream=None):
+    _context_free(lib().sppo_dropout(DTYPES.get(dtype, dtype), rows, cols, _ptr(x), ldx, _ptr(res), ldres, _ref(drop),
+                                     _ptr(y), ldy, _stream(stream)))
+
+
+def sppo_block_norm_fwd(bn, rows, drop, x, ldx, b, ldb, h, ldh, z, ldz, stats, stream=None):
+    _context_free(lib().sppo_block_norm_fwd(_ref(bn), rows, _ref(drop), _ptr(x), ldx, _ptr(b), ldb, _ptr(h), ldh,
+                                            _ptr(z), ldz, _ref(stats), _stream(stream)))
+
+
+def sppo_block_norm_bwd_workspace(bn, rows) -> int:
+    return int(lib().sppo_block_norm_bwd_workspace(_ref(bn), rows))
+
+
+def sppo_block_norm_bwd(bn, rows, drop, b, ldb, h, ldh, stats, dz, lddz, dh, lddh, dx, lddx, db, lddb, grads,
+                        workspace, workspace_bytes, accumulate=1, stream=None):
+    _context_free(lib().sppo_block_norm_bwd(_ref(bn), rows, _ref(drop), _ptr(b), ldb, _ptr(h), ldh, _ref(stats),
+                                            _ptr(dz), lddz, _ptr(dh), lddh, _ptr(dx), lddx, _ptr(db), lddb,
+                                            _ref(grads), int(accumulate), _ptr(workspace), workspace_bytes,
+                                            _stream(stream)))
+
+
+def sppo_embedding_fwd(rows, H, V, ids, table, ldt, scale, drop, y, ldy, dtype="bf16", id_type="i64", stream=None):
+    _context_free(lib().sppo_embedding_fwd(DTYPES.get(dtype, dtype), ID_TYPES.get(id_type, id_type), rows, H, V,
+                                           _ptr(ids), _ptr(table), ldt, scale, _ref(drop), _ptr(y), ldy,
+                                           _stream(stream)))
+
+
+def sppo_embedding_bwd_workspace(rows, H) -> int:
+    return int(lib().sppo_embedding_bwd_workspace(rows, H))
+
+
+def sppo_embedding_bwd(rows, H, V, ids, dy, lddy, scale, drop, dtable, lddt, workspace, workspace_bytes,
+                       accumulate=1, dtype="bf16", id_type="i64", stream=None):
+    _context_free(lib().sppo_embedding_bwd(DTYPES.get(dtype, dtype), ID_TYPES.get(id_type, id_type), rows, H, V,
+                                           _ptr(ids), _ptr(dy), lddy, scale, _ref(drop), _ptr(dtable), lddt,
+                                           int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
