@@ -579,7 +579,7 @@ sppo_status sppo_block_norm_bwd(const sppo_block_norm* bn, int64_t rows, const s
  * ids [rows] of id_type.  An id outside [0, V) (padding, another rank's part
  * of a split vocabulary) gives a row of zeros, and nothing is read for it.
  * drop: NULL for none (W = H).  rows <= 2^28, V < 2^31, H <= 2^20
- * (UNSUPPORTED otherwise). */
+ * and rows * H <= 2^38 (UNSUPPORTED otherwise; the gradient's too). */
 typedef enum { SPPO_I32 = 0, SPPO_I64 = 1 } sppo_id_type;
 sppo_status sppo_embedding_fwd(sppo_dtype dtype, sppo_id_type id_type, int64_t rows, int32_t H, int64_t V,
                                const void* ids, const void* table, int64_t ldt, float scale, const sppo_drop* drop,

@@ -58,6 +58,32 @@ __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedArgs a, FastDi
   }
 }
 
+// ------------------------------------------------------------------ zeros
+// Overwriting starts from a table of zeros (rows with tokens are written
+// again later).  The fill is the largest stream of bytes of the backward and
+// nothing before the sums needs it, so it rides along with the sort: the sort's
+// few workgroups come first in each launch, the others clear a part of the table.
+struct ZeroArgs {
+  float* table;
+  int64_t ld, v0, v1;  // rows [v0, v1)
+  int H;
+};
+
+// The share of block `block` of `blocks`, in pieces of 16 bytes.
+template <int NT>
+__device__ __forceinline__ void zero_rows(const ZeroArgs& z, int64_t block, int64_t blocks) {
+  const int64_t per_row = z.H / 4, stride = blocks * NT;
+  const int64_t dr = stride / per_row, dc = stride - dr * per_row, i = block * NT + threadIdx.x;
+  int64_t r = i / per_row, c = i - r * per_row;
+  for (r += z.v0; r < z.v1; r += dr, c += dc) {
+    if (c >= per_row) {
+      c -= per_row;
+      if (++r >= z.v1) return;
+    }
+    *reinterpret_cast<f32x4*>(z.table + r * z.ld + 4 * c) = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
 // ------------------------------------------------------------------ the sort
 // Least significant digit first, up to kMaxDigitBits bits a pass.  The keys
 // are cut into at most kMaxSortTiles tiles, one workgroup each; a pass counts
@@ -87,8 +113,12 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& s, int64_t i) {
   return s.key ? s.key[i] : token(s.ids, s.id64, i, s.V);
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs s) {
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs s, ZeroArgs z) {
   __shared__ uint32_t cnt[kMaxDigits];
+  if ((int)blockIdx.x >= s.tiles) {
+    zero_rows<kSortThreads>(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    return;
+  }
   const int digits = 1 << s.bits;
   for (int d = threadIdx.x; d < digits; d += kSortThreads) cnt[d] = 0;
   __syncthreads();
@@ -100,7 +130,28 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs s) {
   for (int d = threadIdx.x; d < digits; d += kSortThreads) s.counts[(int64_t)blockIdx.x * digits + d] = cnt[d];
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s) {
+// The rank of a key among the wave's keys with the same digit: those of the
+// wave's earlier rounds (the counter), then the lanes below.  Lanes without a
+// key take part with in = false.
+__device__ __forceinline__ uint32_t wave_rank(uint32_t d, int bits, bool in, uint32_t* cnt) {
+  const int lane = threadIdx.x & 63;
+  uint64_t same = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t ones = __ballot((d >> b) & 1);
+    same &= (d >> b) & 1 ? ones : ~ones;
+  }
+  const int first = in ? __ffsll((unsigned long long)same) - 1 : lane;
+  uint32_t old = 0;
+  if (in && lane == first) old = atomicAdd(&cnt[d], (uint32_t)__popcll(same));
+  old = __shfl(old, first);
+  return old + __popcll(same & (((uint64_t)1 << lane) - 1));
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, ZeroArgs z) {
+  if ((int)blockIdx.x >= s.tiles) {
+    zero_rows<kSortThreads>(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    return;
+  }
   __shared__ uint32_t base[kMaxDigits];             // next place of each digit of this tile
   __shared__ uint32_t cnt[kSortWaves][kMaxDigits];  // keys of each digit in a wave, then their first place
   __shared__ uint32_t wsum[kSortWaves];
@@ -135,9 +186,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s) 
     for (int u = 0; u < kSortWaves; ++u)
       if (tid < digits) cnt[u][tid] = 0;
     __syncthreads();
-    // A wave holds kSortKeys times 64 consecutive keys; a key's rank among
-    // the wave's keys of its digit: those of earlier rounds (the counter),
-    // and the lanes below with the same digit.
+    // a wave holds kSortKeys times 64 consecutive keys
     uint32_t key[kSortKeys], row[kSortKeys], rank[kSortKeys];
 #pragma unroll
     for (int u = 0; u < kSortKeys; ++u) {
@@ -146,16 +195,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s) 
       key[u] = in ? sort_key(s, i) : 0;
       row[u] = in ? (s.key ? s.row[i] : (uint32_t)i) : 0;
       const uint32_t d = (key[u] >> s.shift) & (digits - 1);
-      uint64_t same = __ballot(in);
-      for (int b = 0; b < s.bits; ++b) {
-        const uint64_t ones = __ballot((d >> b) & 1);
-        same &= (d >> b) & 1 ? ones : ~ones;
-      }
-      const int first = in ? __ffsll((unsigned long long)same) - 1 : lane;
-      uint32_t old = 0;
-      if (in && lane == first) old = atomicAdd(&cnt[w][d], (uint32_t)__popcll(same));
-      old = __shfl(old, first);
-      rank[u] = old + __popcll(same & (((uint64_t)1 << lane) - 1));
+      rank[u] = wave_rank(d, s.bits, in, cnt[w]);
     }
     __syncthreads();
     if (tid < digits) {
@@ -182,96 +222,199 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s) 
   }
 }
 
+// Up to kSmallKeys keys every compute unit has to itself: the place of row i is
+// the number of rows j with (token_j, j) < (token_i, i), counted over all rows,
+// which a workgroup holds in LDS.  n^2 comparisons of two instructions beat the
+// passes of a sort (four launches of 5 us for 8192 rows) while launches and
+// their gaps are what costs: 11 us for 8192 rows.
+constexpr int kSmallKeys = 16384, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
+
+// split: lanes that share a row's comparisons (1, 2 or 4); a workgroup ranks
+// 64 / split rows, its waves and their lane groups taking blocks of 64 rows j
+// in turn.  In a block before row i's own an equal token counts, in one after
+// it doesn't: the comparison is against token_i + 1 or token_i.
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs s, int split, ZeroArgs z) {
+  __shared__ __attribute__((aligned(16))) uint32_t key[kSmallKeys];
+  __shared__ uint32_t place[64];
+  if ((int)blockIdx.x >= s.tiles) {
+    zero_rows<kRankThreads>(z, blockIdx.x - s.tiles, gridDim.x - s.tiles);
+    return;
+  }
+  const int n = (int)s.n, blocks = (n + 63) / 64, tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
+  for (int i = tid; i < 64 * blocks; i += kRankThreads) key[i] = i < n ? token(s.ids, s.id64, i, s.V) : 0xffffffffu;
+  if (tid < 64) place[tid] = 0;
+  __syncthreads();
+  const int rows = 64 / split, li = lane & (rows - 1), i = blockIdx.x * rows + li;
+  const uint32_t mine = key[i];  // i < 64 * blocks: rows divides 64
+  uint32_t below = 0;
+  for (int jb = w * split + lane / rows; jb < blocks; jb += kRankWaves * split) {
+    const uint32_t* kj = key + 64 * jb;
+    if (jb != i / 64) {
+      const uint32_t bound = mine + (jb < i / 64);
+#pragma unroll
+      for (int j = 0; j < 64; j += 4) {
+        const u32x4 k4 = *reinterpret_cast<const u32x4*>(kj + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) below += k4[e] < bound;
+      }
+    } else {
+#pragma unroll 8
+      for (int j = 0; j < 64; ++j) below += kj[j] < mine + (64 * jb + j < i);
+    }
+  }
+  atomicAdd(&place[li], below);  // whole numbers: any order gives the same
+  __syncthreads();
+  if (tid < rows && i < n) {
+    s.key_out[place[tid]] = mine;
+    s.row_out[place[tid]] = (uint32_t)i;
+  }
+}
+
 // ------------------------------------------------------------------ the sums
-constexpr int kTile = 32;  // sorted rows of a workgroup
-constexpr int kSlab = kThreads * 8;  // columns of a workgroup
+// A wave takes kTile sorted places and kSlab columns; the waves of a tile come
+// one after another, so that whole rows are on their way at a time (8192 rows
+// of 4096 columns, 3300 tokens: 34 us, 5.2 TB/s; with the tiles first 41).
+// After a fill of the table it takes 44 us: the fill's last 256 MB are still
+// in the memory-side cache and leave it while the sums run (stores that go
+// past that cache make the fill 38 us longer).  A run of at most kTile
+// rows belongs to the tile where it begins, which follows it past its end, so
+// it is summed at once; only of a longer run do the tiles it crosses leave
+// partial sums.  The last places of a tile before, its own and those it may
+// follow a run to fit the wave's lanes, one each.
+constexpr int kTile = 16;
+constexpr int kSlab = 64 * 8;
+constexpr int kAhead = 4;  // rows on their way
 
 struct SumArgs {
   int64_t n;
   const uint32_t* key;  // sorted tokens (outside the table: V, at the end)
   const uint32_t* row;
-  float* part;          // [tiles][2][H]: the run that enters the tile, the run that leaves it
+  float* part;          // [tiles][2][H] of long runs: the one that enters the tile, the one that leaves it
 };
 
-__global__ __launch_bounds__(256) void embed_zero_kernel(EmbedArgs a) {
-  for (int64_t v = blockIdx.x; v < a.V; v += gridDim.x)
-    for (int c = 4 * threadIdx.x; c < a.H; c += 1024)
-      *reinterpret_cast<f32x4*>(a.dtable + v * a.lddt + c) = f32x4{0.f, 0.f, 0.f, 0.f};
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
-  const int c = blockIdx.y * kSlab + 8 * threadIdx.x;
-  if (c >= a.H) return;
-  const int64_t i0 = (int64_t)blockIdx.x * kTile, i1 = i0 + kTile < s.n ? i0 + kTile : s.n;
-  const Dropper drop(a.drop);
+// The rows' addresses depend on nothing but the sorted list, so kAhead rows
+// are read ahead, and where the sums add to the table so are its old rows, at
+// the places where runs begin (read where a run ends, each costs a trip to
+// memory).
+template <typename T, bool ADD>
+__global__ __launch_bounds__(64) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
+  const uint32_t slabs = (a.H + kSlab - 1) / kSlab, tile = blockIdx.x / slabs;
+  const int lane = threadIdx.x, c = (blockIdx.x - tile * slabs) * kSlab + 8 * lane;
+  const bool in = c < a.H;
   const uint32_t V = (uint32_t)a.V;
-  const uint32_t prev = i0 > 0 ? s.key[i0 - 1] : V;  // V: no run enters
-  const uint32_t next = i1 < s.n ? s.key[i1] : V;    // V: no run leaves
-  uint32_t cur = s.key[i0];
-  bool entered = cur == prev;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto flush = [&](bool leaves) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= a.scale;
-    if (entered || leaves) {
-      Eight<float>::store(s.part + ((int64_t)blockIdx.x * 2 + (entered ? 0 : 1)) * a.H + c, acc);
-    } else {
-      float* out = a.dtable + (int64_t)cur * a.lddt + c;
-      if (a.accumulate) {
-        float o[8];
-        load8f(out, o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += o[e];
-      }
-      Eight<float>::store(out, acc);
-    }
+  const int64_t at = (int64_t)tile * kTile - kTile + lane;  // lane kTile + u holds the tile's place u
+  const bool there = at >= 0 && at < s.n;
+  const uint32_t my_key = there ? s.key[at] : V, my_row = there ? s.row[at] : 0;
+  auto key_at = [&](int u) { return (uint32_t)__builtin_amdgcn_readlane(my_key, kTile + u); };
+  auto row_at = [&](int u) { return (uint32_t)__builtin_amdgcn_readlane(my_row, kTile + u); };
+  // the run with place u: [from, to), as far as the lanes reach
+  auto run = [&](int u, int& from, int& to) {
+    const uint64_t m = __ballot(my_key == key_at(u));
+    from = __ffsll((unsigned long long)m) - 1 - kTile;
+    to = 64 - __clzll(m) - kTile;
   };
-  for (int64_t i = i0; i < i1; ++i) {
-    const uint32_t k = s.key[i];
-    if (k != cur) {
-      flush(false);
-      cur = k;
-      entered = false;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    }
-    if (k >= V) return;
-    const uint32_t r = s.row[i];
-    Eight<T> x;
-    x.load(static_cast<const T*>(a.dy) + (int64_t)r * a.ldy + c);
-    float f[8];
-    x.get(f);
-    drop.apply((uint64_t)(a.drop.row0 + r) * (a.H / 8) + c / 8, f);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += f[e];
+  if (key_at(0) >= V) return;
+  int from, to, first = 0, stop = kTile;
+  run(0, from, to);
+  bool entered = from < 0;
+  if (entered && to - from <= kTile) {  // short: the tile before sums it
+    first = to;
+    entered = false;
   }
-  flush(cur == next);
+  bool leaves = false;  // the last run, a long one
+  if (key_at(kTile - 1) < V) {
+    run(kTile - 1, from, to);
+    if (to > kTile) {
+      if (to - from <= kTile) stop = to;
+      else leaves = true;
+    }
+  } else {
+    stop = __popcll(__ballot(lane >= kTile && lane < 2 * kTile && my_key < V));
+  }
+  const Dropper drop(a.drop);
+  Eight<T> x[kAhead];
+  Eight<float> old[ADD ? kAhead : 1];
+  auto begins = [&](int u) { return u == first || key_at(u - 1) != key_at(u); };
+  auto load = [&](int u, int slot) {
+    if (u >= stop || !in) return;
+    x[slot].load(static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy + c);
+    if constexpr (ADD)
+      if (begins(u)) old[slot].load(a.dtable + (int64_t)key_at(u) * a.lddt + c);
+  };
+#pragma unroll
+  for (int v = 0; v < kAhead; ++v) load(first + v, v);
+  float acc[8], base[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = base[e] = 0.f;
+  for (int j = first; j < stop; j += kAhead) {
+#pragma unroll
+    for (int v = 0; v < kAhead; ++v) {
+      const int u = j + v;
+      if (u >= stop) return;
+      float f[8];
+      x[v].get(f);
+      drop.apply((uint64_t)(a.drop.row0 + row_at(u)) * (a.H / 8) + c / 8, f);
+      if (begins(u)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = f[e];
+        if constexpr (ADD) old[v].get(base);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += f[e];
+      }
+      load(u + kAhead, v);
+      const bool last = u + 1 == stop;
+      if (!last && !begins(u + 1)) continue;
+      float o[8];
+      if (entered || (last && leaves)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = acc[e] * a.scale;
+        if (in) Eight<float>::store(s.part + ((int64_t)tile * 2 + (entered ? 0 : 1)) * a.H + c, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = ADD ? acc[e] * a.scale + base[e] : acc[e] * a.scale;
+        if (in) Eight<float>::store(a.dtable + (int64_t)key_at(u) * a.lddt + c, o);
+      }
+      entered = false;
+    }
+  }
 }
 
-// The run that leaves tile t (if one begins there): its partial sums, from
-// tile t's second and the following tiles' first, in tile order.
+// The long runs: the one that begins in this tile and leaves it, if there is
+// one, from the tile's second partial sum and the following tiles' first ones,
+// in kJoinGroups groups of tiles in turn and then in group order.  Most
+// workgroups find none and end after one trip to memory.
 constexpr int kJoinCols = 256, kJoinGroups = 4;
-__global__ __launch_bounds__(kJoinCols / 4 * kJoinGroups) void embed_join_kernel(EmbedArgs a, SumArgs s) {
+constexpr int kJoinThreads = kJoinCols / 4 * kJoinGroups;
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, SumArgs s) {
   __shared__ __attribute__((aligned(16))) float red[kJoinGroups][kJoinCols];
-  const int64_t t = blockIdx.x, i0 = t * kTile, last = i0 + kTile - 1;
-  if (last + 1 >= s.n) return;
-  const uint32_t k = s.key[last], V = (uint32_t)a.V;
-  if (k >= V || s.key[last + 1] != k) return;
-  if (s.key[i0] == k && i0 > 0 && s.key[i0 - 1] == k) return;  // it began before this tile
-  // the last tile the run reaches: the last place whose key is k
-  int64_t lo = last + 1, hi = s.n;  // key[lo] == k; key[hi] > k, or the end
-  while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (s.key[mid] == k) lo = mid;
-    else hi = mid;
+  const int lane = threadIdx.x & 63;
+  const int64_t t = blockIdx.x, i0 = t * kTile;
+  // lane kTile + u holds place u; lane kTile - 1 the place before
+  const int64_t at = i0 - kTile + lane;
+  const uint32_t V = (uint32_t)a.V;
+  const uint32_t mine = at >= 0 && at < s.n ? s.key[at] : V;
+  const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(mine, 2 * kTile - 1);
+  if (k >= V) return;
+  const uint64_t m = __ballot(mine == k);
+  const int from = __ffsll((unsigned long long)m) - 1 - kTile, to = 64 - __clzll(m) - kTile;
+  if (from < 0 || to <= kTile || to - from <= kTile) return;
+  int64_t end = t;  // the last tile whose last place is the run's
+  for (;;) {
+    const int64_t p = (end + 1 + lane) * kTile + kTile - 1;
+    const uint64_t no = ~__ballot(p < s.n && s.key[p] == k);
+    if (no) {
+      end += __ffsll((unsigned long long)no) - 1;
+      break;
+    }
+    end += 64;
   }
-  const int64_t end = lo / kTile;
+  if ((end + 1) * kTile < s.n && s.key[(end + 1) * kTile] == k) ++end;  // it ends inside the next one
   const int lc = threadIdx.x % (kJoinCols / 4) * 4, grp = threadIdx.x / (kJoinCols / 4);
   const int c = blockIdx.y * kJoinCols + lc;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   if (c < a.H) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t u = t + grp; u <= end; u += kJoinGroups)
       sum += *reinterpret_cast<const f32x4*>(s.part + (u * 2 + (u == t ? 1 : 0)) * a.H + c);
   }
@@ -337,30 +480,61 @@ hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
   s.ids = a.ids;
   s.id64 = a.id64;
   s.V = a.V;
+  const int launches = a.rows <= kSmallKeys ? 1 : 2 * passes;  // of the sort: each clears its part of the table
+  int part = 0;
+  auto zeros = [&]() {
+    ZeroArgs z{a.dtable, a.lddt, a.V * part / launches, a.V * (part + 1) / launches, a.H};
+    ++part;
+    if (a.accumulate) z.v0 = z.v1;
+    return z;
+  };
+  // workgroups of nt threads that clear z: 32 pieces a thread, at most four a compute unit
+  auto zero_blocks = [&](const ZeroArgs& z, int64_t nt) {
+    const int64_t b = ((z.v1 - z.v0) * (z.H / 4) + 32 * nt - 1) / (32 * nt), most = 4 * (int64_t)device_cus();
+    return (unsigned)(b < most ? b : most);
+  };
   hipError_t e;
-  if (!a.accumulate) {
-    hipLaunchKernelGGL(embed_zero_kernel, dim3((unsigned)(a.V < 65536 ? a.V : 65536)), dim3(256), 0, stream, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  for (int i = 0, at = 0; i < passes; ++i) {
-    s.shift = at;
-    s.bits = (bits - at + passes - i - 1) / (passes - i);
-    at += s.bits;
-    s.key_out = arr[2 * (i & 1)];
-    s.row_out = arr[2 * (i & 1) + 1];
-    hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)s.tiles), dim3(kSortThreads), 0, stream, s);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(sort_scatter_kernel, dim3((unsigned)s.tiles), dim3(kSortThreads), 0, stream, s);
+  if (a.rows <= kSmallKeys) {
+    s.key_out = arr[0];
+    s.row_out = arr[1];
+    // the fewest rows a workgroup that leave no compute unit without one
+    const int split = a.rows <= 16 * (int64_t)device_cus() ? 4 : a.rows <= 32 * (int64_t)device_cus() ? 2 : 1;
+    s.tiles = (int)((a.rows * split + 63) / 64);
+    const ZeroArgs z = zeros();
+    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)s.tiles + zero_blocks(z, kRankThreads)), dim3(kRankThreads), 0,
+                       stream, s, split, z);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     s.key = s.key_out;
     s.row = s.row_out;
+  } else {
+    for (int i = 0, at = 0; i < passes; ++i) {
+      s.shift = at;
+      s.bits = (bits - at + passes - i - 1) / (passes - i);
+      at += s.bits;
+      s.key_out = arr[2 * (i & 1)];
+      s.row_out = arr[2 * (i & 1) + 1];
+      ZeroArgs z = zeros();
+      hipLaunchKernelGGL(sort_count_kernel, dim3((unsigned)s.tiles + zero_blocks(z, kSortThreads)), dim3(kSortThreads),
+                         0, stream, s, z);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      z = zeros();
+      hipLaunchKernelGGL(sort_scatter_kernel, dim3((unsigned)s.tiles + zero_blocks(z, kSortThreads)),
+                         dim3(kSortThreads), 0, stream, s, z);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      s.key = s.key_out;
+      s.row = s.row_out;
+    }
   }
   SumArgs u{a.rows, s.key, s.row, reinterpret_cast<float*>(ws + p.part)};
-  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3((unsigned)p.tiles, (unsigned)((a.H + kSlab - 1) / kSlab)),
-                     dim3(kThreads), 0, stream, a, u);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)p.tiles, (unsigned)((a.H + kJoinCols - 1) / kJoinCols)),
-                     dim3(kJoinCols / 4 * kJoinGroups), 0, stream, a, u);
+  const dim3 grid((unsigned)(p.tiles * ((a.H + kSlab - 1) / kSlab)));
+  if (a.accumulate)
+    hipLaunchKernelGGL((embed_sum_kernel<T, true>), grid, dim3(64), 0, stream, a, u);
+  else
+    hipLaunchKernelGGL((embed_sum_kernel<T, false>), grid, dim3(64), 0, stream, a, u);
+  if ((e = hipGetLastError()) != hipSuccess || a.rows <= kTile) return e;  // no long run
+  hipLaunchKernelGGL(embed_join_kernel,
+                     dim3((unsigned)p.tiles, (unsigned)((a.H + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
+                     stream, a, u);
   return hipGetLastError();
 }
 

@@ -109,8 +109,8 @@ sppo_status check_embedding(int dtype, int id_type, int64_t rows, int32_t H, int
   if (!ids || !aligned(ids, id_type == SPPO_I64 ? 8 : 4))
     return fail(SPPO_ERR_INVALID_ARG, "embedding: null or misaligned ids");
   if (!std::isfinite(scale)) return fail(SPPO_ERR_INVALID_ARG, "embedding: the scale is not finite");
-  if (rows > sppo::kMaxEmbedRows || V > INT32_MAX || H > sppo::kMaxEmbedH)
-    return fail(SPPO_ERR_UNSUPPORTED, "embedding: rows above 2^28, V above 2^31 - 1 or H above 2^20");
+  if (rows > sppo::kMaxEmbedRows || V > INT32_MAX || H > sppo::kMaxEmbedH || rows > sppo::kMaxEmbedElems / H)
+    return fail(SPPO_ERR_UNSUPPORTED, "embedding: rows above 2^28, V above 2^31 - 1, H above 2^20 or rows * H above 2^38");
   return SPPO_OK;
 }
 
@@ -221,7 +221,8 @@ sppo_status sppo_embedding_fwd(sppo_dtype dtype, sppo_id_type id_type, int64_t r
 }
 
 size_t sppo_embedding_bwd_workspace(int64_t rows, int32_t H) {
-  if (rows <= 0 || rows > sppo::kMaxEmbedRows || H <= 0 || H % 8 || H > sppo::kMaxEmbedH) return 0;
+  if (rows <= 0 || rows > sppo::kMaxEmbedRows || H <= 0 || H % 8 || H > sppo::kMaxEmbedH || rows > sppo::kMaxEmbedElems / H)
+    return 0;
   return sppo::embedding_workspace(rows, H);
 }
 

@@ -544,6 +544,9 @@ def make_ids(rows, V, kind, seed):
         ids = g.permutation(V)[:rows] if rows <= V else g.permutation(rows) % V
     elif kind == "zipf":
         ids = np.minimum(np.exp(g.random(rows) * np.log(V + 1.0)).astype(np.int64) - 1, V - 1)
+    elif kind == "runs":  # every run length from 1 to 40, beginning at every place of a tile, rows shuffled
+        n = g.integers(1, 41, size=rows)
+        ids = g.permutation(np.repeat(np.arange(rows), n)[:rows] % V)
     else:  # padding and ids of other ranks' parts, also past 32 bits
         ids = g.integers(-3, V + 3, size=rows)
     return ids.astype(np.int64)
@@ -562,6 +565,12 @@ EMBED_CASES = [
     (4099, 256, 33000, "bf16", "i32", "zipf", 0.1, 1.0),
     (300001, 8, 300000, "bf16", "i64", "zipf", 0.0, 1.0),  # three passes of the sort, several steps a tile
     (150000, 16, 3, "f32", "i32", "outside", 0.3, 1.0),
+    (4096, 24, 4096, "bf16", "i32", "runs", 0.0, 1.0),     # the ranking with 4, 2 and 1 lanes a row
+    (8191, 16, 9000, "f32", "i64", "runs", 0.0, 1.0),
+    (16384, 8, 20000, "f32", "i64", "runs", 0.0, 1.0),
+    (16385, 512, 20000, "bf16", "i64", "runs", 0.0, 1.0),  # one more than it takes
+    (16, 16, 4, "f32", "i64", "same", 0.0, 1.0),
+    (17, 16, 4, "f32", "i64", "same", 0.0, 1.0),
 ]
 
 

@@ -191,6 +191,7 @@ def test_block_norm_workspace_grows_with_rows():
     (dict(ids=A + 4), BAD), (dict(dtype=4), BAD), (dict(id_type=2), BAD), (dict(scale=float("nan")), BAD),
     (dict(act=None), BAD), (dict(act=A + 8), BAD), (dict(ld=56), BAD), (dict(table=None), BAD), (dict(table=A + 4), BAD),
     (dict(ldt=60), BAD), (dict(p=1.0), BAD), (dict(rows=(1 << 28) + 1), UNSUP), (dict(V=1 << 31), UNSUP),
+    (dict(rows=1 << 28, H=1032, ld=1032, ldt=1032), UNSUP),
     (dict(H=(1 << 20) + 8, ld=1 << 21, ldt=1 << 21), UNSUP),
 ])
 def test_embedding_refuses(change, status):
