@@ -521,7 +521,7 @@ typedef struct {
   sppo_dtype dtype;
   sppo_norm post, pre;
   sppo_gate gate_kind;
-  float eps;                /* > 0 where there is a norm                    */
+  float eps;                /* where there is a norm: > 0, a normal number  */
   float residual_scale, branch_scale;  /* finite                            */
   const float* post_gamma;  /* [H], needed unless post is NONE              */
   const float* post_beta;   /* [H] or NULL                                  */

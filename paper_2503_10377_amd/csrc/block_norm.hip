@@ -13,27 +13,38 @@ namespace {
 constexpr int kNone = 0, kLayer = 1, kRms = 2;
 constexpr int kChannel = 1, kToken = 2;
 
-// Mean and 1 / sqrt(var + eps) of the row that the team holds in v.  Each wave
-// takes the mean of its own columns and the squares around it; the waves'
-// pairs are then joined (M2 = sum M2_w + n_w (mean_w - mean)^2), so one
-// exchange serves both moments and nothing cancels.  red: an LDS image for
-// this call alone until the next barrier but one (callers alternate two).
+// A team's exchange of two moments: each wave's sum and squares, its number of
+// columns and the inverse of that.
+struct alignas(16) Moments {
+  float s, q, n, inv;
+};
+
+// Fills the parts of the images that stay: the waves' columns.
 template <int TEAM, int PER>
-__device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int tid, bool rms, float eps, float* red,
-                                            float& mean, float& rstd) {
-  constexpr int NW = TEAM / 64;
-  const int wv = tid >> 6;
-  auto columns = [&](int w) {  // of wave w
+__device__ __forceinline__ void init_moments(Moments (*red)[TEAM / 64], int H, int tid) {
+  if (tid < 2 * (TEAM / 64)) {
+    const int w = tid >> 1;
     int n = 0;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int left = H - 8 * (64 * w + TEAM * p);
       n += left <= 0 ? 0 : (left < 512 ? left : 512);
     }
-    return n;
-  };
-  float s = 0.f, q = 0.f;
-  float m = 0.f;
+    red[tid & 1][w].n = (float)n;
+    red[tid & 1][w].inv = n > 0 ? 1.f / n : 0.f;
+  }
+}
+
+// Mean and 1 / sqrt(var + eps) of the row that the team holds in v.  Each wave
+// takes the mean of its own columns and the squares around it; the waves'
+// pairs are then joined (M2 = sum M2_w + n_w (mean_w - mean)^2), so one
+// exchange serves both moments and nothing cancels.  red: one of the team's
+// two images (written past the barrier that ended the reads of its last use).
+template <int TEAM, int PER>
+__device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int tid, bool rms, float inv_h, float eps,
+                                            Moments* red, float& mean, float& rstd) {
+  constexpr int NW = TEAM / 64;
+  float s = 0.f, q = 0.f, m = 0.f;
   if (!rms) {
 #pragma unroll
     for (int p = 0; p < PER; ++p)
@@ -42,8 +53,7 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
         for (int e = 0; e < 8; ++e) s += v[p][e];
       }
     s = wave_sum(s);
-    const int n = columns(wv);
-    m = n > 0 ? s / n : 0.f;
+    m = s * (NW > 1 ? red[tid >> 6].inv : inv_h);
   }
 #pragma unroll
   for (int p = 0; p < PER; ++p)
@@ -51,115 +61,140 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float d = v[p][e] - m;
-        q += d * d;
+        q = fmaf(d, d, q);
       }
     }
   q = wave_sum(q);
   if constexpr (NW > 1) {
     if ((tid & 63) == 0) {
-      red[2 * wv] = s;
-      red[2 * wv + 1] = q;
+      red[tid >> 6].s = s;
+      red[tid >> 6].q = q;
     }
     __syncthreads();
+    Moments r[NW];
     s = q = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) s += red[2 * w];
-    m = rms ? 0.f : s / H;
+    for (int w = 0; w < NW; ++w) {
+      r[w] = red[w];
+      s += r[w].s;
+    }
+    m = s * inv_h;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      q += red[2 * w + 1];
-      const int n = columns(w);
-      if (!rms && n > 0) {
-        const float d = red[2 * w] / n - m;
-        q += n * d * d;
-      }
+      const float d = fmaf(-r[w].n, m, r[w].s);  // n_w (mean_w - mean); zero for RMS, whose sums are zero
+      q += fmaf(d * r[w].inv, d, r[w].q);
     }
   }
   mean = m;
-  rstd = 1.f / sqrtf(q / H + eps);
+  rstd = __builtin_amdgcn_rsqf(fmaf(q, inv_h, eps));  // within an ulp
 }
 
-// Forward.  NT threads, teams of TEAM (the workgroup, or one wave of it).
+// Forward.  NT threads, teams of TEAM (the workgroup, or one wave of it); a
+// team takes rows in turn, so the parameters stay in its registers (read per
+// row they would be 2.5 times the activations' bytes, out of L2), with the
+// gate folded into the norm after the branch:
+//   gate n = bh (gate gamma) + gate beta.
+// The next row's x and b are on their way while a row is worked on.
 template <typename T, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   static_assert(TEAM == NT || TEAM == 64, "");
-  __shared__ float red[2][2 * (NT / 64)];
+  __shared__ Moments red[2][TEAM / 64];
+  constexpr int TEAMS = NT / TEAM;
   const int H = a.H, tid = threadIdx.x % TEAM;
-  const int64_t row = (int64_t)blockIdx.x * (NT / TEAM) + threadIdx.x / TEAM;
-  if (TEAM < NT && row >= a.rows) return;
+  const int64_t step = (int64_t)gridDim.x * TEAMS;
+  int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+  if (row >= a.rows) return;
+  if constexpr (TEAM > 64) {
+    init_moments<TEAM, PER>(red, H, tid);
+    __syncthreads();
+  }
   const Dropper drop(a.drop);
-  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  const T* b = static_cast<const T*>(a.b) + row * a.ldb;
-  Eight<T> xr[PER], br[PER];
+  const bool post = a.post != kNone, pre = a.pre != kNone;
+  const float inv_h = 1.f / H;
+  float pg[PER][8], pb[PER][8], qg[PER][8], qb[PER][8];
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int c = 8 * (tid + TEAM * p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pg[p][e] = 1.f, pb[p][e] = qg[p][e] = qb[p][e] = 0.f;
     if (c < H) {
-      br[p].load(b + c);
-      xr[p].load(x + c);
-    }
-  }
-  float v[PER][8];
-#pragma unroll
-  for (int p = 0; p < PER; ++p)
-    if (8 * (tid + TEAM * p) < H) br[p].get(v[p]);
-  float mean = 0.f, rstd = 1.f;
-  if (a.post != kNone) {
-    row_moments<TEAM, PER>(v, H, tid, a.post == kRms, a.eps, red[0], mean, rstd);
-    if (tid == 0) {
-      if (a.post == kLayer) a.post_mean[row] = mean;
-      a.post_rstd[row] = rstd;
-    }
-  }
-  const float scale = a.gate_kind == kToken ? a.bscale * a.gate[row] : a.bscale;
-  const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
-#pragma unroll
-  for (int p = 0; p < PER; ++p) {
-    const int c = 8 * (tid + TEAM * p);
-    if (c < H) {
-      float w[8];
-      if (a.post != kNone) {
-        load8f(a.post_gamma + c, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] = (v[p][e] - mean) * rstd * w[e];
-        if (a.post_beta) {
-          load8f(a.post_beta + c, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[p][e] += w[e];
-        }
-      }
+      if (post) load8f(a.post_gamma + c, pg[p]);
+      if (post && a.post_beta) load8f(a.post_beta + c, pb[p]);
       if (a.gate_kind == kChannel) {
-        load8f(a.gate + c, w);
+        float g[8];
+        load8f(a.gate + c, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] *= w[e];
+        for (int e = 0; e < 8; ++e) pg[p][e] *= g[e], pb[p][e] *= g[e];
       }
-      drop.apply(g0 + c / 8, v[p]);
-      xr[p].get(w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[p][e] = a.alpha * w[e] + scale * v[p][e];
-      Eight<T>::store(static_cast<T*>(a.h) + row * a.ldh + c, v[p]);
+      if (pre) load8f(a.pre_gamma + c, qg[p]);
+      if (pre && a.pre_beta) load8f(a.pre_beta + c, qb[p]);
     }
   }
-  if (a.pre == kNone) return;
-  row_moments<TEAM, PER>(v, H, tid, a.pre == kRms, a.eps, red[1], mean, rstd);
-  if (tid == 0) {
-    if (a.pre == kLayer) a.pre_mean[row] = mean;
-    a.pre_rstd[row] = rstd;
-  }
+  Eight<T> xn[PER], bn[PER];
+  auto load = [&](int64_t r) {
 #pragma unroll
-  for (int p = 0; p < PER; ++p) {
-    const int c = 8 * (tid + TEAM * p);
-    if (c < H) {
-      float w[8];
-      load8f(a.pre_gamma + c, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[p][e] = (v[p][e] - mean) * rstd * w[e];
-      if (a.pre_beta) {
-        load8f(a.pre_beta + c, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] += w[e];
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      if (c < H) {
+        bn[p].load(static_cast<const T*>(a.b) + r * a.ldb + c);
+        xn[p].load(static_cast<const T*>(a.x) + r * a.ldx + c);
       }
-      Eight<T>::store(static_cast<T*>(a.z) + row * a.ldz + c, v[p]);
+    }
+  };
+  load(row);
+  int ph = 0;
+  for (; row < a.rows; row += step) {
+    Eight<T> xr[PER];
+    float v[PER][8];
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      xr[p] = xn[p];
+      bn[p].get(v[p]);
+    }
+    if (row + step < a.rows) load(row + step);
+    float mean = 0.f, rstd = 1.f;
+    if (post) {
+      row_moments<TEAM, PER>(v, H, tid, a.post == kRms, inv_h, a.eps, red[ph], mean, rstd);
+      ph ^= 1;
+      if (tid == 0) {
+        if (a.post == kLayer) a.post_mean[row] = mean;
+        a.post_rstd[row] = rstd;
+      }
+    }
+    float scale = a.bscale * drop.scale;
+    if (a.gate_kind == kToken) scale *= a.gate[row];
+    const float shift = -mean * rstd;
+    const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      if (c < H) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift), pg[p][e], pb[p][e]);
+        drop.mask(g0 + c / 8, v[p]);
+        float x[8];
+        xr[p].get(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(v[p][e], scale, a.alpha * x[e]);
+        Eight<T>::store(static_cast<T*>(a.h) + row * a.ldh + c, v[p]);
+      }
+    }
+    if (!pre) continue;
+    row_moments<TEAM, PER>(v, H, tid, a.pre == kRms, inv_h, a.eps, red[ph], mean, rstd);
+    ph ^= 1;
+    if (tid == 0) {
+      if (a.pre == kLayer) a.pre_mean[row] = mean;
+      a.pre_rstd[row] = rstd;
+    }
+    const float shift2 = -mean * rstd;
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      if (c < H) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift2), qg[p][e], qb[p][e]);
+        Eight<T>::store(static_cast<T*>(a.z) + row * a.ldz + c, v[p]);
+      }
     }
   }
 }
@@ -213,60 +248,86 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
   }
 }
 
+// A team takes rows in turn with the parameters in registers (gate and gamma
+// as one) and the next row's h, dz, dh and b on their way, and adds its part of
+// the column sums row by row.
 template <typename T, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
   static_assert(TEAM == NT || TEAM == 64, "");
   constexpr int TEAMS = NT / TEAM;
-  // The team's exchanges alternate between two images: a wave writes one only
-  // past the barrier that ended the reads of its last use.
+  // the team's exchanges alternate between two images, as in the forward
   __shared__ float red[2][3 * (NT / 64)];
-  int ph = 0;
+  constexpr bool AHEAD = sizeof(T) * PER <= 4;  // two groups of fp32 leave no registers for a row ahead
   const int H = a.H, tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block;
   const int64_t r1 = r0 + a.rows_per_block < a.rows ? r0 + a.rows_per_block : a.rows;
   const Dropper drop(a.drop);
-  const Slots slots = bn_slots(a);
   const bool pre = a.pre != kNone, post = a.post != kNone;
-  const bool need_b = a.b != nullptr;
-  float sum[4][PER][8];
+  const float inv_h = 1.f / H;
+  float sum[4][PER][8], qg[PER][8], pg[PER][8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int p = 0; p < PER; ++p) {
+    const int c = 8 * (tid + TEAM * p);
 #pragma unroll
-    for (int p = 0; p < PER; ++p)
+    for (int e = 0; e < 8; ++e) {
+      pg[p][e] = 1.f;
+      qg[p][e] = sum[0][p][e] = sum[1][p][e] = sum[2][p][e] = sum[3][p][e] = 0.f;
+    }
+    if (c < H) {
+      if (pre) load8f(a.pre_gamma + c, qg[p]);
+      if (post) load8f(a.post_gamma + c, pg[p]);
+      if (a.gate_kind == kChannel) {
+        float g[8];
+        load8f(a.gate + c, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[i][p][e] = 0.f;
-  for (int64_t row = r0 + team; row < r1; row += TEAMS) {
-    Eight<T> hr[PER], br[PER], zr[PER], dr[PER];
+        for (int e = 0; e < 8; ++e) pg[p][e] *= g[e];
+      }
+    }
+  }
+  Eight<T> hn[PER], bn[PER], zn[PER], dn[PER];
+#pragma unroll
+  for (int p = 0; p < PER; ++p) hn[p].zero(), bn[p].zero(), zn[p].zero(), dn[p].zero();
+  auto load = [&](int64_t row) {
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
-      hr[p].zero(); br[p].zero(); zr[p].zero(); dr[p].zero();
       if (c < H) {
         if (pre) {
-          hr[p].load(static_cast<const T*>(a.h) + row * a.ldh + c);
-          zr[p].load(static_cast<const T*>(a.dz) + row * a.lddz + c);
+          hn[p].load(static_cast<const T*>(a.h) + row * a.ldh + c);
+          zn[p].load(static_cast<const T*>(a.dz) + row * a.lddz + c);
         }
-        if (a.dh) dr[p].load(static_cast<const T*>(a.dh) + row * a.lddh + c);
-        if (need_b) br[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
+        if (a.dh) dn[p].load(static_cast<const T*>(a.dh) + row * a.lddh + c);
+        if (a.b) bn[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
       }
     }
+  };
+  int64_t row = r0 + team;
+  if (AHEAD && row < r1) load(row);
+  int ph = 0;
+  for (; row < r1; row += TEAMS) {
+    if (!AHEAD) load(row);
+    Eight<T> hr[PER], br[PER], zr[PER];
     float D[PER][8];
 #pragma unroll
-    for (int p = 0; p < PER; ++p) dr[p].get(D[p]);
+    for (int p = 0; p < PER; ++p) {
+      hr[p] = hn[p];
+      br[p] = bn[p];
+      zr[p] = zn[p];
+      dn[p].get(D[p]);
+    }
+    if (AHEAD && row + TEAMS < r1) load(row + TEAMS);
     if (pre) {
-      const float mean = a.pre == kLayer ? a.pre_mean[row] : 0.f, rstd = a.pre_rstd[row];
+      const float rstd = a.pre_rstd[row], shift = a.pre == kLayer ? -a.pre_mean[row] * rstd : 0.f;
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        const int c = 8 * (tid + TEAM * p);
-        if (c < H) {
-          float hv[8], zv[8], gm[8];
+        if (8 * (tid + TEAM * p) < H) {
+          float hv[8], zv[8];
           hr[p].get(hv);
           zr[p].get(zv);
-          load8f(a.pre_gamma + c, gm);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float xh = (hv[e] - mean) * rstd, g = zv[e] * gm[e];
+            const float xh = fmaf(hv[e], rstd, shift), g = zv[e] * qg[p][e];
             s[0] += g;
             s[1] += g * xh;
             sum[0][p][e] += zv[e] * xh;
@@ -276,48 +337,51 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
       }
       team_sum<TEAM>(s, tid, red[ph]);
       ph ^= 1;
-      const float m1 = a.pre == kLayer ? s[0] / H : 0.f, m2 = s[1] / H;
+      const float m1 = a.pre == kLayer ? s[0] * inv_h : 0.f, m2 = s[1] * inv_h;
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        const int c = 8 * (tid + TEAM * p);
-        if (c < H) {
-          float hv[8], zv[8], gm[8];
+        if (8 * (tid + TEAM * p) < H) {
+          float hv[8], zv[8];
           hr[p].get(hv);
           zr[p].get(zv);
-          load8f(a.pre_gamma + c, gm);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) D[p][e] += rstd * (zv[e] * gm[e] - m1 - (hv[e] - mean) * rstd * m2);
+          for (int e = 0; e < 8; ++e)
+            D[p][e] += rstd * (fmaf(zv[e], qg[p][e], -m1) - fmaf(hv[e], rstd, shift) * m2);
         }
       }
     }
-    const float mean = a.post == kLayer ? a.post_mean[row] : 0.f, rstd = post ? a.post_rstd[row] : 1.f;
+    const float rstd = post ? a.post_rstd[row] : 1.f, shift = a.post == kLayer ? -a.post_mean[row] * rstd : 0.f;
     const float k = a.gate_kind == kToken ? a.gate[row] : 1.f;
+    const float scale = a.bscale * drop.scale;
     const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
-    float s[3] = {0.f, 0.f, 0.f};  // of m gamma gate_c, of that times bh (no post norm: of m b), of m beta
+    float s[3] = {0.f, 0.f, 0.f};  // of w = m gamma gate_c, of w bh (no post norm: of m b), of m beta
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
       if (c < H) {
         float o[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = a.alpha * D[p][e];
+        for (int e = 0; e < 8; ++e) {
+          o[e] = a.alpha * D[p][e];
+          D[p][e] *= scale;
+        }
         Eight<T>::store(static_cast<T*>(a.dx) + row * a.lddx + c, o);
-        drop.apply(g0 + c / 8, D[p]);
-        float bv[8], gm[8], bt[8], gc[8];
+        drop.mask(g0 + c / 8, D[p]);
+        if (a.gate_kind == kToken && post && a.post_beta) {
+          float bt[8];
+          load8f(a.post_beta + c, bt);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[2] += D[p][e] * bt[e];
+        }
+        float bv[8];
         br[p].get(bv);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) gm[e] = gc[e] = 1.f, bt[e] = 0.f;
-        if (post) load8f(a.post_gamma + c, gm);
-        if (post && a.post_beta) load8f(a.post_beta + c, bt);
-        if (a.gate_kind == kChannel) load8f(a.gate + c, gc);
-#pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float m = a.bscale * D[p][e], bh = (bv[e] - mean) * rstd;
-          const float w = m * gm[e] * gc[e];
+          const float m = D[p][e], bh = fmaf(bv[e], rstd, shift), w = m * pg[p][e];
+          const float mb = post || m != 0.f ? bh : 0.f;  // a dropped element is zero whatever b holds
           s[0] += w;
-          s[1] += m != 0.f ? w * bh : 0.f;  // a dropped element is zero whatever b holds
-          s[2] += m * bt[e];
-          sum[2][p][e] += m != 0.f ? k * m * bh : 0.f;
+          s[1] += w * mb;
+          sum[2][p][e] += (k * m) * mb;
           sum[3][p][e] += k * m;
           D[p][e] = w;
         }
@@ -328,7 +392,8 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
       ph ^= 1;
     }
     if (a.gate_kind == kToken && a.d_gate && tid == 0) a.d_gate[row] = s[1] + s[2];
-    const float m1 = a.post == kLayer ? k * s[0] / H : 0.f, m2 = k * s[1] / H;
+    const float m1 = a.post == kLayer ? s[0] * inv_h : 0.f, m2 = s[1] * inv_h;
+    const float kr = k * rstd;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
@@ -337,7 +402,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           float bv[8];
           br[p].get(bv);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) D[p][e] = rstd * (k * D[p][e] - m1 - (bv[e] - mean) * rstd * m2);
+          for (int e = 0; e < 8; ++e) D[p][e] = kr * (D[p][e] - m1 - fmaf(bv[e], rstd, shift) * m2);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) D[p][e] *= k;
@@ -347,6 +412,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
     }
   }
   // The workgroup's column sums: its teams' in team order.
+  const Slots slots = bn_slots(a);
   float* part = a.part + (int64_t)blockIdx.x * slots.n * H;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -429,9 +495,10 @@ constexpr int kMaxBlocks = 512;  // two a compute unit
 
 template <typename T, int NT, int TEAM, int PER>
 hipError_t fwd(const BlockNormArgs& a, hipStream_t stream) {
-  const int64_t teams = NT / TEAM;
-  hipLaunchKernelGGL((bn_fwd_kernel<T, NT, TEAM, PER>), dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(NT), 0,
-                     stream, a);
+  const int64_t teams = NT / TEAM, all = (a.rows + teams - 1) / teams;
+  const int64_t most = (int64_t)device_cus() * (NT < 1024 ? 1024 / NT : 1);  // 16 waves a compute unit
+  hipLaunchKernelGGL((bn_fwd_kernel<T, NT, TEAM, PER>), dim3((unsigned)(all < most ? all : most)), dim3(NT), 0, stream,
+                     a);
   return hipGetLastError();
 }
 
@@ -444,27 +511,34 @@ hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
 // Rows a workgroup works on at a time: up to 1024 columns a wave holds a row.
 int teams_of(int H) { return H <= 1024 ? 4 : 1; }
 
+// bf16 rows take two groups of eight columns a thread where they can: what a
+// wave does once per row (its share of the sums, the statistics) is half as
+// much per element (forward of 8192 x 4096 with one: 88 us).  fp32 rows have
+// twice the bytes and twice the registers per element.
 template <typename T>
 hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
+  constexpr int P = sizeof(T) == 2 ? 2 : 1;
   if (a.H <= 512) return fwd<T, 256, 64, 1>(a, stream);
   if (a.H <= 1024) return fwd<T, 256, 64, 2>(a, stream);
-  if (a.H <= 2048) return fwd<T, 256, 256, 1>(a, stream);
-  if (a.H <= 4096) return fwd<T, 512, 512, 1>(a, stream);
-  return fwd<T, 1024, 1024, 1>(a, stream);
+  if (a.H <= 2048) return fwd<T, 256 / P, 256 / P, P>(a, stream);
+  if (a.H <= 4096) return fwd<T, 512 / P, 512 / P, P>(a, stream);
+  return fwd<T, 512, 512, 2>(a, stream);  // 1024 threads would have 128 registers each, too few
 }
 
 template <typename T>
 hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
+  constexpr int P = sizeof(T) == 2 ? 2 : 1;
   if (a.H <= 512) return bwd<T, 256, 64, 1>(a, stream);
   if (a.H <= 1024) return bwd<T, 256, 64, 2>(a, stream);
-  if (a.H <= 2048) return bwd<T, 256, 256, 1>(a, stream);
-  if (a.H <= 4096) return bwd<T, 512, 512, 1>(a, stream);
-  return bwd<T, 1024, 1024, 1>(a, stream);
+  if (a.H <= 2048) return bwd<T, 256 / P, 256 / P, P>(a, stream);
+  if (a.H <= 4096) return bwd<T, 512 / P, 512 / P, P>(a, stream);
+  return bwd<T, 512, 512, 2>(a, stream);
 }
 
 int64_t bwd_blocks(int64_t rows, int H) {
   const int64_t teams = teams_of(H), groups = (rows + teams - 1) / teams;
-  return groups < kMaxBlocks ? groups : kMaxBlocks;
+  const int64_t most = H <= 4096 ? kMaxBlocks : kMaxBlocks / 2;  // past 4096 columns a workgroup fills a compute unit
+  return groups < most ? groups : most;
 }
 
 }  // namespace

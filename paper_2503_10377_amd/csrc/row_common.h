@@ -78,18 +78,28 @@ __device__ __forceinline__ void load8f(const float* p, float (&f)[8]) {
   }
 }
 
+// a ^ b ^ c in one instruction.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
+
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC 2011): ten rounds of two
-// 32 x 32 -> 64 bit products on a 128-bit counter, with a 64-bit key.
+// 32 x 32 -> 64 bit products on a 128-bit counter, with a 64-bit key.  The
+// products (v_mad_u64_u32, a quarter of the rate) are what it costs.  The seed
+// has to be the same for the whole wave.
 __device__ __forceinline__ u32x4 philox(uint64_t counter, uint64_t offset, uint64_t seed) {
   uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32);
   uint32_t c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
   uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+  // The rounds' keys are added up here, by the scalar unit: kept across a
+  // kernel's loop they would take 18 scalar registers, which it then lacks.
+  asm volatile("" : "+s"(k0), "+s"(k1));
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
     const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+    c0 = xor3((uint32_t)(p1 >> 32), c1, k0);
     c1 = (uint32_t)p1;
-    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+    c2 = xor3((uint32_t)(p0 >> 32), c3, k1);
     c3 = (uint32_t)p0;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -101,19 +111,25 @@ __device__ __forceinline__ u32x4 philox(uint64_t counter, uint64_t offset, uint6
 struct Dropper {
   uint64_t seed, offset;
   uint32_t t16;  // threshold in the high half word; 0: everything is kept
-  float scale;
+  float scale;   // of the kept elements
   __device__ __forceinline__ explicit Dropper(const DropArgs& d)
-      : seed(d.seed), offset(d.offset), t16(d.threshold << 16), scale(d.scale) {
+      : seed(d.seed), offset(d.offset), t16(d.threshold << 16), scale(d.threshold ? d.scale : 1.f) {
     if (d.offset_dev) offset += *d.offset_dev;
   }
-  // f (the elements 8 g .. 8 g + 7 of the whole sequence) with the dropped
-  // ones zero and the others scaled.  A half word is compared in the upper
-  // half of a word: the low one shifted there, the high one where it is.
-  __device__ __forceinline__ void apply(uint64_t g, float (&f)[8]) const {
+  // f: the elements 8 g .. 8 g + 7 of the whole sequence; the dropped ones
+  // become zero, the others are left for the caller to scale.
+  __device__ __forceinline__ void mask(uint64_t g, float (&f)[8]) const {
     if (t16 == 0) return;
     const u32x4 w = philox(g, offset, seed);
+    const uint16_t t = (uint16_t)(t16 >> 16);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = (e & 1 ? w[e >> 1] : w[e >> 1] << 16) >= t16 ? f[e] * scale : 0.f;
+    for (int e = 0; e < 8; ++e)
+      f[e] = (e & 1 ? w[e >> 1] >= t16 : (uint16_t)w[e >> 1] >= t) ? f[e] : 0.f;
+  }
+  __device__ __forceinline__ void apply(uint64_t g, float (&f)[8]) const {
+    mask(g, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= scale;
   }
 };
 

@@ -58,8 +58,8 @@ sppo_status check_norm(const sppo_block_norm* bn, int64_t rows) {
   if (post < SPPO_NORM_NONE || post > SPPO_NORM_RMS || pre < SPPO_NORM_NONE || pre > SPPO_NORM_RMS ||
       gate < SPPO_GATE_NONE || gate > SPPO_GATE_TOKEN)
     return fail(SPPO_ERR_INVALID_ARG, "block norm: unknown norm or gate");
-  if ((post != SPPO_NORM_NONE || pre != SPPO_NORM_NONE) && !(bn->eps > 0.f && std::isfinite(bn->eps)))
-    return fail(SPPO_ERR_INVALID_ARG, "block norm: eps must be positive");
+  if ((post != SPPO_NORM_NONE || pre != SPPO_NORM_NONE) && !(bn->eps > 0.f && std::isnormal(bn->eps)))
+    return fail(SPPO_ERR_INVALID_ARG, "block norm: eps must be positive and a normal number");
   if (!std::isfinite(bn->residual_scale) || !std::isfinite(bn->branch_scale))
     return fail(SPPO_ERR_INVALID_ARG, "block norm: a scale is not finite");
   if ((post != SPPO_NORM_NONE && !bn->post_gamma) || (pre != SPPO_NORM_NONE && !bn->pre_gamma) ||

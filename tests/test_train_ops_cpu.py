@@ -139,7 +139,7 @@ FULL = dict(post="layer", pre="layer", gate_kind="channel", post_gamma=A, post_b
 
 @pytest.mark.parametrize("change,status", [
     (dict(H=12), BAD), (dict(H=8200), BAD), (dict(H=0), BAD), (dict(dtype=9), BAD), (dict(post=3), BAD),
-    (dict(pre=-1), BAD), (dict(gate_kind=7), BAD), (dict(eps=0.0), BAD), (dict(eps=float("inf")), BAD),
+    (dict(pre=-1), BAD), (dict(gate_kind=7), BAD), (dict(eps=0.0), BAD), (dict(eps=float("inf")), BAD), (dict(eps=1e-40), BAD),
     (dict(residual_scale=float("nan")), BAD), (dict(branch_scale=float("inf")), BAD), (dict(post_gamma=None), BAD),
     (dict(pre_gamma=None), BAD), (dict(gate=None), BAD), (dict(pre_beta=A + 2), BAD),
 ])
