@@ -111,6 +111,18 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   const Dropper drop(a.drop);
   const bool post = a.post != kNone, pre = a.pre != kNone;
   const float inv_h = 1.f / H;
+  Eight<T> xn[PER], bn[PER];
+  auto load = [&](int64_t r) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int c = 8 * (tid + TEAM * p);
+      if (c < H) {
+        bn[p].load(static_cast<const T*>(a.b) + r * a.ldb + c);
+        xn[p].load(static_cast<const T*>(a.x) + r * a.ldx + c);
+      }
+    }
+  };
+  load(row);  // on its way before the parameters
   float pg[PER][8], pb[PER][8], qg[PER][8], qb[PER][8];
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
@@ -130,18 +142,6 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       if (pre && a.pre_beta) load8f(a.pre_beta + c, qb[p]);
     }
   }
-  Eight<T> xn[PER], bn[PER];
-  auto load = [&](int64_t r) {
-#pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const int c = 8 * (tid + TEAM * p);
-      if (c < H) {
-        bn[p].load(static_cast<const T*>(a.b) + r * a.ldb + c);
-        xn[p].load(static_cast<const T*>(a.x) + r * a.ldx + c);
-      }
-    }
-  };
-  load(row);
   int ph = 0;
   for (; row < a.rows; row += step) {
     Eight<T> xr[PER];
@@ -251,40 +251,21 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
 // A team takes rows in turn with the parameters in registers (gate and gamma
 // as one) and the next row's h, dz, dh and b on their way, and adds its part of
 // the column sums row by row.
-template <typename T, int NT, int TEAM, int PER>
+template <typename T, bool POST, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
-  static_assert(TEAM == NT || TEAM == 64, "");
   constexpr int TEAMS = NT / TEAM;
   // the team's exchanges alternate between two images, as in the forward
-  __shared__ float red[2][3 * (NT / 64)];
+  __shared__ float red_all[TEAMS][2][3 * (TEAM / 64)];
+  auto& red = red_all[threadIdx.x / TEAM];
   constexpr bool AHEAD = sizeof(T) * PER <= 4;  // two groups of fp32 leave no registers for a row ahead
   const int H = a.H, tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block;
   const int64_t r1 = r0 + a.rows_per_block < a.rows ? r0 + a.rows_per_block : a.rows;
   const Dropper drop(a.drop);
-  const bool pre = a.pre != kNone, post = a.post != kNone;
-  const float inv_h = 1.f / H;
-  float sum[4][PER][8], qg[PER][8], pg[PER][8];
-#pragma unroll
-  for (int p = 0; p < PER; ++p) {
-    const int c = 8 * (tid + TEAM * p);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      pg[p][e] = 1.f;
-      qg[p][e] = sum[0][p][e] = sum[1][p][e] = sum[2][p][e] = sum[3][p][e] = 0.f;
-    }
-    if (c < H) {
-      if (pre) load8f(a.pre_gamma + c, qg[p]);
-      if (post) load8f(a.post_gamma + c, pg[p]);
-      if (a.gate_kind == kChannel) {
-        float g[8];
-        load8f(a.gate + c, g);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pg[p][e] *= g[e];
-      }
-    }
-  }
+  const bool pre = a.pre != kNone;
+  const float inv_h = 1.f / H, scale = a.bscale * drop.scale;
   Eight<T> hn[PER], bn[PER], zn[PER], dn[PER];
+  float st[5] = {1.f, 0.f, 1.f, 0.f, 1.f};  // the row's statistics and gate
 #pragma unroll
   for (int p = 0; p < PER; ++p) hn[p].zero(), bn[p].zero(), zn[p].zero(), dn[p].zero();
   auto load = [&](int64_t row) {
@@ -300,12 +281,39 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
         if (a.b) bn[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
       }
     }
+    if (pre) st[0] = a.pre_rstd[row];
+    if (a.pre == kLayer) st[1] = a.pre_mean[row];
+    if (POST) st[2] = a.post_rstd[row];
+    if (a.post == kLayer) st[3] = a.post_mean[row];
+    if (a.gate_kind == kToken) st[4] = a.gate[row];
   };
   int64_t row = r0 + team;
-  if (AHEAD && row < r1) load(row);
+  if (row < r1) load(row);  // on its way before the parameters
+  float sum[4][PER][8], qg[PER][8], pg[PER][8];
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int c = 8 * (tid + TEAM * p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      pg[p][e] = 1.f;
+      qg[p][e] = sum[0][p][e] = sum[1][p][e] = sum[2][p][e] = sum[3][p][e] = 0.f;
+    }
+    if (c < H) {
+      if (pre) load8f(a.pre_gamma + c, qg[p]);
+      if (POST) load8f(a.post_gamma + c, pg[p]);
+      if (a.gate_kind == kChannel) {
+        float g[8];
+        load8f(a.gate + c, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pg[p][e] *= g[e];
+      }
+    }
+  }
   int ph = 0;
-  for (; row < r1; row += TEAMS) {
-    if (!AHEAD) load(row);
+  // Teams of several waves meet at the workgroup's barriers: all go round as
+  // often as the first (a team without a row has zeros, which add nothing).
+  for (; TEAM > 64 && TEAMS > 1 ? row - team < r1 : row < r1; row += TEAMS) {
+    const bool real = row < r1;
     Eight<T> hr[PER], br[PER], zr[PER];
     float D[PER][8];
 #pragma unroll
@@ -315,9 +323,16 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
       zr[p] = zn[p];
       dn[p].get(D[p]);
     }
-    if (AHEAD && row + TEAMS < r1) load(row + TEAMS);
+    const float rstd1 = st[0], shift1 = -st[1] * rstd1, rstd = st[2], shift = -st[3] * rstd, k = st[4];
+    if (AHEAD) {
+      if (row + TEAMS < r1) {
+        load(row + TEAMS);
+      } else if (TEAM > 64 && TEAMS > 1) {
+#pragma unroll
+        for (int p = 0; p < PER; ++p) hn[p].zero(), bn[p].zero(), zn[p].zero(), dn[p].zero();
+      }
+    }
     if (pre) {
-      const float rstd = a.pre_rstd[row], shift = a.pre == kLayer ? -a.pre_mean[row] * rstd : 0.f;
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
@@ -327,7 +342,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           zr[p].get(zv);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float xh = fmaf(hv[e], rstd, shift), g = zv[e] * qg[p][e];
+            const float xh = fmaf(hv[e], rstd1, shift1), g = zv[e] * qg[p][e];
             s[0] += g;
             s[1] += g * xh;
             sum[0][p][e] += zv[e] * xh;
@@ -346,13 +361,10 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           zr[p].get(zv);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            D[p][e] += rstd * (fmaf(zv[e], qg[p][e], -m1) - fmaf(hv[e], rstd, shift) * m2);
+            D[p][e] += rstd1 * (fmaf(zv[e], qg[p][e], -m1) - fmaf(hv[e], rstd1, shift1) * m2);
         }
       }
     }
-    const float rstd = post ? a.post_rstd[row] : 1.f, shift = a.post == kLayer ? -a.post_mean[row] * rstd : 0.f;
-    const float k = a.gate_kind == kToken ? a.gate[row] : 1.f;
-    const float scale = a.bscale * drop.scale;
     const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
     float s[3] = {0.f, 0.f, 0.f};  // of w = m gamma gate_c, of w bh (no post norm: of m b), of m beta
 #pragma unroll
@@ -365,40 +377,42 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           o[e] = a.alpha * D[p][e];
           D[p][e] *= scale;
         }
-        Eight<T>::store(static_cast<T*>(a.dx) + row * a.lddx + c, o);
+        if (real) Eight<T>::store(static_cast<T*>(a.dx) + row * a.lddx + c, o);
         drop.mask(g0 + c / 8, D[p]);
-        if (a.gate_kind == kToken && post && a.post_beta) {
+        if (a.gate_kind == kToken && POST && a.post_beta) {
           float bt[8];
           load8f(a.post_beta + c, bt);
 #pragma unroll
           for (int e = 0; e < 8; ++e) s[2] += D[p][e] * bt[e];
         }
-        float bv[8];
-        br[p].get(bv);
+        if (POST || a.gate_kind != kNone) {
+          float bv[8];
+          br[p].get(bv);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float m = D[p][e], bh = fmaf(bv[e], rstd, shift), w = m * pg[p][e];
-          const float mb = post || m != 0.f ? bh : 0.f;  // a dropped element is zero whatever b holds
-          s[0] += w;
-          s[1] += w * mb;
-          sum[2][p][e] += (k * m) * mb;
-          sum[3][p][e] += k * m;
-          D[p][e] = w;
+          for (int e = 0; e < 8; ++e) {
+            const float m = D[p][e], bh = fmaf(bv[e], rstd, shift), w = m * pg[p][e];
+            const float mb = POST || m != 0.f ? bh : 0.f;  // a dropped element is zero whatever b holds
+            s[0] += w;
+            s[1] += w * mb;
+            sum[2][p][e] += (k * m) * mb;
+            if (POST) sum[3][p][e] += k * m;
+            D[p][e] = w;
+          }
         }
       }
     }
-    if (post || a.gate_kind == kToken) {
+    if (POST || a.gate_kind == kToken) {
       team_sum<TEAM>(s, tid, red[ph]);
       ph ^= 1;
     }
-    if (a.gate_kind == kToken && a.d_gate && tid == 0) a.d_gate[row] = s[1] + s[2];
+    if (a.gate_kind == kToken && a.d_gate && tid == 0 && real) a.d_gate[row] = s[1] + s[2];
     const float m1 = a.post == kLayer ? s[0] * inv_h : 0.f, m2 = s[1] * inv_h;
     const float kr = k * rstd;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
       if (c < H) {
-        if (post) {
+        if constexpr (POST) {
           float bv[8];
           br[p].get(bv);
 #pragma unroll
@@ -407,16 +421,17 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) D[p][e] *= k;
         }
-        Eight<T>::store(static_cast<T*>(a.db) + row * a.lddb + c, D[p]);
+        if (real) Eight<T>::store(static_cast<T*>(a.db) + row * a.lddb + c, D[p]);
       }
     }
+    if (!AHEAD && row + TEAMS < r1) load(row + TEAMS);  // (a lone team)
   }
   // The workgroup's column sums: its teams' in team order.
   const Slots slots = bn_slots(a);
   float* part = a.part + (int64_t)blockIdx.x * slots.n * H;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (!slots.on[i]) continue;
+    if ((i == 3 && !POST) || !slots.on[i]) continue;
     if constexpr (TEAMS > 1) {
       __shared__ __attribute__((aligned(16))) float comb[TEAMS][8 * TEAM * PER];
       __syncthreads();
@@ -440,40 +455,43 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
 }
 
 // The column sums over the workgroups, and the gradients made from them.  A
-// workgroup covers 32 columns with 32 groups of rows: group t adds blocks t,
-// t + 32, ... in order, then the groups are added pairwise.
-constexpr int kRedCols = 32, kRedGroups = 32;
-__global__ __launch_bounds__(kRedCols / 4 * kRedGroups) void bn_reduce_kernel(BlockNormArgs a) {
+// workgroup covers 32 columns, with 256 threads for each sum that is needed:
+// 32 groups of rows, group t adding blocks t, t + 32, ... in order (the loads
+// all at once), then the groups are added pairwise.
+constexpr int kRedCols = 32, kRedGroups = 32, kRedThreads = kRedCols / 4 * kRedGroups;
+__global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArgs a) {
   __shared__ __attribute__((aligned(16))) float red[4][kRedGroups][kRedCols + 4];
-  const int lc = threadIdx.x % (kRedCols / 4) * 4, t = threadIdx.x / (kRedCols / 4);
+  __shared__ float total[4][kRedCols];
+  const int i = threadIdx.x / kRedThreads, th = threadIdx.x % kRedThreads;
+  const int lc = th % (kRedCols / 4) * 4, t = th / (kRedCols / 4);
   const int c = blockIdx.x * kRedCols + lc, H = a.H;
   const Slots slots = bn_slots(a);
+  const int64_t step = (int64_t)slots.n * H;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (c < H) {
+    const float* p = a.part + (int64_t)i * H + c;
+#pragma unroll 16
+    for (int b = t; b < a.nblocks; b += kRedGroups) s += *reinterpret_cast<const f32x4*>(p + b * step);
+  }
+  *reinterpret_cast<f32x4*>(&red[i][t][lc]) = s;
+  __syncthreads();
+  if (th < kRedCols) {
+    float v[kRedGroups];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (slots.on[i] && c < H) {
-#pragma unroll 8
-      for (int b = t; b < a.nblocks; b += kRedGroups)
-        s += *reinterpret_cast<const f32x4*>(a.part + ((int64_t)b * slots.n + slots.at[i]) * H + c);
+    for (int u = 0; u < kRedGroups; ++u) v[u] = red[i][u][th];
+#pragma unroll
+    for (int n = kRedGroups / 2; n > 0; n /= 2) {
+#pragma unroll
+      for (int u = 0; u < n; ++u) v[u] += v[u + n];
     }
-    *reinterpret_cast<f32x4*>(&red[i][t][lc]) = s;
+    total[i][th] = v[0];
   }
   __syncthreads();
   const int oc = blockIdx.x * kRedCols + threadIdx.x;
   if (threadIdx.x >= kRedCols || oc >= H) return;
   float S[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float v[kRedGroups];
-#pragma unroll
-    for (int u = 0; u < kRedGroups; ++u) v[u] = red[i][u][threadIdx.x];
-#pragma unroll
-    for (int n = kRedGroups / 2; n > 0; n /= 2) {
-#pragma unroll
-      for (int u = 0; u < n; ++u) v[u] += v[u + n];
-    }
-    S[i] = v[0];
-  }
+  for (int u = 0; u < 4; ++u) S[u] = slots.on[u] ? total[slots.at[u]][threadIdx.x] : 0.f;
   const bool post = a.post != kNone, chan = a.gate_kind == kChannel;
   auto put = [&](float* dst, float x) {
     if (a.accumulate) dst[oc] += x;
@@ -491,8 +509,6 @@ __global__ __launch_bounds__(kRedCols / 4 * kRedGroups) void bn_reduce_kernel(Bl
   }
 }
 
-constexpr int kMaxBlocks = 512;  // two a compute unit
-
 template <typename T, int NT, int TEAM, int PER>
 hipError_t fwd(const BlockNormArgs& a, hipStream_t stream) {
   const int64_t teams = NT / TEAM, all = (a.rows + teams - 1) / teams;
@@ -504,12 +520,13 @@ hipError_t fwd(const BlockNormArgs& a, hipStream_t stream) {
 
 template <typename T, int NT, int TEAM, int PER>
 hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((bn_bwd_kernel<T, NT, TEAM, PER>), dim3((unsigned)a.nblocks), dim3(NT), 0, stream, a);
+  const dim3 grid((unsigned)a.nblocks), block(NT);
+  if (a.post != kNone)
+    hipLaunchKernelGGL((bn_bwd_kernel<T, true, NT, TEAM, PER>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((bn_bwd_kernel<T, false, NT, TEAM, PER>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
-
-// Rows a workgroup works on at a time: up to 1024 columns a wave holds a row.
-int teams_of(int H) { return H <= 1024 ? 4 : 1; }
 
 // bf16 rows take two groups of eight columns a thread where they can: what a
 // wave does once per row (its share of the sums, the statistics) is half as
@@ -525,19 +542,31 @@ hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
   return fwd<T, 512, 512, 2>(a, stream);  // 1024 threads would have 128 registers each, too few
 }
 
+// The backward's workgroups hold as many teams as fit 512 threads, one
+// workgroup a compute unit, so that few of them leave column sums (8192 x 4096
+// with 512 workgroups of one team: 100 us with the sums' reduction, with 256 of
+// two teams 94); up to 512 columns a wave needs fewer registers and twice as
+// many fit.
 template <typename T>
 hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
   if (a.H <= 512) return bwd<T, 256, 64, 1>(a, stream);
-  if (a.H <= 1024) return bwd<T, 256, 64, 2>(a, stream);
-  if (a.H <= 2048) return bwd<T, 256 / P, 256 / P, P>(a, stream);
-  if (a.H <= 4096) return bwd<T, 512 / P, 512 / P, P>(a, stream);
+  if (a.H <= 1024) return bwd<T, 512, 64, 2>(a, stream);
+  if (a.H <= 2048) return bwd<T, 512, 256 / P, P>(a, stream);
+  if (a.H <= 4096) return bwd<T, 512, 512 / P, P>(a, stream);
   return bwd<T, 512, 512, 2>(a, stream);
 }
 
-int64_t bwd_blocks(int64_t rows, int H) {
-  const int64_t teams = teams_of(H), groups = (rows + teams - 1) / teams;
-  const int64_t most = H <= 4096 ? kMaxBlocks : kMaxBlocks / 2;  // past 4096 columns a workgroup fills a compute unit
+// Teams of a workgroup of the backward (as dispatched above), and the most
+// workgroups a number of rows takes.
+int teams_of(int H, int f32) {
+  if (H <= 512) return 4;
+  if (H <= 1024) return 8;
+  if (H <= 2048) return f32 ? 2 : 4;
+  return H <= 4096 && !f32 ? 2 : 1;
+}
+int64_t bwd_blocks(int64_t rows, int H, int f32) {
+  const int64_t teams = teams_of(H, f32), groups = (rows + teams - 1) / teams, most = H <= 512 ? 512 : 256;
   return groups < most ? groups : most;
 }
 
@@ -548,7 +577,7 @@ size_t block_norm_bwd_workspace(const BlockNormArgs& a) {
   BlockNormArgs b = a;
   float any;
   b.d_post_gamma = b.d_post_beta = b.d_gate = b.d_pre_gamma = b.d_pre_beta = &any;
-  return (size_t)bwd_blocks(a.rows, a.H) * bn_slots(b).n * (size_t)a.H * sizeof(float);
+  return (size_t)bwd_blocks(a.rows, a.H, a.f32) * bn_slots(b).n * (size_t)a.H * sizeof(float);
 }
 
 hipError_t launch_block_norm_fwd(const BlockNormArgs& a, hipStream_t stream) {
@@ -559,13 +588,14 @@ hipError_t launch_block_norm_fwd(const BlockNormArgs& a, hipStream_t stream) {
 hipError_t launch_block_norm_bwd(const BlockNormArgs& a, hipStream_t stream) {
   if (a.rows <= 0 || a.H <= 0 || a.H % 8 || a.H > kBnMaxH) return hipErrorInvalidValue;
   BlockNormArgs b = a;
-  const int64_t teams = teams_of(a.H), most = bwd_blocks(a.rows, a.H);
+  const int64_t teams = teams_of(a.H, a.f32), most = bwd_blocks(a.rows, a.H, a.f32);
   b.rows_per_block = (int)((a.rows + most * teams - 1) / (most * teams) * teams);
   b.nblocks = (int)((a.rows + b.rows_per_block - 1) / b.rows_per_block);
   const hipError_t e = a.f32 ? backward<float>(b, stream) : backward<uint16_t>(b, stream);
-  if (e != hipSuccess || bn_slots(a).n == 0) return e;
+  const int sums = bn_slots(a).n;
+  if (e != hipSuccess || sums == 0) return e;
   hipLaunchKernelGGL(bn_reduce_kernel, dim3((unsigned)((a.H + kRedCols - 1) / kRedCols)),
-                     dim3(kRedCols / 4 * kRedGroups), 0, stream, b);
+                     dim3((unsigned)(sums * kRedThreads)), 0, stream, b);
   return hipGetLastError();
 }
 

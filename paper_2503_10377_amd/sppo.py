@@ -238,6 +238,9 @@ def _stream(s) -> int | None:
     if s is None:
         import torch
 
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None and torch.cuda.is_initialized():  # the same stream, without a Stream object (2.7 us)
+            return raw(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream
     if hasattr(s, "cuda_stream"):
         return s.cuda_stream

@@ -283,10 +283,10 @@ def bwd_check(c, h, dz, dh, dx, db, g, start=0.0):
     ref = O.block_norm_bwd(b, hn, st, dzn, dhn, cfg, par, c.keep)
     D = ref["D"]
     eD = np.zeros_like(D)
-    # Column sums: a workgroup adds its rows one by one (at most ceil(rows /
-    # 512) + 4), its teams' sums, then up to 512 workgroups' in 32 groups of
-    # 16 and a tree of 5.
-    depth = -(-c.rows // 512) + 4 + 4 + 16 + 5 + 4
+    # Column sums: a team adds its rows one by one (a workgroup has at most
+    # ceil(rows / 256) + 8 of them), then a workgroup's up to 8 teams, then up
+    # to 512 workgroups' in 32 groups of 16 and a tree of 5.
+    depth = -(-c.rows // 256) + 8 + 8 + 16 + 5 + 4
 
     def col(name, terms, err, axis=0):
         if name in g:
@@ -691,3 +691,20 @@ def test_embedding_gradient_in_graphs():
             t[4]()
             torch.cuda.synchronize()
             assert torch.equal(t[3], x)
+
+
+def test_calls_without_a_stream_run_on_the_current_one():
+    """A call without a stream inside torch.cuda.stream(s) goes to s: it waits
+    for what s holds (a long copy), not for the default stream."""
+    announce("current stream")
+    from paper_2503_10377_amd.sppo import _stream
+    s = torch.cuda.Stream()
+    assert _stream(None) == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(s):
+        assert _stream(None) == s.cuda_stream
+        x = torch.ones(1 << 26, device="cuda", dtype=BF)
+        y = x * 2
+        z = torch.empty_like(x)
+        L.sppo_dropout(1 << 12, 1 << 14, y, 1 << 14, L.drop_spec(0.0, 0), z, 1 << 14)
+    s.synchronize()
+    assert torch.all(z == 2)
