@@ -11,6 +11,8 @@ With t the global row (row0 + r), c the column and W the row's width:
     norm     LayerNorm (v - mean) rstd gamma + beta, RMSNorm v rstd gamma + beta
     block    n = N_post(b); h = alpha x + s keep (g n); z = N_pre(h)
     lookup   y = keep (s table[id]), zero for ids outside the table
+    layer    the layer of transformer_layer whose two branches join the stream
+             by block (LN2 the norm behind the first, none behind the second)
 
 Pins (tests/test_train_ops_cpu.py): the generator's published answers; the
 drawn share of kept elements; central differences of every gradient; the
@@ -18,7 +20,12 @@ lookup's gradient as the transpose of the lookup.
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
+
+from .causal_attention import attention_bwd, attention_fwd
+from .transformer_layer import gelu, gelu_grad, layer_norm, layer_norm_bwd
 
 _U32 = 0xFFFFFFFF
 
@@ -110,7 +117,7 @@ def block_norm_bwd(b, h, stats, dz, dh, cfg, par, keep):
     """Gradients of sum(dz z) + sum(dh h) at x, b and the parameters, from the
     kept b, h and statistics (dz None where there is no z, dh None: zero)."""
     out = {}
-    D = np.zeros_like(keep) if dh is None else _f64(dh)
+    D = np.zeros(keep.shape) if dh is None else _f64(dh)
     if cfg["pre"] != "none":
         hh = _hat(h, stats["pre_mean"], stats["pre_rstd"])
         out["pre_gamma"], out["pre_beta"] = (_f64(dz) * hh).sum(axis=0), _f64(dz).sum(axis=0)
@@ -149,4 +156,50 @@ def embedding_bwd(ids, dy, V, scale, keep=None):
     ok = (ids >= 0) & (ids < V)
     out = np.zeros((V, dy.shape[1]))
     np.add.at(out, ids[ok], scale * dy[ok])
+    return out
+
+
+def layer_with_ends(x, dy, p, hq, hkv, d, ends, keep1, keep2, eps=1e-5):
+    """Forward and backward of the layer with block ends, unchunked, batch 1.
+    ends: norm, gate (bool), alpha, scale.  p: the layer's parameters and
+    g_end1, b_end1, gate1, g_end2, b_end2, gate2 where ends has them.  keep1,
+    keep2: the two dropouts' factors [S, H].  Returns y, dx and the gradients
+    by the parameters' names with a d in front (dw_*, dg1, ...)."""
+    x, dy = _f64(x), _f64(dy)
+    S = len(x)
+    cfg = [dict(post=ends["norm"], pre=pre, gate="channel" if ends["gate"] else "none", eps=eps, alpha=ends["alpha"],
+                scale=ends["scale"]) for pre in ("layer", "none")]
+    par = [dict(post_gamma=p.get(f"g_end{n}"), post_beta=p.get(f"b_end{n}"), gate=p.get(f"gate{n}"),
+                pre_gamma=p["g2"], pre_beta=p["b2"]) for n in (1, 2)]
+    w = {k: _f64(p[k]) for k in ("w_qkv", "w_o", "w_1", "w_2")}
+    u, m1, r1 = layer_norm(x, p["g1"], p["b1"], eps)
+    qkv = u @ w["w_qkv"]
+    split = np.split(qkv, [hq * d, (hq + hkv) * d], axis=1)
+    q, k, v = (t.reshape(1, S, n, d) for t, n in zip(split, (hq, hkv, hkv)))
+    scale = 1.0 / math.sqrt(d)
+    o4, lse = attention_fwd(q, k, v, scale)
+    o = o4.reshape(S, -1)
+    e1 = o @ w["w_o"]
+    f1 = block_norm_fwd(x, e1, cfg[0], par[0], keep1)
+    a = f1["z"] @ w["w_1"]
+    g = gelu(a)
+    e2 = g @ w["w_2"]
+    f2 = block_norm_fwd(f1["h"], e2, cfg[1], par[1], keep2)
+    out = {"y": f2["h"]}
+    b2 = block_norm_bwd(e2, None, f2, None, dy, cfg[1], par[1], keep2)
+    out["dw_2"] = g.T @ b2["db"]
+    da = (b2["db"] @ w["w_2"].T) * gelu_grad(a)
+    out["dw_1"] = f1["z"].T @ da
+    b1 = block_norm_bwd(e1, f1["h"], f1, da @ w["w_1"].T, b2["dx"], cfg[0], par[0], keep1)
+    out["dg2"], out["db2"] = b1["pre_gamma"], b1["pre_beta"]
+    out["dw_o"] = o.T @ b1["db"]
+    do4 = (b1["db"] @ w["w_o"].T).reshape(1, S, hq, d)
+    dqkv = np.concatenate([t.reshape(S, -1) for t in attention_bwd(q, k, v, do4, scale, o4, lse)], axis=1)
+    out["dw_qkv"] = u.T @ dqkv
+    dx, out["dg1"], out["db1"] = layer_norm_bwd(x, p["g1"], m1, r1, dqkv @ w["w_qkv"].T)
+    out["dx"] = b1["dx"] + dx
+    for n, b in ((1, b1), (2, b2)):
+        for ours, theirs in (("post_gamma", f"g_end{n}"), ("post_beta", f"b_end{n}"), ("gate", f"gate{n}")):
+            if p.get(theirs) is not None:
+                out["d" + theirs] = b[ours]
     return out

@@ -28,6 +28,19 @@ offloaded) and comes back into the chunk's region.
 The host stays at most ``host_ahead`` chunk boundaries ahead of the device
 (a HostPacer; 0 lets it run free).
 
+Two options put the training operators around the blocks:
+  ends=BlockEnds(...)  how a block's output b joins the residual stream, in
+      one call with the LayerNorm that follows (sppo_block_norm_fwd/_bwd):
+          h = alpha x + s drop(gate1 N1(O W_o)),  z = LN2(h)
+          y = alpha h + s drop(gate2 N2(gelu(a) W_2))
+      with a norm after the branch (or none), a gate per channel (or none),
+      scales and dropout.  The masks are drawn again in the backward; b_i and
+      the norms' statistics are further planes where the backward needs them.
+  vocab=V              the walk starts from tokens: x_i = drop(scale
+      w_emb[tokens_i]) is looked up in the forward and again in the backward
+      (it is no plane, so it does not travel), and dx_i becomes the table's
+      gradient, added up over the reverse walk.
+
 Only C-ABI calls and torch allocations happen here; every arithmetic step
 runs in the library's kernels.
 """
@@ -39,20 +52,69 @@ from . import sppo as L
 from .pacing import HostPacer
 from .ring import DeviceArena, KeepArena, plan_capacity, plane_layout, walk_schedule
 
-PLANES = ("x", "h", "a", "m1", "r1", "m2", "r2")
+PLANES = ("x", "h", "a", "m1", "r1", "m2", "r2")  # without options
+
+# Where a step draws masks: the offsets of its three calls, added to the step's.
+DROP_EMBED, DROP_ATTN, DROP_MLP, DROP_STRIDE = 0, 1, 2, 3
+
+
+class BlockEnds:
+    """How the layer's two blocks join the residual stream: the norm after
+    the branch ("none", "layer", "rms"), a gate per channel, the scales of the
+    stream and of the branch, and the dropout's p."""
+
+    def __init__(self, norm="none", gate=False, residual_scale=1.0, branch_scale=1.0, dropout=0.0):
+        if norm not in L.NORMS:
+            raise ValueError(f"unknown norm {norm!r}")
+        if not 0.0 <= dropout < 1.0:
+            raise ValueError("dropout must be in [0, 1)")
+        self.norm, self.gate = norm, bool(gate)
+        self.residual_scale, self.branch_scale, self.dropout = residual_scale, branch_scale, dropout
+
+    @property
+    def keeps_branch(self):
+        """Whether the backward needs the branch's output."""
+        return self.norm != "none" or self.gate
+
+    def params(self, n):
+        """Names of block n's parameters ([H] fp32 each), as block_norm takes
+        them; the layer's are these with a p, their gradients with a dp."""
+        names = {}
+        if self.norm != "none":
+            names["post_gamma"] = f"g_end{n}"
+        if self.norm == "layer":
+            names["post_beta"] = f"b_end{n}"
+        if self.gate:
+            names["gate"] = f"gate{n}"
+        return names
 
 
 class ChunkedLayer:
     def __init__(self, S, n_chunks, Hq, Hkv, D, offsets=None, offload="none", device="cuda", eps=1e-5,
-                 host_ahead=2, fwd_slots=4):
+                 host_ahead=2, fwd_slots=4, ends=None, vocab=None, embed_scale=1.0):
         H = Hq * D
         wt = (Hq + 2 * Hkv) * D
         if H % 256 or wt % 256 or H > 8192:
             raise ValueError("the layer needs Hq*D and (Hq+2Hkv)*D multiples of 256 and Hq*D <= 8192")
+        if vocab is not None and not 0 < vocab < 2 ** 31:
+            raise ValueError("vocab must be in [1, 2^31)")
         self.S, self.N, self.Hq, self.Hkv, self.D, self.H, self.Wt = S, n_chunks, Hq, Hkv, D, H, wt
         self.eps = eps
         self.device = device
-        row_bytes = [2 * H, 2 * H, 8 * H, 4, 4, 4, 4]  # x, h, a bf16; mean/rstd of LN1, LN2 fp32
+        self.ends, self.vocab, self.embed_scale = ends, vocab, embed_scale
+        # bytes of a row of each plane: x, h, a bf16, mean/rstd of LN1, LN2 fp32;
+        # with block ends their branches (bf16) and statistics
+        self.row_bytes = dict(zip(PLANES, (2 * H, 2 * H, 8 * H, 4, 4, 4, 4)))
+        if vocab is not None:
+            del self.row_bytes["x"]
+        if ends is not None and ends.keeps_branch:
+            self.row_bytes.update(e1=2 * H, e2=2 * H)
+        if ends is not None and ends.norm != "none":
+            self.row_bytes.update(er1=4, er2=4)
+        if ends is not None and ends.norm == "layer":
+            self.row_bytes.update(em1=4, em2=4)
+        self.planes = tuple(self.row_bytes)
+        row_bytes = list(self.row_bytes.values())
         self.ctx = L.sppo_create(1, S, n_chunks, Hq, Hkv, D, dtype="bf16", chunk_offsets=offsets,
                                  offload=offload, extra_row_bytes=row_bytes)
         self.offsets = L.sppo_get_offsets(self.ctx)
@@ -88,12 +150,30 @@ class ChunkedLayer:
         wsb = max(L.sppo_layernorm_bwd_workspace(self.chunk_len(i), H) for i in range(self.N))
         self.ws = torch.empty(wsb // 4, dtype=f32, device=dev)
         self.ws_bytes = wsb
+        if self.ends is not None:
+            self.branch, self.dbranch = e(sm, H), e(sm, H)
+            probe = [L.block_norm(H, "bf16", post=self.ends.norm, pre=pre, gate_kind="channel" if self.ends.gate else
+                                  "none", eps=self.eps, post_gamma=self.dk, post_beta=self.dk, gate=self.dk,
+                                  pre_gamma=self.dk, pre_beta=self.dk) for pre in ("layer", "none")]
+            self.ends_ws_bytes = max(L.sppo_block_norm_bwd_workspace(b, sm) for b in probe)
+            self.ends_ws = torch.empty(max(self.ends_ws_bytes, 16) // 4, dtype=f32, device=dev)
+        if self.vocab is not None:
+            self.x, self.dx = e(sm, H), e(sm, H)
+            self.emb_ws_bytes = L.sppo_embedding_bwd_workspace(sm, H)
+            self.emb_ws = torch.empty(self.emb_ws_bytes // 4, dtype=f32, device=dev)
 
     def alloc_outputs(self):
         H, Wt, dev = self.H, self.Wt, self.device
         f32 = torch.float32
-        return {"y": torch.empty(self.S, H, dtype=torch.bfloat16, device=dev),
-                "dx": torch.empty(self.S, H, dtype=torch.bfloat16, device=dev),
+        more = {}
+        if self.vocab is None:
+            more["dx"] = torch.empty(self.S, H, dtype=torch.bfloat16, device=dev)
+        else:
+            more["dw_emb"] = torch.empty(self.vocab, H, dtype=f32, device=dev)
+        if self.ends is not None:
+            for n in (1, 2):
+                more.update({"d" + k: torch.empty(H, dtype=f32, device=dev) for k in self.ends.params(n).values()})
+        return {"y": torch.empty(self.S, H, dtype=torch.bfloat16, device=dev), **more,
                 "dw_qkv": torch.empty(H, Wt, dtype=f32, device=dev),
                 "dw_o": torch.empty(self.Hq * self.D, H, dtype=f32, device=dev),
                 "dw_1": torch.empty(H, 4 * H, dtype=f32, device=dev),
@@ -103,7 +183,7 @@ class ChunkedLayer:
     def offload_bytes_per_row(self):
         """Bytes per token row of the offload set: Q, O, LSE, the extra planes
         (and K, V in the QKVOL modes)."""
-        b = 2 * self.Hq * self.D * 2 + 4 * self.Hq + 12 * self.H + 16
+        b = 2 * self.Hq * self.D * 2 + 4 * self.Hq + sum(self.row_bytes.values())
         if self.offload in (L.SPPO_OFFLOAD_QKVOL, L.SPPO_OFFLOAD_QKVOL_EVICT):
             b += 2 * self.Hkv * self.D * 2
         return b
@@ -115,9 +195,9 @@ class ChunkedLayer:
     # ------------------------------------------------------------ the walk
     def region_planes(self, i):
         """Byte sizes of chunk i's saved tensors in its arena region."""
-        n, H, HqD = self.chunk_len(i), self.H, self.Hq * self.D
-        return {"q": 2 * n * HqD, "o": 2 * n * HqD, "lse": 4 * self.Hq * n, "x": 2 * n * H, "h": 2 * n * H,
-                "a": 8 * n * H, "m1": 4 * n, "r1": 4 * n, "m2": 4 * n, "r2": 4 * n}
+        n, HqD = self.chunk_len(i), self.Hq * self.D
+        return {"q": 2 * n * HqD, "o": 2 * n * HqD, "lse": 4 * self.Hq * n,
+                **{k: n * b for k, b in self.row_bytes.items()}}
 
     def prepare(self, offload_chunks, lookahead):
         """Allocate the device arena and keep buffers for a walk with these
@@ -148,17 +228,35 @@ class ChunkedLayer:
         po = self._planes[i][0]
         pl = lambda name, shape, dt: self.arena.view(off + po[name], shape, dt)  # noqa: E731
         v = dict(q=pl("q", (n, HqD), bf), o=pl("o", (n, HqD), bf), lse=pl("lse", (self.Hq, n), f32),
-                 h=pl("h", (n, H), bf), a=pl("a", (n, 4 * H), bf),
-                 **{k: pl(k, (n,), f32) for k in ("m1", "r1", "m2", "r2")})
-        v["x"] = x if x is not None else pl("x", (n, H), bf)
+                 **{k: pl(k, (n,), f32) if b == 4 else pl(k, (n, b // 2), bf) for k, b in self.row_bytes.items()
+                    if k != "x"})
+        v["x"] = x if x is not None else self.x[:n] if self.vocab is not None else pl("x", (n, H), bf)
         return off, v
 
     def _bufs(self, v, keep):
         return L.chunk_bufs(q=v["q"], o=v["o"], lse=v["lse"], k=self.k, v=self.v,
-                            extra=[v[name] for name in PLANES], keep=keep)
+                            extra=[v[name] for name in self.planes], keep=keep)
+
+    def _end(self, n, p, v):
+        """The description of block n's end (with LN2 behind the first) and its
+        statistics, for a chunk's views."""
+        e = self.ends
+        pre = dict(pre="layer", pre_gamma=p["g2"], pre_beta=p["b2"]) if n == 1 else {}
+        bn = L.block_norm(self.H, "bf16", post=e.norm, gate_kind="channel" if e.gate else "none", eps=self.eps,
+                          residual_scale=e.residual_scale, branch_scale=e.branch_scale,
+                          **{k: p[name] for k, name in e.params(n).items()}, **pre)
+        st = L.block_norm_stats(v.get(f"em{n}"), v.get(f"er{n}"), v["m2"] if n == 1 else None,
+                                v["r2"] if n == 1 else None)
+        return bn, st
+
+    def _end_grads(self, n, out):
+        g = {k: out["d" + name] for k, name in self.ends.params(n).items()}
+        if n == 1:
+            g.update(pre_gamma=out["dg2"], pre_beta=out["db2"])
+        return L.block_norm_grads(**g)
 
     def step(self, inp, p, out, offload_chunks=None, lookahead=2, poison=False, stream=None, marks=None,
-             ops=None):
+             ops=None, seed=0, offset=0):
         """Forward and backward of the layer over all chunks.  inp: x, dy
         [S, H] bf16 (x's chunk rows are the x planes: offloading a chunk
         makes its rows of x dead, and the prefetch brings them back into the
@@ -167,7 +265,11 @@ class ChunkedLayer:
         weights (w_qkv, w_o, w_1, w_2 bf16; g1, b1, g2, b2 fp32).  marks:
         list that receives ((phase, chunk), event) at every chunk boundary.
         ops: list that receives (category, algorithmic flop, start event,
-        end event) around every library call on the compute stream."""
+        end event) around every library call on the compute stream.  With
+        vocab, inp holds tokens [S] (int32 or int64) instead of x, p w_emb
+        [vocab, H] bf16, and out dw_emb instead of dx; with ends, p their
+        parameters (BlockEnds.params) in fp32.  seed, offset: of the step's
+        dropout, which draws at offsets offset .. offset + DROP_STRIDE - 1."""
         s = torch.cuda.current_stream() if stream is None else stream
         H, Wt, HqD, HkvD = self.H, self.Wt, self.Hq * self.D, self.Hkv * self.D
         if offload_chunks is None:
@@ -176,7 +278,10 @@ class ChunkedLayer:
         self.prepare(offl, lookahead)
         arena, keep = self.arena, self.keep
         arena.reset()
-        x, dy = inp["x"], inp["dy"]
+        ends, dy = self.ends, inp["dy"]
+        x = inp["x"] if self.vocab is None else None
+        drop_p = ends.dropout if ends is not None else 0.0
+        id_type = "i32" if x is None and inp["tokens"].dtype == torch.int32 else "i64"
 
         def mark(label):
             self.pacer.boundary(s)
@@ -206,6 +311,13 @@ class ChunkedLayer:
         ln_bwd = timed("layernorm", L.sppo_layernorm_bwd)
         gelu = timed("gelu", L.sppo_gelu_bf16)
         pack = timed("pack", L.sppo_pack_qkv_grad)
+        end_fwd = timed("block_norm", L.sppo_block_norm_fwd)
+        end_bwd = timed("block_norm", L.sppo_block_norm_bwd)
+        embed = timed("embedding", L.sppo_embedding_fwd)
+        embed_bwd = timed("embedding", L.sppo_embedding_bwd)
+        drop = lambda site, row0: L.drop_spec(drop_p, seed, offset + site, row0) if drop_p > 0 else None
+        lookup = lambda n, c0: embed(n, H, self.vocab, inp["tokens"][c0:], p["w_emb"], H, self.embed_scale,
+                                     drop(DROP_EMBED, c0), self.x, H, "bf16", id_type, s)
         pairs = lambda a: self.chunk_len(a[1]) * self.offsets[a[1]] + self.chunk_len(a[1]) * (self.chunk_len(a[1]) + 1) // 2
         attn_fwd = timed("attn_fwd", L.sppo_attn_fwd_chunk, lambda a: 4 * self.D * self.Hq * pairs(a))
         attn_bwd = timed("attn_bwd", L.sppo_attn_bwd_chunk, lambda a: 10 * self.D * self.Hq * pairs(a))
@@ -219,7 +331,9 @@ class ChunkedLayer:
         for i in range(self.N):
             mark(("fwd", i))
             n, c0 = self.chunk_len(i), self.offsets[i]
-            slot, v = self._acquire(i, s, x=x[c0:c0 + n])
+            slot, v = self._acquire(i, s, x=None if x is None else x[c0:c0 + n])
+            if x is None:
+                lookup(n, c0)
             u, z, g = self.u[:n], self.z[:n], self.g[:n]
             ln_fwd(n, H, v["x"], H, p["g1"], p["b1"], self.eps, u, H, v["m1"], v["r1"], s)
             wq = self.wT["w_qkv"]
@@ -227,11 +341,22 @@ class ChunkedLayer:
             gemm("nt", n, HkvD, H, u, H, wq[HqD:], H, self.k[c0:], HkvD, stream=s)
             gemm("nt", n, HkvD, H, u, H, wq[HqD + HkvD:], H, self.v[c0:], HkvD, stream=s)
             attn_fwd(self.ctx, i, v["q"], self.k, self.v, v["o"], v["lse"], s)
-            gemm("nt", n, H, HqD, v["o"], HqD, self.wT["w_o"], HqD, v["h"], H, "add_bf16", v["x"], H, stream=s)
-            ln_fwd(n, H, v["h"], H, p["g2"], p["b2"], self.eps, z, H, v["m2"], v["r2"], s)
+            if ends is None:
+                gemm("nt", n, H, HqD, v["o"], HqD, self.wT["w_o"], HqD, v["h"], H, "add_bf16", v["x"], H, stream=s)
+                ln_fwd(n, H, v["h"], H, p["g2"], p["b2"], self.eps, z, H, v["m2"], v["r2"], s)
+            else:
+                e1, e2 = v.get("e1", self.branch), v.get("e2", self.branch)
+                gemm("nt", n, H, HqD, v["o"], HqD, self.wT["w_o"], HqD, e1, H, stream=s)
+                bn, st = self._end(1, p, v)
+                end_fwd(bn, n, drop(DROP_ATTN, c0), v["x"], H, e1, H, v["h"], H, z, H, st, s)
             gemm("nt", n, 4 * H, H, z, H, self.wT["w_1"], H, g, 4 * H, "gelu", v["a"], 4 * H, stream=s)
-            gemm("nt", n, H, 4 * H, g, 4 * H, self.wT["w_2"], 4 * H, out["y"][c0:], H, "add_bf16", v["h"], H,
-                 stream=s)
+            if ends is None:
+                gemm("nt", n, H, 4 * H, g, 4 * H, self.wT["w_2"], 4 * H, out["y"][c0:], H, "add_bf16", v["h"], H,
+                     stream=s)
+            else:
+                gemm("nt", n, H, 4 * H, g, 4 * H, self.wT["w_2"], 4 * H, e2, H, stream=s)
+                bn, st = self._end(2, p, v)
+                end_fwd(bn, n, drop(DROP_MLP, c0), v["h"], H, e2, H, out["y"][c0:], H, None, 0, st, s)
             if i in offl:
                 L.sppo_offload_issue(self.ctx, i, self._bufs(v, keep.ptr(i)), s)
                 arena.release(slot, after_offload=True)
@@ -281,31 +406,52 @@ class ChunkedLayer:
             u, z, g = self.u[:n], self.z[:n], self.g[:n]
             da, dz, dh, dO = self.da[:n], self.dz[:n], self.dh[:n], self.dO[:n]
             dyi = dy[c0:c0 + n]
+            add = 0 if first else 1
+            dres, dbr = dyi, dyi  # gradients of h (along the stream) and of the MLP's output
+            if ends is not None:
+                # y = alpha h + s drop(gate2 N2(e2))
+                dres, dbr = dh, self.dbranch
+                bn, st = self._end(2, p, v)
+                end_bwd(bn, n, drop(DROP_MLP, c0), v.get("e2"), H, None, 0, st, None, 0, dyi, H, dres, H, dbr, H,
+                        self._end_grads(2, out), self.ends_ws, self.ends_ws_bytes, add, s)
             # y = h + gelu(a) W2
             gelu(v["a"], g, n * 4 * H, s)
-            gemm("nt", n, 4 * H, H, dyi, H, p["w_2"], H, da, 4 * H, "dgelu", v["a"], 4 * H, stream=s)
-            gemm("tn", 4 * H, H, n, g, 4 * H, dyi, H, out["dw_2"], H, wacc, stream=s)
+            gemm("nt", n, 4 * H, H, dbr, H, p["w_2"], H, da, 4 * H, "dgelu", v["a"], 4 * H, stream=s)
+            gemm("tn", 4 * H, H, n, g, 4 * H, dbr, H, out["dw_2"], H, wacc, stream=s)
             # a = z W1, z = LN2(h)
             ln_fwd(n, H, v["h"], H, p["g2"], p["b2"], self.eps, z, H, v["m2"], v["r2"], s)
             gemm("nt", n, H, 4 * H, da, 4 * H, p["w_1"], 4 * H, dz, H, stream=s)
             gemm("tn", H, 4 * H, n, z, H, da, 4 * H, out["dw_1"], 4 * H, wacc, stream=s)
-            ln_bwd(n, H, v["h"], H, p["g2"], v["m2"], v["r2"], dz, H, dyi, H, dh, H, out["dg2"],
-                                 out["db2"], self.ws, self.ws_bytes, accumulate=0 if first else 1, stream=s)
+            if ends is None:
+                ln_bwd(n, H, v["h"], H, p["g2"], v["m2"], v["r2"], dz, H, dyi, H, dh, H, out["dg2"],
+                                     out["db2"], self.ws, self.ws_bytes, accumulate=0 if first else 1, stream=s)
+                dbr = dh
+            else:
+                # h = alpha x + s drop(gate1 N1(e1)), z = LN2(h); dh: from h's gradient to x's
+                bn, st = self._end(1, p, v)
+                end_bwd(bn, n, drop(DROP_ATTN, c0), v.get("e1"), H, v["h"], H, st, dz, H, dres, H, dh, H, dbr, H,
+                        self._end_grads(1, out), self.ends_ws, self.ends_ws_bytes, add, s)
             # h = x + O Wo
-            gemm("nt", n, HqD, H, dh, H, p["w_o"], H, dO, HqD, stream=s)
-            gemm("tn", HqD, H, n, v["o"], HqD, dh, H, out["dw_o"], H, wacc, stream=s)
+            gemm("nt", n, HqD, H, dbr, H, p["w_o"], H, dO, HqD, stream=s)
+            gemm("tn", HqD, H, n, v["o"], HqD, dbr, H, out["dw_o"], H, wacc, stream=s)
             attn_bwd(self.ctx, i, v["q"], self.k, self.v, v["o"], v["lse"], dO, self.dq[:n],
                                   self.dk, self.dv, s)
             # q, k, v = u W_qkv (chunk i's dK/dV rows are complete now)
             dqkv = self.dqkv[:n]
             pack(n, HqD, HkvD, self.dq[:n], self.dk, self.dv, c0, dqkv, s)
+            if x is None:
+                lookup(n, c0)
             ln_fwd(n, H, v["x"], H, p["g1"], p["b1"], self.eps, u, H, v["m1"], v["r1"], s)
             gemm("nt", n, H, Wt, dqkv, Wt, p["w_qkv"], Wt, self.du[:n], H, stream=s)
             gemm("tn", H, Wt, n, u, H, dqkv, Wt, out["dw_qkv"], Wt, wacc, stream=s)
             # u = LN1(x); x also reaches h
+            dxi = self.dx if x is None else out["dx"][c0:]
             ln_bwd(n, H, v["x"], H, p["g1"], v["m1"], v["r1"], self.du[:n], H, dh, H,
-                                 out["dx"][c0:], H, out["dg1"], out["db1"], self.ws, self.ws_bytes,
+                                 dxi, H, out["dg1"], out["db1"], self.ws, self.ws_bytes,
                                  accumulate=0 if first else 1, stream=s)
+            if x is None:
+                embed_bwd(n, H, self.vocab, inp["tokens"][c0:], dxi, H, self.embed_scale, drop(DROP_EMBED, c0),
+                          out["dw_emb"], H, self.emb_ws, self.emb_ws_bytes, add, "bf16", id_type, s)
             arena.release(slot)
         mark(("end", -1))
 

@@ -101,6 +101,57 @@ def test_embedding_gradient_is_the_transpose_of_the_lookup():
     assert abs(lhs - rhs) <= 640 * 2.0 ** -53 * 10 * 10
 
 
+@pytest.mark.parametrize("norm,gate", [("layer", True), ("rms", False), ("none", False), ("none", True)])
+def test_layer_with_ends_matches_differences(norm, gate):
+    """Central differences (step 1e-5) of L = sum(dy y) along one random
+    direction of every input and parameter: rounding 1e3 terms of order 1 times
+    1.1e-16 / 2e-5 = 6e-9, truncation 1e-10 times a third derivative along the
+    direction of order 1e3; gate 1e-6 of the sum of magnitudes."""
+    g = np.random.default_rng(11)
+    S, hq, hkv, d = 6, 2, 1, 4
+    H = hq * d
+    p = {"w_qkv": g.normal(size=(H, (hq + 2 * hkv) * d)) / 3, "w_o": g.normal(size=(H, H)) / 3,
+         "w_1": g.normal(size=(H, 4 * H)) / 3, "w_2": g.normal(size=(4 * H, H)) / 6,
+         "g1": 1 + 0.1 * g.normal(size=H), "b1": 0.1 * g.normal(size=H),
+         "g2": 1 + 0.1 * g.normal(size=H), "b2": 0.1 * g.normal(size=H)}
+    for n in (1, 2):
+        if norm != "none":
+            p[f"g_end{n}"] = 1 + 0.1 * g.normal(size=H)
+        if norm == "layer":
+            p[f"b_end{n}"] = 0.1 * g.normal(size=H)
+        if gate:
+            p[f"gate{n}"] = g.uniform(0.5, 1.5, size=H)
+    ends = dict(norm=norm, gate=gate, alpha=0.9, scale=0.7)
+    keep = [O.keep_factor(S, H, 0.25, 5, o) for o in (1, 2)]
+    x, dy = g.normal(size=(S, H)), g.normal(size=(S, H))
+    run = lambda q: O.layer_with_ends(q["x"], dy, q, hq, hkv, d, ends, *keep)
+    base = dict(p, x=x)
+    ref = run(base)
+    assert set(ref) == {"y"} | {"d" + k for k in base}
+    for name, val in base.items():
+        t = g.normal(size=val.shape)
+        up, dn = (run(dict(base, **{name: val + s * 1e-5 * t})) for s in (1, -1))
+        diff = (dy * (up["y"] - dn["y"])).sum() / 2e-5
+        along = ref["d" + name] * t
+        assert abs(diff - along.sum()) <= 1e-6 * np.abs(along).sum() + 1e-8, name
+
+
+def test_layer_with_plain_ends_is_the_layer():
+    from oracle import transformer_layer as T
+    g = np.random.default_rng(12)
+    S, hq, hkv, d = 7, 2, 2, 4
+    H = hq * d
+    p = {"w_qkv": g.normal(size=(H, 3 * H)), "w_o": g.normal(size=(H, H)), "w_1": g.normal(size=(H, 4 * H)),
+         "w_2": g.normal(size=(4 * H, H)), "g1": g.normal(size=H), "b1": g.normal(size=H), "g2": g.normal(size=H),
+         "b2": g.normal(size=H)}
+    x, dy = g.normal(size=(S, H)), g.normal(size=(S, H))
+    a = T.layer(x, dy, p, hq, hkv, d)
+    one = np.ones((S, H))
+    b = O.layer_with_ends(x, dy, p, hq, hkv, d, dict(norm="none", gate=False, alpha=1.0, scale=1.0), one, one)
+    for k in a:
+        np.testing.assert_allclose(a[k], b[k], rtol=1e-12, atol=1e-12 * np.abs(a[k]).max())
+
+
 # ------------------------------------------------------------------ refusals
 A = 4096  # any aligned non-null address: nothing is launched on a refusal
 
