@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, 
 // which a workgroup holds in LDS.  n^2 comparisons of two instructions beat the
 // passes of a sort (four launches of 5 us for 8192 rows) while launches and
 // their gaps are what costs: 11 us for 8192 rows.
-constexpr int kSmallKeys = 16384, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
+constexpr int kSmallKeys = 8192, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 
 // split: lanes that share a row's comparisons (1, 2 or 4); a workgroup ranks
 // 64 / split rows, its waves and their lane groups taking blocks of 64 rows j
@@ -429,6 +429,100 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, S
   }
 }
 
+// ------------------------------------------------------------------ few rows
+// Up to kDirectRows rows need no sorted list: a workgroup takes row i and
+// kSlab columns, finds the rows with i's token by comparing all tokens (each
+// lane holds kDirectRows / 64 of them), ends if one comes before i, and else
+// sums them, wave w those of rows 64 w and on, then the waves' sums in order.  The
+// workgroups after those clear the rows that no token names (they find that
+// out the same way), so the whole gradient is one launch.
+constexpr int kDirectRows = 256, kDirectHeld = kDirectRows / 64, kDirectAhead = 8;
+
+template <typename T>
+__global__ __launch_bounds__(256) void embed_direct_kernel(EmbedArgs a, int sums) {
+  __shared__ __attribute__((aligned(16))) float red[3][kSlab];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n = (int)a.rows;
+  const uint32_t V = (uint32_t)a.V;
+  uint32_t held[kDirectHeld];  // tokens of rows 64 u + lane
+#pragma unroll
+  for (int u = 0; u < kDirectHeld; ++u) held[u] = 64 * u + lane < n ? token(a.ids, a.id64, 64 * u + lane, a.V) : V;
+  if ((int)blockIdx.x >= sums) {
+    const int64_t blocks = gridDim.x - sums;
+    for (int64_t v = ((int64_t)blockIdx.x - sums) * 4 + w; v < a.V; v += blocks * 4) {
+      bool named = false;
+#pragma unroll
+      for (int u = 0; u < kDirectHeld; ++u) named |= held[u] == (uint32_t)v;
+      if (__ballot(named)) continue;
+      for (int c = 4 * lane; c < a.H; c += 256)
+        *reinterpret_cast<f32x4*>(a.dtable + v * a.lddt + c) = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    return;
+  }
+  const int slabs = (a.H + kSlab - 1) / kSlab, i = blockIdx.x / slabs;
+  const int c = (blockIdx.x - i * slabs) * kSlab + 8 * lane;
+  const bool in = c < a.H;
+  const uint32_t k = token(a.ids, a.id64, i, a.V);
+  if (k >= V) return;
+  uint64_t same[kDirectHeld];  // the rows with token k
+#pragma unroll
+  for (int u = 0; u < kDirectHeld; ++u) {
+    same[u] = __ballot(held[u] == k);
+    const int64_t before = (int64_t)i - 64 * u;  // rows of this word before i
+    if (before > 0 && (before >= 64 ? same[u] : same[u] & (((uint64_t)1 << before) - 1))) return;
+  }
+  const Dropper drop(a.drop);
+  uint64_t left = same[0];  // of the wave's rows
+#pragma unroll
+  for (int u = 1; u < kDirectHeld; ++u)
+    if (w == u) left = same[u];
+  const int mine = __popcll(left);
+  Eight<T> x[kDirectAhead];
+  int row[kDirectAhead];
+  auto load = [&](int m, int slot) {
+    if (m >= mine) return;
+    row[slot] = 64 * w + __ffsll((unsigned long long)left) - 1;
+    left &= left - 1;
+    if (in) x[slot].load(static_cast<const T*>(a.dy) + (int64_t)row[slot] * a.ldy + c);
+  };
+#pragma unroll
+  for (int v = 0; v < kDirectAhead; ++v) load(v, v);
+  float acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  for (int j = 0; j < mine; j += kDirectAhead) {
+#pragma unroll
+    for (int v = 0; v < kDirectAhead; ++v) {
+      if (j + v >= mine) break;
+      float f[8];
+      x[v].get(f);
+      drop.apply((uint64_t)(a.drop.row0 + row[v]) * (a.H / 8) + c / 8, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += f[e];
+      load(j + v + kDirectAhead, v);
+    }
+  }
+  if (w > 0) Eight<float>::store(&red[w - 1][8 * lane], acc);
+  __syncthreads();
+  if (w > 0 || !in) return;
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {
+    float f[8];
+    load8f(&red[u][8 * lane], f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += f[e];
+  }
+  float* out = a.dtable + (int64_t)k * a.lddt + c;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] *= a.scale;
+  if (a.accumulate) {
+    float o[8];
+    load8f(out, o);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += o[e];
+  }
+  Eight<float>::store(out, acc);
+}
+
 // ------------------------------------------------------------------ the plan
 struct Plan {
   int64_t tiles;  // of the sums
@@ -465,6 +559,13 @@ hipError_t forward(const EmbedArgs& a, hipStream_t stream) {
 
 template <typename T>
 hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
+  if (a.rows <= kDirectRows) {
+    const int64_t slabs = (a.H + kSlab - 1) / kSlab, most = 4 * (int64_t)device_cus();
+    const int64_t zero = a.accumulate ? 0 : (a.V + 3) / 4 < most ? (a.V + 3) / 4 : most;
+    hipLaunchKernelGGL(embed_direct_kernel<T>, dim3((unsigned)(a.rows * slabs + zero)), dim3(256), 0, stream, a,
+                       (int)(a.rows * slabs));
+    return hipGetLastError();
+  }
   const Plan p = plan(a.rows, a.H);
   char* ws = static_cast<char*>(a.workspace);
   uint32_t* arr[4];
@@ -531,7 +632,7 @@ hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((embed_sum_kernel<T, true>), grid, dim3(64), 0, stream, a, u);
   else
     hipLaunchKernelGGL((embed_sum_kernel<T, false>), grid, dim3(64), 0, stream, a, u);
-  if ((e = hipGetLastError()) != hipSuccess || a.rows <= kTile) return e;  // no long run
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(embed_join_kernel,
                      dim3((unsigned)p.tiles, (unsigned)((a.H + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
                      stream, a, u);

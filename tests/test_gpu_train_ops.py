@@ -569,8 +569,11 @@ EMBED_CASES = [
     (8191, 16, 9000, "f32", "i64", "runs", 0.0, 1.0),
     (16384, 8, 20000, "f32", "i64", "runs", 0.0, 1.0),
     (16385, 512, 20000, "bf16", "i64", "runs", 0.0, 1.0),  # one more than it takes
-    (16, 16, 4, "f32", "i64", "same", 0.0, 1.0),
     (17, 16, 4, "f32", "i64", "same", 0.0, 1.0),
+    (256, 520, 4, "bf16", "i32", "same", 0.1, 1.0),        # the most rows without a sorted list, one run
+    (255, 24, 90, "f32", "i64", "runs", 0.0, 1.0),
+    (200, 1032, 300, "bf16", "i64", "outside", 0.1, 1.0),
+    (257, 16, 4, "f32", "i64", "same", 0.0, 1.0),          # one more
 ]
 
 
