@@ -43,7 +43,7 @@ __device__ __forceinline__ void init_moments(Moments (*red)[TEAM / 64], int H, i
 template <int TEAM, int PER>
 __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int tid, bool rms, float inv_h, float eps,
                                             Moments* red, float& mean, float& rstd) {
-  constexpr int NW = TEAM / 64;
+  constexpr int NW = TEAM / 64, LANES = TEAM < 64 ? TEAM : 64;
   float s = 0.f, q = 0.f, m = 0.f;
   if (!rms) {
 #pragma unroll
@@ -52,7 +52,7 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += v[p][e];
       }
-    s = wave_sum(s);
+    s = lanes_sum<LANES>(s);
     m = s * (NW > 1 ? red[tid >> 6].inv : inv_h);
   }
 #pragma unroll
@@ -64,7 +64,7 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
         q = fmaf(d, d, q);
       }
     }
-  q = wave_sum(q);
+  q = lanes_sum<LANES>(q);
   if constexpr (NW > 1) {
     if ((tid & 63) == 0) {
       red[tid >> 6].s = s;
@@ -89,16 +89,16 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
   rstd = __builtin_amdgcn_rsqf(fmaf(q, inv_h, eps));  // within an ulp
 }
 
-// Forward.  NT threads, teams of TEAM (the workgroup, or one wave of it); a
-// team takes rows in turn, so the parameters stay in its registers (read per
+// Forward.  NT threads, teams of TEAM (the workgroup, one wave of it, or for
+// narrow rows a half or a quarter of one); a team takes rows in turn, so the parameters stay in its registers (read per
 // row they would be 2.5 times the activations' bytes, out of L2), with the
 // gate folded into the norm after the branch:
 //   gate n = bh (gate gamma) + gate beta.
 // The next row's x and b are on their way while a row is worked on.
 template <typename T, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
-  static_assert(TEAM == NT || TEAM == 64, "");
-  __shared__ Moments red[2][TEAM / 64];
+  static_assert(TEAM == NT || TEAM <= 64, "");
+  __shared__ Moments red[2][TEAM > 64 ? TEAM / 64 : 1];
   constexpr int TEAMS = NT / TEAM;
   const int H = a.H, tid = threadIdx.x % TEAM;
   const int64_t step = (int64_t)gridDim.x * TEAMS;
@@ -231,7 +231,7 @@ __host__ __device__ inline Slots bn_slots(const BlockNormArgs& a) {
 template <int TEAM, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  for (int i = 0; i < N; ++i) v[i] = lanes_sum<TEAM < 64 ? TEAM : 64>(v[i]);
   if constexpr (TEAM > 64) {
     constexpr int NW = TEAM / 64;
     if ((tid & 63) == 0) {
@@ -255,8 +255,8 @@ template <typename T, bool POST, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
   constexpr int TEAMS = NT / TEAM;
   // the team's exchanges alternate between two images, as in the forward
-  __shared__ float red_all[TEAMS][2][3 * (TEAM / 64)];
-  auto& red = red_all[threadIdx.x / TEAM];
+  __shared__ float red_all[TEAM > 64 ? TEAMS : 1][2][TEAM > 64 ? 3 * (TEAM / 64) : 1];
+  auto& red = red_all[TEAM > 64 ? threadIdx.x / TEAM : 0];
   constexpr bool AHEAD = sizeof(T) * PER <= 4;  // two groups of fp32 leave no registers for a row ahead
   const int H = a.H, tid = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
   const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block;
@@ -429,22 +429,30 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
   // The workgroup's column sums: its teams' in team order.
   const Slots slots = bn_slots(a);
   float* part = a.part + (int64_t)blockIdx.x * slots.n * H;
+  constexpr int SLOTS = POST ? 4 : 3;  // S3 is of the norm after the branch
+  if constexpr (TEAMS > 1) {
+    __shared__ __attribute__((aligned(16))) float comb[SLOTS][TEAMS][8 * TEAM * PER];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((i == 3 && !POST) || !slots.on[i]) continue;
-    if constexpr (TEAMS > 1) {
-      __shared__ __attribute__((aligned(16))) float comb[TEAMS][8 * TEAM * PER];
-      __syncthreads();
+    for (int i = 0; i < SLOTS; ++i) {
+      if (!slots.on[i]) continue;
 #pragma unroll
-      for (int p = 0; p < PER; ++p) Eight<float>::store(&comb[team][8 * (tid + TEAM * p)], sum[i][p]);
-      __syncthreads();
-      for (int c = threadIdx.x; c < H; c += NT) {
-        float t = comb[0][c];
+      for (int p = 0; p < PER; ++p) Eight<float>::store(&comb[i][team][8 * (tid + TEAM * p)], sum[i][p]);
+    }
+    __syncthreads();
+    for (int c = 4 * threadIdx.x; c < H; c += 4 * NT) {
 #pragma unroll
-        for (int u = 1; u < TEAMS; ++u) t += comb[u][c];
-        part[slots.at[i] * H + c] = t;
+      for (int i = 0; i < SLOTS; ++i) {
+        if (!slots.on[i]) continue;
+        f32x4 t = *reinterpret_cast<const f32x4*>(&comb[i][0][c]);
+#pragma unroll
+        for (int u = 1; u < TEAMS; ++u) t += *reinterpret_cast<const f32x4*>(&comb[i][u][c]);
+        *reinterpret_cast<f32x4*>(part + slots.at[i] * H + c) = t;
       }
-    } else {
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+      if (!slots.on[i]) continue;
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
         const int c = 8 * (tid + TEAM * p);
@@ -535,6 +543,8 @@ hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
 template <typename T>
 hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
+  if (a.H <= 128) return fwd<T, 256, 16, 1>(a, stream);
+  if (a.H <= 256) return fwd<T, 256, 32, 1>(a, stream);
   if (a.H <= 512) return fwd<T, 256, 64, 1>(a, stream);
   if (a.H <= 1024) return fwd<T, 256, 64, 2>(a, stream);
   if (a.H <= 2048) return fwd<T, 256 / P, 256 / P, P>(a, stream);
@@ -550,6 +560,8 @@ hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
 template <typename T>
 hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
+  if (a.H <= 128) return bwd<T, 256, 16, 1>(a, stream);
+  if (a.H <= 256) return bwd<T, 256, 32, 1>(a, stream);
   if (a.H <= 512) return bwd<T, 256, 64, 1>(a, stream);
   if (a.H <= 1024) return bwd<T, 512, 64, 2>(a, stream);
   if (a.H <= 2048) return bwd<T, 512, 256 / P, P>(a, stream);
@@ -560,7 +572,7 @@ hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
 // Teams of a workgroup of the backward (as dispatched above), and the most
 // workgroups a number of rows takes.
 int teams_of(int H, int f32) {
-  if (H <= 512) return 4;
+  if (H <= 512) return H <= 128 ? 16 : H <= 256 ? 8 : 4;
   if (H <= 1024) return 8;
   if (H <= 2048) return f32 ? 2 : 4;
   return H <= 4096 && !f32 ? 2 : 1;

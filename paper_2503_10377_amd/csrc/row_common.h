@@ -23,6 +23,22 @@ __device__ __forceinline__ float wave_sum(float v) {
   return sum_groups(v);
 }
 
+// The same over the N = 16, 32 or 64 consecutive lanes that hold a row.
+template <int N>
+__device__ __forceinline__ float lanes_sum(float v) {
+  static_assert(N == 16 || N == 32 || N == 64, "");
+  if constexpr (N == 64) return wave_sum(v);
+  v += dpp<0xB1>(v);
+  v += dpp<0x4E>(v);
+  v += dpp<0x141>(v);
+  v += dpp<0x140>(v);
+  if constexpr (N == 32) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
+
 // Four floats of a buffer whose caller promises a float's alignment.
 using f32x4_a4 = float __attribute__((ext_vector_type(4), aligned(4)));
 

@@ -352,6 +352,11 @@ NORM_CASES = [
     (2, 8192, 8200, "bf16", "none", "none", "channel", False, 0.4, 1.0, 1.0),
     (5000, 72, 72, "bf16", "layer", "layer", "channel", True, 0.1, 1.0, 1.0),
     (9, 64, 64, "f32", "none", "none", "none", False, 0.0, 0.0, 1.0),
+    (1000, 128, 136, "f32", "rms", "layer", "token", True, 0.1, 1.0, 1.0),
+    (77, 136, 136, "bf16", "layer", "rms", "channel", True, 0.1, 1.0, 1.0),
+    (33, 256, 256, "f32", "none", "layer", "channel", True, 0.1, 1.0, 1.0),
+    (1100, 768, 768, "bf16", "layer", "layer", "channel", True, 0.1, 1.0, 1.0),
+    (515, 3000, 3008, "bf16", "layer", "layer", "channel", True, 0.1, 1.0, 1.0),
 ]
 
 
