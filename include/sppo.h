@@ -522,7 +522,7 @@ typedef struct {
   sppo_norm post, pre;
   sppo_gate gate_kind;
   float eps;                /* where there is a norm: > 0, a normal number  */
-  float residual_scale, branch_scale;  /* finite                            */
+  float residual_scale, branch_scale;  /* finite, |branch_scale| < 2^112    */
   const float* post_gamma;  /* [H], needed unless post is NONE              */
   const float* post_beta;   /* [H] or NULL                                  */
   const float* gate;        /* [H] or [rows], needed unless gate is NONE    */
@@ -575,8 +575,8 @@ sppo_status sppo_block_norm_bwd(const sppo_block_norm* bn, int64_t rows, const s
                                 void* db, int64_t lddb, const sppo_block_norm_grads* grads, int32_t accumulate,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
-/* y[r] = keep * (scale * table[ids[r]]), table [V, H] with row stride ldt;
- * ids [rows] of id_type.  An id outside [0, V) (padding, another rank's part
+/* y[r] = keep * (scale * table[ids[r]]), table [V, H] with row stride ldt,
+ * |scale| < 2^112; ids [rows] of id_type.  An id outside [0, V) (padding, another rank's part
  * of a split vocabulary) gives a row of zeros, and nothing is read for it.
  * drop: NULL for none (W = H).  rows <= 2^28, V < 2^31, H <= 2^20
  * and rows * H <= 2^38 (UNSUPPORTED otherwise; the gradient's too). */

@@ -281,7 +281,11 @@ class ChunkedLayer:
         ends, dy = self.ends, inp["dy"]
         x = inp["x"] if self.vocab is None else None
         drop_p = ends.dropout if ends is not None else 0.0
-        id_type = "i32" if x is None and inp["tokens"].dtype == torch.int32 else "i64"
+        if x is None:
+            tokens = inp["tokens"]
+            if tokens.dtype not in (torch.int32, torch.int64) or tokens.shape != (self.S,) or not tokens.is_contiguous():
+                raise ValueError(f"tokens must be [{self.S}] contiguous int32 or int64")
+            id_type = "i32" if tokens.dtype == torch.int32 else "i64"
 
         def mark(label):
             self.pacer.boundary(s)
@@ -316,7 +320,7 @@ class ChunkedLayer:
         embed = timed("embedding", L.sppo_embedding_fwd)
         embed_bwd = timed("embedding", L.sppo_embedding_bwd)
         drop = lambda site, row0: L.drop_spec(drop_p, seed, offset + site, row0) if drop_p > 0 else None
-        lookup = lambda n, c0: embed(n, H, self.vocab, inp["tokens"][c0:], p["w_emb"], H, self.embed_scale,
+        lookup = lambda n, c0: embed(n, H, self.vocab, tokens[c0:], p["w_emb"], H, self.embed_scale,
                                      drop(DROP_EMBED, c0), self.x, H, "bf16", id_type, s)
         pairs = lambda a: self.chunk_len(a[1]) * self.offsets[a[1]] + self.chunk_len(a[1]) * (self.chunk_len(a[1]) + 1) // 2
         attn_fwd = timed("attn_fwd", L.sppo_attn_fwd_chunk, lambda a: 4 * self.D * self.Hq * pairs(a))
@@ -450,7 +454,7 @@ class ChunkedLayer:
                                  dxi, H, out["dg1"], out["db1"], self.ws, self.ws_bytes,
                                  accumulate=0 if first else 1, stream=s)
             if x is None:
-                embed_bwd(n, H, self.vocab, inp["tokens"][c0:], dxi, H, self.embed_scale, drop(DROP_EMBED, c0),
+                embed_bwd(n, H, self.vocab, tokens[c0:], dxi, H, self.embed_scale, drop(DROP_EMBED, c0),
                           out["dw_emb"], H, self.emb_ws, self.emb_ws_bytes, add, "bf16", id_type, s)
             arena.release(slot)
         mark(("end", -1))

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   }
   const Dropper drop(a.drop);
   const bool post = a.post != kNone, pre = a.pre != kNone;
-  const float inv_h = 1.f / H;
+  const float inv_h = 1.f / H, scale = a.bscale * drop.scale;
   Eight<T> xn[PER], bn[PER];
   auto load = [&](int64_t r) {
 #pragma unroll
@@ -161,9 +161,7 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
         a.post_rstd[row] = rstd;
       }
     }
-    float scale = a.bscale * drop.scale;
-    if (a.gate_kind == kToken) scale *= a.gate[row];
-    const float shift = -mean * rstd;
+    const float shift = -mean * rstd, gate = a.gate_kind == kToken ? a.gate[row] : 1.f;
     const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
@@ -171,6 +169,10 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       if (c < H) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift), pg[p][e], pb[p][e]);
+        if (a.gate_kind == kToken) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[p][e] *= gate;
+        }
         drop.mask(g0 + c / 8, v[p]);
         float x[8];
         xr[p].get(x);

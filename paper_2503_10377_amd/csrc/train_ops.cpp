@@ -13,7 +13,10 @@
 namespace {
 
 sppo_status fail(sppo_status st, const char* msg) {
-  sppo::set_thread_error(msg);
+  try {
+    sppo::set_thread_error(msg);
+  } catch (...) {  // no memory for the message: the status says enough
+  }
   return st;
 }
 
@@ -28,6 +31,10 @@ bool dtype_ok(int dtype) { return dtype == SPPO_F32 || dtype == SPPO_BF16; }
 
 // A row-major activation of `width` columns.
 bool act_ok(const void* p, int64_t ld, int64_t width) { return p && aligned(p, 16) && ld >= width && ld % 8 == 0; }
+
+// A scale that the kernels multiply with the dropout's (at most 65536): finite
+// after that, so that it leaves a dropped element zero.
+bool scale_ok(float scale) { return std::isfinite(scale * 65536.f); }
 
 // The dropout of rows x width elements; NULL: none.
 sppo_status drop_args(const sppo_drop* d, int64_t rows, int64_t width, sppo::DropArgs* out) {
@@ -60,8 +67,8 @@ sppo_status check_norm(const sppo_block_norm* bn, int64_t rows) {
     return fail(SPPO_ERR_INVALID_ARG, "block norm: unknown norm or gate");
   if ((post != SPPO_NORM_NONE || pre != SPPO_NORM_NONE) && !(bn->eps > 0.f && std::isnormal(bn->eps)))
     return fail(SPPO_ERR_INVALID_ARG, "block norm: eps must be positive and a normal number");
-  if (!std::isfinite(bn->residual_scale) || !std::isfinite(bn->branch_scale))
-    return fail(SPPO_ERR_INVALID_ARG, "block norm: a scale is not finite");
+  if (!std::isfinite(bn->residual_scale) || !scale_ok(bn->branch_scale))
+    return fail(SPPO_ERR_INVALID_ARG, "block norm: a scale is not finite, or branch_scale 2^112 and above");
   if ((post != SPPO_NORM_NONE && !bn->post_gamma) || (pre != SPPO_NORM_NONE && !bn->pre_gamma) ||
       (gate != SPPO_GATE_NONE && !bn->gate))
     return fail(SPPO_ERR_INVALID_ARG, "block norm: a norm without gamma, or no gate values");
@@ -108,7 +115,7 @@ sppo_status check_embedding(int dtype, int id_type, int64_t rows, int32_t H, int
   if (rows <= 0 || V <= 0 || H <= 0 || H % 8) return fail(SPPO_ERR_INVALID_ARG, "embedding: bad rows, V or H");
   if (!ids || !aligned(ids, id_type == SPPO_I64 ? 8 : 4))
     return fail(SPPO_ERR_INVALID_ARG, "embedding: null or misaligned ids");
-  if (!std::isfinite(scale)) return fail(SPPO_ERR_INVALID_ARG, "embedding: the scale is not finite");
+  if (!scale_ok(scale)) return fail(SPPO_ERR_INVALID_ARG, "embedding: the scale is not finite, or 2^112 and above");
   if (rows > sppo::kMaxEmbedRows || V > INT32_MAX || H > sppo::kMaxEmbedH || rows > sppo::kMaxEmbedElems / H)
     return fail(SPPO_ERR_UNSUPPORTED, "embedding: rows above 2^28, V above 2^31 - 1, H above 2^20 or rows * H above 2^38");
   return SPPO_OK;

@@ -130,3 +130,11 @@ def test_layer_with_ends_refuses():
         BlockEnds(dropout=1.0)
     with pytest.raises(ValueError):
         ChunkedLayer(256, 1, 2, 2, 128, vocab=0)
+    lay = ChunkedLayer(256, 1, 2, 2, 128, vocab=10)
+    out = lay.alloc_outputs()
+    inp, p = setup(256, 2, 2, 128, None, 10, 1)
+    t = inp["tokens"].cuda()
+    for bad in (t[:255], t.to(torch.int16), t.repeat(2)[::2]):  # too short, another type, with gaps
+        with pytest.raises(ValueError):
+            lay.step({"tokens": bad, "dy": inp["dy"].cuda()}, {k: v.cuda() for k, v in p.items()}, out)
+    lay.close()

@@ -447,6 +447,17 @@ def test_block_norm_gates_only_what_is_kept():
         assert torch.equal(got[2]["gate"], base[2]["gate"])
 
 
+def test_block_norm_drops_what_an_infinite_gate_makes():
+    announce("block norm, infinite gate of a row")
+    c = Case(8, 256, 256, "bf16", "layer", "none", "token", True, 0.5, seed=16)
+    c.dpar["gate"][3] = float("inf")
+    h, _ = c.forward()
+    want = to_np(c.x)[3, :256]
+    dropped = c.keep[3] == 0
+    assert np.array_equal(to_np(h)[3][dropped], want[dropped])
+    assert not np.isfinite(to_np(h)[3][~dropped]).any()
+
+
 def test_block_norm_gradient_matches_differences():
     """The fp32 backward along random directions of every input against
     central differences of the kernel's own forward, e = 2^-6: the forward's

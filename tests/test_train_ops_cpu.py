@@ -191,7 +191,7 @@ FULL = dict(post="layer", pre="layer", gate_kind="channel", post_gamma=A, post_b
 @pytest.mark.parametrize("change,status", [
     (dict(H=12), BAD), (dict(H=8200), BAD), (dict(H=0), BAD), (dict(dtype=9), BAD), (dict(post=3), BAD),
     (dict(pre=-1), BAD), (dict(gate_kind=7), BAD), (dict(eps=0.0), BAD), (dict(eps=float("inf")), BAD), (dict(eps=1e-40), BAD),
-    (dict(residual_scale=float("nan")), BAD), (dict(branch_scale=float("inf")), BAD), (dict(post_gamma=None), BAD),
+    (dict(residual_scale=float("nan")), BAD), (dict(branch_scale=float("inf")), BAD), (dict(branch_scale=-1e34), BAD), (dict(post_gamma=None), BAD),
     (dict(pre_gamma=None), BAD), (dict(gate=None), BAD), (dict(pre_beta=A + 2), BAD),
 ])
 def test_block_norm_refuses_a_bad_description(change, status):
@@ -239,7 +239,7 @@ def test_block_norm_workspace_grows_with_rows():
 
 @pytest.mark.parametrize("change,status", [
     (dict(rows=0), BAD), (dict(V=0), BAD), (dict(H=20), BAD), (dict(H=0), BAD), (dict(ids=None), BAD),
-    (dict(ids=A + 4), BAD), (dict(dtype=4), BAD), (dict(id_type=2), BAD), (dict(scale=float("nan")), BAD),
+    (dict(ids=A + 4), BAD), (dict(dtype=4), BAD), (dict(id_type=2), BAD), (dict(scale=float("nan")), BAD), (dict(scale=1e34), BAD),
     (dict(act=None), BAD), (dict(act=A + 8), BAD), (dict(ld=56), BAD), (dict(table=None), BAD), (dict(table=A + 4), BAD),
     (dict(ldt=60), BAD), (dict(p=1.0), BAD), (dict(rows=(1 << 28) + 1), UNSUP), (dict(V=1 << 31), UNSUP),
     (dict(rows=1 << 28, H=1032, ld=1032, ldt=1032), UNSUP),
