@@ -253,8 +253,11 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
 // A team takes rows in turn with the parameters in registers (gate and gamma
 // as one) and the next row's h, dz, dh and b on their way, and adds its part of
 // the column sums row by row.
-template <typename T, bool POST, int NT, int TEAM, int PER>
+// MODE: what the branch needs beyond its mask.
+enum { kPlain = 0, kGated = 1, kNormed = 2 };
+template <typename T, int MODE, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
+  constexpr bool POST = MODE == kNormed;
   constexpr int TEAMS = NT / TEAM;
   // the team's exchanges alternate between two images, as in the forward
   __shared__ float red_all[TEAM > 64 ? TEAMS : 1][2][TEAM > 64 ? 3 * (TEAM / 64) : 1];
@@ -280,14 +283,14 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           zn[p].load(static_cast<const T*>(a.dz) + row * a.lddz + c);
         }
         if (a.dh) dn[p].load(static_cast<const T*>(a.dh) + row * a.lddh + c);
-        if (a.b) bn[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
+        if (MODE != kPlain && a.b) bn[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
       }
     }
     if (pre) st[0] = a.pre_rstd[row];
     if (a.pre == kLayer) st[1] = a.pre_mean[row];
     if (POST) st[2] = a.post_rstd[row];
     if (a.post == kLayer) st[3] = a.post_mean[row];
-    if (a.gate_kind == kToken) st[4] = a.gate[row];
+    if (MODE != kPlain && a.gate_kind == kToken) st[4] = a.gate[row];
   };
   int64_t row = r0 + team;
   if (row < r1) load(row);  // on its way before the parameters
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
     if (c < H) {
       if (pre) load8f(a.pre_gamma + c, qg[p]);
       if (POST) load8f(a.post_gamma + c, pg[p]);
-      if (a.gate_kind == kChannel) {
+      if (MODE != kPlain && a.gate_kind == kChannel) {
         float g[8];
         load8f(a.gate + c, g);
 #pragma unroll
@@ -387,7 +390,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) s[2] += D[p][e] * bt[e];
         }
-        if (POST || a.gate_kind != kNone) {
+        if constexpr (MODE != kPlain) {
           float bv[8];
           br[p].get(bv);
 #pragma unroll
@@ -403,11 +406,11 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
         }
       }
     }
-    if (POST || a.gate_kind == kToken) {
+    if (POST || (MODE == kGated && a.gate_kind == kToken)) {
       team_sum<TEAM>(s, tid, red[ph]);
       ph ^= 1;
     }
-    if (a.gate_kind == kToken && a.d_gate && tid == 0 && real) a.d_gate[row] = s[1] + s[2];
+    if (MODE != kPlain && a.gate_kind == kToken && a.d_gate && tid == 0 && real) a.d_gate[row] = s[1] + s[2];
     const float m1 = a.post == kLayer ? s[0] * inv_h : 0.f, m2 = s[1] * inv_h;
     const float kr = k * rstd;
 #pragma unroll
@@ -419,7 +422,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           br[p].get(bv);
 #pragma unroll
           for (int e = 0; e < 8; ++e) D[p][e] = kr * (D[p][e] - m1 - fmaf(bv[e], rstd, shift) * m2);
-        } else {
+        } else if constexpr (MODE == kGated) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) D[p][e] *= k;
         }
@@ -431,7 +434,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
   // The workgroup's column sums: its teams' in team order.
   const Slots slots = bn_slots(a);
   float* part = a.part + (int64_t)blockIdx.x * slots.n * H;
-  constexpr int SLOTS = POST ? 4 : 3;  // S3 is of the norm after the branch
+  constexpr int SLOTS = 2 + MODE;  // S2 is of the gate or the norm after the branch, S3 of that norm
   if constexpr (TEAMS > 1) {
     __shared__ __attribute__((aligned(16))) float comb[SLOTS][TEAMS][8 * TEAM * PER];
 #pragma unroll
@@ -532,9 +535,11 @@ template <typename T, int NT, int TEAM, int PER>
 hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)a.nblocks), block(NT);
   if (a.post != kNone)
-    hipLaunchKernelGGL((bn_bwd_kernel<T, true, NT, TEAM, PER>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((bn_bwd_kernel<T, kNormed, NT, TEAM, PER>), grid, block, 0, stream, a);
+  else if (a.gate_kind != kNone)
+    hipLaunchKernelGGL((bn_bwd_kernel<T, kGated, NT, TEAM, PER>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((bn_bwd_kernel<T, false, NT, TEAM, PER>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((bn_bwd_kernel<T, kPlain, NT, TEAM, PER>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 

@@ -590,6 +590,9 @@ EMBED_CASES = [
     (255, 24, 90, "f32", "i64", "runs", 0.0, 1.0),
     (200, 1032, 300, "bf16", "i64", "outside", 0.1, 1.0),
     (257, 16, 4, "f32", "i64", "same", 0.0, 1.0),          # one more
+    (1024, 520, 70, "bf16", "i64", "runs", 0.1, 1.0),
+    (1000, 16, 300, "f32", "i32", "outside", 0.0, 1.0),
+    (1025, 16, 4, "f32", "i64", "same", 0.0, 1.0),
 ]
 
 
