@@ -161,23 +161,19 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
         a.post_rstd[row] = rstd;
       }
     }
-    const float shift = -mean * rstd, gate = a.gate_kind == kToken ? a.gate[row] : 1.f;
+    const float shift = -mean * rstd, factor = a.gate_kind == kToken ? scale * a.gate[row] : scale;
     const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
       if (c < H) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift), pg[p][e], pb[p][e]);
-        if (a.gate_kind == kToken) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[p][e] *= gate;
-        }
+        for (int e = 0; e < 8; ++e) v[p][e] = factor * fmaf(fmaf(v[p][e], rstd, shift), pg[p][e], pb[p][e]);
         drop.mask(g0 + c / 8, v[p]);
         float x[8];
         xr[p].get(x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(v[p][e], scale, a.alpha * x[e]);
+        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(a.alpha, x[e], v[p][e]);
         Eight<T>::store(static_cast<T*>(a.h) + row * a.ldh + c, v[p]);
       }
     }
