@@ -274,17 +274,21 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs s, int spli
 }
 
 // ------------------------------------------------------------------ the sums
-// A wave takes kTile sorted places and kSlab columns; the waves of a tile come
-// one after another, so that whole rows are on their way at a time (8192 rows
-// of 4096 columns, 3300 tokens: 34 us, 5.2 TB/s; with the tiles first 41).
-// After a fill of the table it takes 44 us: the fill's last 256 MB are still
-// in the memory-side cache and leave it while the sums run (stores that go
-// past that cache make the fill 38 us longer).  A run of at most kTile
-// rows belongs to the tile where it begins, which follows it past its end, so
-// it is summed at once; only of a longer run do the tiles it crosses leave
-// partial sums.  The last places of a tile before, its own and those it may
-// follow a run to fit the wave's lanes, one each.
-constexpr int kTile = 16;
+// A workgroup takes kGroup sorted places and kSlab columns, each of its waves
+// kTile of the places; the workgroups of a group's columns come one after
+// another, so that whole rows are on their way at a time (8192 rows of 4096
+// columns, 3300 tokens: 34 us, 5.2 TB/s; with the places first 41).  After a
+// fill of the table it takes 44 us: the fill's last 256 MB are still in the
+// memory-side cache and leave it while the sums run (stores that go past that
+// cache make the fill 38 us longer).
+//
+// A run of at most kTile rows belongs to the wave where it begins, which
+// follows it past its places, so it is summed at once.  Of a longer run the
+// waves that it crosses leave partial sums: in LDS, where the workgroup adds
+// them in order, and of a run that also crosses workgroups those sums in `part`
+// for the last kernel.  The last places before a wave's own, its own and those
+// it may follow a run to fit its lanes, one each.
+constexpr int kTile = 16, kGroup = 4 * kTile;
 constexpr int kSlab = 64 * 8;
 constexpr int kAhead = 4;  // rows on their way
 
@@ -292,7 +296,7 @@ struct SumArgs {
   int64_t n;
   const uint32_t* key;  // sorted tokens (outside the table: V, at the end)
   const uint32_t* row;
-  float* part;          // [tiles][2][H] of long runs: the one that enters the tile, the one that leaves it
+  float* part;          // [groups][2][H] of long runs: the one that enters the group, the one that leaves it
 };
 
 // The rows' addresses depend on nothing but the sorted list, so kAhead rows
@@ -300,12 +304,18 @@ struct SumArgs {
 // the places where runs begin (read where a run ends, each costs a trip to
 // memory).
 template <typename T, bool ADD>
-__global__ __launch_bounds__(64) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
-  const uint32_t slabs = (a.H + kSlab - 1) / kSlab, tile = blockIdx.x / slabs;
-  const int lane = threadIdx.x, c = (blockIdx.x - tile * slabs) * kSlab + 8 * lane;
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
+  // A wave's partial sums: of a long run that enters it and of one that leaves it.
+  __shared__ __attribute__((aligned(16))) float part[4][2][kSlab];
+  __shared__ uint32_t enters[4], leaves[4];  // their tokens; V: there is none
+  __shared__ uint32_t ends[4];               // whether the run that enters ends with the wave's places or before
+  const uint32_t slabs = (a.H + kSlab - 1) / kSlab, group = blockIdx.x / slabs;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int c0 = (blockIdx.x - group * slabs) * kSlab, c = c0 + 8 * lane;
   const bool in = c < a.H;
   const uint32_t V = (uint32_t)a.V;
-  const int64_t at = (int64_t)tile * kTile - kTile + lane;  // lane kTile + u holds the tile's place u
+  // lane kTile + u holds the wave's place u
+  const int64_t at = (int64_t)group * kGroup + w * kTile - kTile + lane;
   const bool there = at >= 0 && at < s.n;
   const uint32_t my_key = there ? s.key[at] : V, my_row = there ? s.row[at] : 0;
   auto key_at = [&](int u) { return (uint32_t)__builtin_amdgcn_readlane(my_key, kTile + u); };
@@ -316,23 +326,36 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
     from = __ffsll((unsigned long long)m) - 1 - kTile;
     to = 64 - __clzll(m) - kTile;
   };
-  if (key_at(0) >= V) return;
-  int from, to, first = 0, stop = kTile;
-  run(0, from, to);
-  bool entered = from < 0;
-  if (entered && to - from <= kTile) {  // short: the tile before sums it
-    first = to;
-    entered = false;
-  }
-  bool leaves = false;  // the last run, a long one
-  if (key_at(kTile - 1) < V) {
-    run(kTile - 1, from, to);
-    if (to > kTile) {
-      if (to - from <= kTile) stop = to;
-      else leaves = true;
+  int first = 0, stop = 0;                // the places to sum
+  bool enter = false, leave = false;      // the first run began before, the last goes on (long ones)
+  uint32_t enter_key = V, leave_key = V;
+  if (key_at(0) < V) {
+    int from, to;
+    stop = kTile;
+    run(0, from, to);
+    enter = from < 0;
+    if (enter && to - from <= kTile) {  // short: the wave before sums it
+      first = to;
+      enter = false;
     }
-  } else {
-    stop = __popcll(__ballot(lane >= kTile && lane < 2 * kTile && my_key < V));
+    if (enter) {
+      enter_key = key_at(0);
+      if (lane == 0) ends[w] = to <= kTile;
+    }
+    if (key_at(kTile - 1) < V) {
+      run(kTile - 1, from, to);
+      if (to > kTile) {
+        if (to - from <= kTile) stop = to;
+        else leave = true;
+      }
+      if (leave && from >= 0) leave_key = key_at(kTile - 1);
+    } else {
+      stop = __popcll(__ballot(lane >= kTile && lane < 2 * kTile && my_key < V));
+    }
+  }
+  if (lane == 0) {
+    enters[w] = enter_key;
+    leaves[w] = leave_key;
   }
   const Dropper drop(a.drop);
   Eight<T> x[kAhead];
@@ -353,7 +376,7 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
 #pragma unroll
     for (int v = 0; v < kAhead; ++v) {
       const int u = j + v;
-      if (u >= stop) return;
+      if (u >= stop) break;
       float f[8];
       x[v].get(f);
       drop.apply((uint64_t)(a.drop.row0 + row_at(u)) * (a.H / 8) + c / 8, f);
@@ -369,42 +392,79 @@ __global__ __launch_bounds__(64) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
       const bool last = u + 1 == stop;
       if (!last && !begins(u + 1)) continue;
       float o[8];
-      if (entered || (last && leaves)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = acc[e] * a.scale;
-        if (in) Eight<float>::store(s.part + ((int64_t)tile * 2 + (entered ? 0 : 1)) * a.H + c, o);
+      for (int e = 0; e < 8; ++e) o[e] = acc[e] * a.scale;
+      if (enter || (last && leave)) {
+        Eight<float>::store(&part[w][enter ? 0 : 1][8 * lane], o);
       } else {
+        if constexpr (ADD) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = ADD ? acc[e] * a.scale + base[e] : acc[e] * a.scale;
+          for (int e = 0; e < 8; ++e) o[e] += base[e];
+        }
         if (in) Eight<float>::store(a.dtable + (int64_t)key_at(u) * a.lddt + c, o);
       }
-      entered = false;
+      enter = false;
     }
   }
+  __syncthreads();
+  // The waves' partial sums in order, two columns a thread.
+  const int lc = 2 * threadIdx.x;
+  if (c0 + lc >= a.H) return;
+  float2 sum = {0.f, 0.f};
+  uint32_t k = V;        // the open run
+  bool before = false;   // it entered the group
+  float* group_part = s.part + (int64_t)group * 2 * a.H + c0 + lc;
+  for (int u = 0; u < 4; ++u) {
+    if (enters[u] < V) {
+      const float2 p = *reinterpret_cast<const float2*>(&part[u][0][lc]);
+      if (k == V) before = true;
+      k = enters[u];
+      sum.x += p.x;
+      sum.y += p.y;
+      if (ends[u]) {
+        float2* out = reinterpret_cast<float2*>(before ? group_part : a.dtable + (int64_t)k * a.lddt + c0 + lc);
+        if (ADD && !before) {
+          const float2 o = *out;
+          sum.x += o.x;
+          sum.y += o.y;
+        }
+        *out = sum;
+        k = V;
+        before = false;
+        sum = {0.f, 0.f};
+      }
+    }
+    if (leaves[u] < V) {
+      k = leaves[u];
+      sum = *reinterpret_cast<const float2*>(&part[u][1][lc]);
+    }
+  }
+  if (k < V) *reinterpret_cast<float2*>(group_part + (before ? 0 : a.H)) = sum;
 }
 
-// The long runs: the one that begins in this tile and leaves it, if there is
-// one, from the tile's second partial sum and the following tiles' first ones,
-// in kJoinGroups groups of tiles in turn and then in group order.  Most
-// workgroups find none and end after one trip to memory.
+// The long runs across groups: the one that begins in this group and leaves
+// it, if there is one, from the group's second partial sum and the following
+// groups' first ones, in kJoinGroups rows of groups in turn and then in row
+// order.  Most workgroups find none and end after one trip to memory.
 constexpr int kJoinCols = 256, kJoinGroups = 4;
 constexpr int kJoinThreads = kJoinCols / 4 * kJoinGroups;
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, SumArgs s) {
   __shared__ __attribute__((aligned(16))) float red[kJoinGroups][kJoinCols];
   const int lane = threadIdx.x & 63;
-  const int64_t t = blockIdx.x, i0 = t * kTile;
-  // lane kTile + u holds place u; lane kTile - 1 the place before
-  const int64_t at = i0 - kTile + lane;
+  const int64_t t = blockIdx.x, i0 = t * kGroup;
   const uint32_t V = (uint32_t)a.V;
-  const uint32_t mine = at >= 0 && at < s.n ? s.key[at] : V;
-  const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(mine, 2 * kTile - 1);
-  if (k >= V) return;
-  const uint64_t m = __ballot(mine == k);
-  const int from = __ffsll((unsigned long long)m) - 1 - kTile, to = 64 - __clzll(m) - kTile;
-  if (from < 0 || to <= kTile || to - from <= kTile) return;
-  int64_t end = t;  // the last tile whose last place is the run's
+  static_assert(kGroup == 64, "a lane per place");
+  if (i0 + kGroup >= s.n) return;
+  const uint32_t mine = s.key[i0 + lane], after = s.key[i0 + kGroup];
+  const uint32_t before = i0 > 0 ? s.key[i0 - 1] : V;
+  const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(mine, 63);
+  if (k >= V || after != k) return;
+  const int from = __ffsll((unsigned long long)__ballot(mine == k)) - 1;
+  if (from == 0 && before == k) return;                                 // it began in an earlier group
+  if (i0 + from + kTile >= s.n || s.key[i0 + from + kTile] != k) return;  // a short run
+  int64_t end = t;  // the last group whose last place is the run's
   for (;;) {
-    const int64_t p = (end + 1 + lane) * kTile + kTile - 1;
+    const int64_t p = (end + 1 + lane) * kGroup + kGroup - 1;
     const uint64_t no = ~__ballot(p < s.n && s.key[p] == k);
     if (no) {
       end += __ffsll((unsigned long long)no) - 1;
@@ -412,7 +472,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, S
     }
     end += 64;
   }
-  if ((end + 1) * kTile < s.n && s.key[(end + 1) * kTile] == k) ++end;  // it ends inside the next one
+  if ((end + 1) * kGroup < s.n && s.key[(end + 1) * kGroup] == k) ++end;  // it ends inside the next one
   const int lc = threadIdx.x % (kJoinCols / 4) * 4, grp = threadIdx.x / (kJoinCols / 4);
   const int c = blockIdx.y * kJoinCols + lc;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -531,16 +591,16 @@ __global__ __launch_bounds__(256) void embed_direct_kernel(EmbedArgs a, int sums
 
 // ------------------------------------------------------------------ the plan
 struct Plan {
-  int64_t tiles;  // of the sums
+  int64_t groups;  // of the sums
   int64_t keys, counts, part, bytes;  // byte offsets: four arrays of n words from 0, then these
 };
 Plan plan(int64_t rows, int H) {
   Plan p;
-  p.tiles = (rows + kTile - 1) / kTile;
+  p.groups = (rows + kGroup - 1) / kGroup;
   p.keys = (rows * 4 + 255) / 256 * 256;
   p.counts = 4 * p.keys;
   p.part = p.counts + (int64_t)kMaxSortTiles * kMaxDigits * 4;
-  p.bytes = p.part + p.tiles * 2 * (int64_t)H * 4;
+  p.bytes = p.part + p.groups * 2 * (int64_t)H * 4;
   return p;
 }
 
@@ -635,14 +695,14 @@ hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
     }
   }
   SumArgs u{a.rows, s.key, s.row, reinterpret_cast<float*>(ws + p.part)};
-  const dim3 grid((unsigned)(p.tiles * ((a.H + kSlab - 1) / kSlab)));
+  const dim3 grid((unsigned)(p.groups * ((a.H + kSlab - 1) / kSlab)));
   if (a.accumulate)
-    hipLaunchKernelGGL((embed_sum_kernel<T, true>), grid, dim3(64), 0, stream, a, u);
+    hipLaunchKernelGGL((embed_sum_kernel<T, true>), grid, dim3(256), 0, stream, a, u);
   else
-    hipLaunchKernelGGL((embed_sum_kernel<T, false>), grid, dim3(64), 0, stream, a, u);
+    hipLaunchKernelGGL((embed_sum_kernel<T, false>), grid, dim3(256), 0, stream, a, u);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(embed_join_kernel,
-                     dim3((unsigned)p.tiles, (unsigned)((a.H + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
+                     dim3((unsigned)p.groups, (unsigned)((a.H + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
                      stream, a, u);
   return hipGetLastError();
 }

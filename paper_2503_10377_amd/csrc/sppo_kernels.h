@@ -304,7 +304,7 @@ struct EmbedArgs {
 };
 constexpr int64_t kMaxEmbedRows = (int64_t)1 << 28;
 constexpr int32_t kMaxEmbedH = 1 << 20;
-constexpr int64_t kMaxEmbedElems = (int64_t)1 << 38;  // the backward's grid: a wave per 16 rows x 512 columns
+constexpr int64_t kMaxEmbedElems = (int64_t)1 << 38;  // the backward's grid: 256 threads per 64 rows x 512 columns
 size_t embedding_workspace(int64_t rows, int H);
 hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t stream);
 hipError_t launch_embedding_bwd(const EmbedArgs& a, hipStream_t stream);

@@ -560,8 +560,9 @@ def make_ids(rows, V, kind, seed):
         ids = g.permutation(V)[:rows] if rows <= V else g.permutation(rows) % V
     elif kind == "zipf":
         ids = np.minimum(np.exp(g.random(rows) * np.log(V + 1.0)).astype(np.int64) - 1, V - 1)
-    elif kind == "runs":  # every run length from 1 to 40, beginning at every place of a tile, rows shuffled
+    elif kind == "runs":  # every run length from 1 to 40 and longer ones, rows shuffled
         n = g.integers(1, 41, size=rows)
+        n[::9] *= 5
         ids = g.permutation(np.repeat(np.arange(rows), n)[:rows] % V)
     else:  # padding and ids of other ranks' parts, also past 32 bits
         ids = g.integers(-3, V + 3, size=rows)
@@ -575,7 +576,7 @@ EMBED_CASES = [
     (33, 264, 7, "bf16", "i32", "outside", 0.1, 64.0),
     (257, 2056, 500, "bf16", "i64", "zipf", 0.1, 8.0),
     (31, 8192, 40, "f32", "i64", "distinct", 0.0, 1.0),
-    (64, 128, 64, "bf16", "i64", "same", 0.2, 1.0),        # a run that is exactly two tiles
+    (64, 128, 64, "bf16", "i64", "same", 0.2, 1.0),
     (3000, 72, 300, "bf16", "i64", "same", 0.0, 2.0),      # one run over every tile
     (5000, 40, 50000, "f32", "i64", "distinct", 0.0, 1.0),
     (4099, 256, 33000, "bf16", "i32", "zipf", 0.1, 1.0),
@@ -584,6 +585,8 @@ EMBED_CASES = [
     (4096, 24, 4096, "bf16", "i32", "runs", 0.0, 1.0),     # the ranking with 4, 2 and 1 lanes a row
     (8191, 16, 9000, "f32", "i64", "runs", 0.0, 1.0),
     (16384, 8, 20000, "f32", "i64", "runs", 0.0, 1.0),
+    (6000, 520, 9, "bf16", "i64", "outside", 0.1, 1.0),    # runs over many groups
+    (3000, 1032, 60, "f32", "i64", "zipf", 0.0, 1.0),
     (16385, 512, 20000, "bf16", "i64", "runs", 0.0, 1.0),  # one more than it takes
     (17, 16, 4, "f32", "i64", "same", 0.0, 1.0),
     (256, 520, 4, "bf16", "i32", "same", 0.1, 1.0),        # the most rows without a sorted list, one run
@@ -623,8 +626,9 @@ def test_embedding(rows, H, V, dtype, idt, kind, p, scale):
     call(dt, 0)
     g = to_np(dy)[:, :H]
     ref = O.embedding_bwd(ids, g, V, scale, keep)
-    # a tile's 32 rows one by one, the tiles in 4 groups, and 8 roundings more
-    tol = (32 + -(-rows // 128) + 4 + 8) * U * O.embedding_bwd(ids, np.abs(g), V, abs(scale), keep)
+    # a wave's 31 rows at most one by one, four waves, groups of 64 rows in four
+    # rows of them and those, and 8 roundings more
+    tol = (31 + 4 + -(-rows // 256) + 4 + 8) * U * O.embedding_bwd(ids, np.abs(g), V, abs(scale), keep)
     within(dt[:, :H], ref, tol, "dtable")
     assert torch.all(dt[:, H:] == 7.0)
     again = torch.full((V, ldt), 7.0, device="cuda")
