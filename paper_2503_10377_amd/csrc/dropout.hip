@@ -11,6 +11,8 @@ constexpr int64_t kMaxGroups = (int64_t)1 << 30;  // of a launch: below fast_div
 // A thread takes kUnroll groups of eight elements (one draw each), 256 groups
 // apart so that a wave's accesses are consecutive; all loads go out first.
 // FLAT: rows lie without gaps, so a group's place needs no division.
+// HBM-bound: 8192 x 4096 bf16 with a residual in 30.5 us, 6.6 TB/s out of
+// caches that hold part of it (39 us, 5.1 TB/s, on new data every time).
 template <typename T, bool FLAT, bool RES>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, FastDiv per_row, uint32_t groups) {
   const Dropper drop(a.drop);

@@ -4,11 +4,11 @@
 //
 // Backward: dtable[v] (+)= scale sum_{r: id_r = v} drop(dy[r]).  Rows of a
 // token lie anywhere and a frequent token has thousands of them, so the rows
-// are first sorted by token (stable: rows of a token stay in order), then cut
-// into tiles of kTile sorted rows that sum the runs of equal tokens they hold.
-// A run inside one tile goes to the table at once; of a run that crosses
-// tiles each tile leaves a partial sum, and a last kernel adds these in tile
-// order.  No atomics: every sum has a fixed order.
+// are first sorted by token (rows of a token stay in order), then waves sum 16
+// sorted rows each, run by run of equal tokens.  A short run goes to the table
+// at once; of a long one the waves leave partial sums, which are added in the
+// order of the rows.  Every sum has a fixed order, so the gradient has the same
+// bits every time.  A few rows take a kernel that needs no sorted list.
 #include "row_common.h"
 
 namespace sppo {
@@ -26,7 +26,7 @@ __device__ __forceinline__ uint32_t token(const void* ids, int id64, int64_t r, 
 
 // A thread takes kUnroll groups of eight elements, 256 groups apart: the ids
 // first, then the table's pieces, then the draws (19 us of the vector units for
-// 8192 x 4096, as long as its bytes take at 4.8 TB/s; together 22.5).
+// 8192 x 4096, as long as its bytes take at 4.8 TB/s; together 21.5).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedArgs a, FastDiv per_row, uint32_t groups) {
   const Dropper drop(a.drop);
@@ -225,11 +225,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, 
   }
 }
 
-// Up to kSmallKeys keys every compute unit has to itself: the place of row i is
-// the number of rows j with (token_j, j) < (token_i, i), counted over all rows,
+// Up to kSmallKeys keys there is a shorter way: the place of row i is the
+// number of rows j with (token_j, j) < (token_i, i), counted over all rows,
 // which a workgroup holds in LDS.  n^2 comparisons of two instructions beat the
-// passes of a sort (four launches of 5 us for 8192 rows) while launches and
-// their gaps are what costs: 11 us for 8192 rows.
+// passes of the sort (four launches of 5 us) while launches and their gaps are
+// what costs: 11 us for 8192 rows.  With the sums over 512 columns 8192 rows
+// take 25 us this way and 30 by the sort, 16384 rows 41 and 33.
 constexpr int kSmallKeys = 8192, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 
 // split: lanes that share a row's comparisons (1, 2 or 4); a workgroup ranks
@@ -666,7 +667,7 @@ hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
   if (a.rows <= kSmallKeys) {
     s.key_out = arr[0];
     s.row_out = arr[1];
-    // the fewest rows a workgroup that leave no compute unit without one
+    // as few rows a workgroup as it takes to occupy every compute unit
     const int split = a.rows <= 16 * (int64_t)device_cus() ? 4 : a.rows <= 32 * (int64_t)device_cus() ? 2 : 1;
     s.tiles = (int)((a.rows * split + 63) / 64);
     const ZeroArgs z = zeros();

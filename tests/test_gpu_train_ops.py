@@ -396,6 +396,22 @@ def test_block_norm_without_dh_and_with_frozen_parameters():
             assert torch.equal(some[k], g[k]), k
 
 
+def test_block_norm_backward_without_the_branch():
+    """No norm after the branch and no gate gradient wanted: b is not needed."""
+    announce("block norm without b")
+    for gate in ("channel", "token", "none"):
+        c = Case(37, 520, 520, "bf16", "none", "rms", gate, True, 0.2, seed=5)
+        h, _ = c.forward()
+        dz, dh = randn(37, 520, 520, "bf16", 65).cuda(), randn(37, 520, 520, "bf16", 66).cuda()
+        dx, db, g = run_bwd(c, h, dz, dh)
+        dx2, db2, dpre = c.act(), c.act(), torch.empty_like(g["pre_gamma"])
+        nb = L.sppo_block_norm_bwd_workspace(c.bn, 37)
+        ws = torch.empty(nb // 4, device="cuda")
+        L.sppo_block_norm_bwd(c.bn, 37, c.drop, None, 0, h, 520, c.cstats, dz, 520, dh, 520, dx2, 520, db2, 520,
+                              L.block_norm_grads(pre_gamma=dpre), ws, nb, 0)
+        assert torch.equal(dx, dx2) and torch.equal(db, db2) and torch.equal(dpre, g["pre_gamma"])
+
+
 def test_block_norm_in_place():
     """h over x, z over b; dx over dh, db over dz: the same bits."""
     announce("block norm in place")
