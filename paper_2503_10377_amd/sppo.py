@@ -232,16 +232,29 @@ def _ptr(x) -> int | None:
     return int(x)
 
 
+_current = None  # () -> the current stream's handle, once torch has a device
+
+
+def _current_stream() -> int:
+    global _current
+    if _current is not None:
+        return _current()
+    import torch
+
+    handle = torch.cuda.current_stream().cuda_stream
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
+        _current = lambda: torch.cuda.current_stream().cuda_stream
+    else:
+        _current = lambda: raw(device())  # the same, without a Stream object (2.7 us of a call's 7.5)
+    return handle
+
+
 def _stream(s) -> int | None:
     if type(s) is int:
         return s
     if s is None:
-        import torch
-
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None and torch.cuda.is_initialized():  # the same stream, without a Stream object (2.7 us)
-            return raw(torch._C._cuda_getDevice())
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if hasattr(s, "cuda_stream"):
         return s.cuda_stream
     return int(s)
