@@ -697,11 +697,12 @@ def test_embedding_past_a_launch():
         within(y[r:r + 1], ref, (HALF["bf16"] + 4 * U) * np.abs(ref), r)
 
 
-def test_embedding_gradient_in_graphs():
+@pytest.mark.parametrize("rows", [100, 700, 9000])  # each way to order the rows
+def test_embedding_gradient_in_graphs(rows):
     """Two captured gradients with a workspace each, replayed at once on two
     streams with new tokens in between: every replay has the eager bits."""
-    announce("embedding gradient in two graphs")
-    rows, H, V = 700, 512, 90
+    announce(f"embedding gradient in two graphs, rows={rows}")
+    H, V = 512, 90
     sides = []
     for i in range(2):
         ids = torch.from_numpy(make_ids(rows, V, "zipf", i)).cuda()
