@@ -37,9 +37,10 @@ Two options put the training operators around the blocks:
       scales and dropout.  The masks are drawn again in the backward; b_i and
       the norms' statistics are further planes where the backward needs them.
   vocab=V              the walk starts from tokens: x_i = drop(scale
-      w_emb[tokens_i]) is looked up in the forward and again in the backward
-      (it is no plane, so it does not travel), and dx_i becomes the table's
-      gradient, added up over the reverse walk.
+      w_emb[tokens_i]), with the block ends' dropout if there are any, is
+      looked up in the forward and again in the backward (it is no plane, so it
+      does not travel), and dx_i becomes the table's gradient, added up over
+      the reverse walk.
 
 Only C-ABI calls and torch allocations happen here; every arithmetic step
 runs in the library's kernels.
@@ -77,8 +78,9 @@ class BlockEnds:
         return self.norm != "none" or self.gate
 
     def params(self, n):
-        """Names of block n's parameters ([H] fp32 each), as block_norm takes
-        them; the layer's are these with a p, their gradients with a dp."""
+        """block_norm's arguments for block n (1: attention, 2: MLP) and the
+        names they have among a step's parameters ([H] fp32 each); their
+        gradients are out["d" + name]."""
         names = {}
         if self.norm != "none":
             names["post_gamma"] = f"g_end{n}"
@@ -283,8 +285,9 @@ class ChunkedLayer:
         drop_p = ends.dropout if ends is not None else 0.0
         if x is None:
             tokens = inp["tokens"]
-            if tokens.dtype not in (torch.int32, torch.int64) or tokens.shape != (self.S,) or not tokens.is_contiguous():
-                raise ValueError(f"tokens must be [{self.S}] contiguous int32 or int64")
+            if tokens.dtype not in (torch.int32, torch.int64) or tokens.shape != (self.S,) \
+                    or not tokens.is_contiguous() or not tokens.is_cuda:
+                raise ValueError(f"tokens must be [{self.S}] contiguous int32 or int64 on the device")
             id_type = "i32" if tokens.dtype == torch.int32 else "i64"
 
         def mark(label):

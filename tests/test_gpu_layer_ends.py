@@ -134,7 +134,8 @@ def test_layer_with_ends_refuses():
     out = lay.alloc_outputs()
     inp, p = setup(256, 2, 2, 128, None, 10, 1)
     t = inp["tokens"].cuda()
-    for bad in (t[:255], t.to(torch.int16), t.repeat(2)[::2]):  # too short, another type, with gaps
+    # too short, another type, with gaps, in host memory
+    for bad in (t[:255], t.to(torch.int16), t.repeat(2)[::2], inp["tokens"]):
         with pytest.raises(ValueError):
             lay.step({"tokens": bad, "dy": inp["dy"].cuda()}, {k: v.cuda() for k, v in p.items()}, out)
     lay.close()
