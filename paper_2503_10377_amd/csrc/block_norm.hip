@@ -95,9 +95,9 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
 // activations' bytes, out of L2), with a channel's gate folded into the norm
 // after the branch: gate n = bh (gate gamma) + gate beta.  The next row's x and
 // b are on their way while a row is worked on.  HBM-bound: 8192 x 4096 bf16
-// with both LayerNorms, gate and dropout in 53 us, 5.1 TB/s, the vector units
-// busy for two thirds of it.
-template <typename T, int NT, int TEAM, int PER>
+// with both LayerNorms, gate and dropout in 55 us, 4.9 TB/s, the vector units
+// busy for 58% of it.
+template <typename T, bool PAST, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   static_assert(TEAM == NT || TEAM <= 64, "");
   __shared__ Moments red[2][TEAM > 64 ? TEAM / 64 : 1];
@@ -119,8 +119,8 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
       if (c < H) {
-        bn[p].load(static_cast<const T*>(a.b) + r * a.ldb + c);
-        xn[p].load(static_cast<const T*>(a.x) + r * a.ldx + c);
+        bn[p].template read<PAST>(static_cast<const T*>(a.b) + r * a.ldb + c);
+        xn[p].template read<PAST>(static_cast<const T*>(a.x) + r * a.ldx + c);
       }
     }
   };
@@ -251,12 +251,13 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
 // A team takes rows in turn with the parameters in registers (gate and gamma
 // as one) and the next row's h, dz, dh, b and statistics on their way, and adds
 // its part of the column sums row by row.  8192 x 4096 bf16 with both
-// LayerNorms, gate and dropout: 87 us and 7 for the sums' reduction, 4.6 TB/s
-// with the column sums' traffic.  MODE: what the branch needs beyond its mask
-// (two waves a SIMD hold all of it in registers; asking for four, with some of
-// it in scratch memory, doubled the time of the plain mode).
+// LayerNorms, gate and dropout: 79 us and 6 for the sums' reduction, 5.1 TB/s
+// with the column sums' traffic (through the caches 87 and 7, dx alone 3 of
+// them).  MODE: what the branch needs beyond its mask (two waves a SIMD hold
+// all of it in registers; asking for four, with some of it in scratch memory,
+// doubled the time of the plain mode).
 enum { kPlain = 0, kGated = 1, kNormed = 2 };
-template <typename T, int MODE, int NT, int TEAM, int PER>
+template <typename T, bool PAST, int MODE, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
   constexpr bool POST = MODE == kNormed;
   constexpr int TEAMS = NT / TEAM;
@@ -280,11 +281,11 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
       const int c = 8 * (tid + TEAM * p);
       if (c < H) {
         if (pre) {
-          hn[p].load(static_cast<const T*>(a.h) + row * a.ldh + c);
-          zn[p].load(static_cast<const T*>(a.dz) + row * a.lddz + c);
+          hn[p].template read<PAST>(static_cast<const T*>(a.h) + row * a.ldh + c);
+          zn[p].template read<PAST>(static_cast<const T*>(a.dz) + row * a.lddz + c);
         }
-        if (a.dh) dn[p].load(static_cast<const T*>(a.dh) + row * a.lddh + c);
-        if (MODE != kPlain && a.b) bn[p].load(static_cast<const T*>(a.b) + row * a.ldb + c);
+        if (a.dh) dn[p].template read<PAST>(static_cast<const T*>(a.dh) + row * a.lddh + c);
+        if (MODE != kPlain && a.b) bn[p].template read<PAST>(static_cast<const T*>(a.b) + row * a.ldb + c);
       }
     }
     if (pre) st[0] = a.pre_rstd[row];
@@ -384,7 +385,12 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           o[e] = a.alpha * D[p][e];
           D[p][e] *= scale;
         }
-        if (real) Eight<T>::store(static_cast<T*>(a.dx) + row * a.lddx + c, o);
+        // dx is next read behind the branch's products, db by the first of them
+        if (real) {
+          T* dx = static_cast<T*>(a.dx) + row * a.lddx + c;
+          if constexpr (PAST) Eight<T>::stream_out(dx, o);
+          else Eight<T>::store(dx, o);
+        }
         drop.mask(g0 + c / 8, D[p]);
         if (a.gate_kind == kToken && POST && a.post_beta) {
           float bt[8];
@@ -524,24 +530,24 @@ __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArg
   }
 }
 
-template <typename T, int NT, int TEAM, int PER>
+template <typename T, bool PAST, int NT, int TEAM, int PER>
 hipError_t fwd(const BlockNormArgs& a, hipStream_t stream) {
   const int64_t teams = NT / TEAM, all = (a.rows + teams - 1) / teams;
   const int64_t most = (int64_t)device_cus() * (NT < 1024 ? 1024 / NT : 1);  // 16 waves a compute unit
-  hipLaunchKernelGGL((bn_fwd_kernel<T, NT, TEAM, PER>), dim3((unsigned)(all < most ? all : most)), dim3(NT), 0, stream,
+  hipLaunchKernelGGL((bn_fwd_kernel<T, PAST, NT, TEAM, PER>), dim3((unsigned)(all < most ? all : most)), dim3(NT), 0, stream,
                      a);
   return hipGetLastError();
 }
 
-template <typename T, int NT, int TEAM, int PER>
+template <typename T, bool PAST, int NT, int TEAM, int PER>
 hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)a.nblocks), block(NT);
   if (a.post != kNone)
-    hipLaunchKernelGGL((bn_bwd_kernel<T, kNormed, NT, TEAM, PER>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((bn_bwd_kernel<T, PAST, kNormed, NT, TEAM, PER>), grid, block, 0, stream, a);
   else if (a.gate_kind != kNone)
-    hipLaunchKernelGGL((bn_bwd_kernel<T, kGated, NT, TEAM, PER>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((bn_bwd_kernel<T, PAST, kGated, NT, TEAM, PER>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((bn_bwd_kernel<T, kPlain, NT, TEAM, PER>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((bn_bwd_kernel<T, PAST, kPlain, NT, TEAM, PER>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -549,33 +555,33 @@ hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
 // wave does once per row (its share of the sums, the statistics) is half as
 // much per element (forward of 8192 x 4096 with one: 88 us).  fp32 rows have
 // twice the bytes and twice the registers per element.
-template <typename T>
+template <typename T, bool PAST>
 hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
-  if (a.H <= 128) return fwd<T, 256, 16, 1>(a, stream);
-  if (a.H <= 256) return fwd<T, 256, 32, 1>(a, stream);
-  if (a.H <= 512) return fwd<T, 256, 64, 1>(a, stream);
-  if (a.H <= 1024) return fwd<T, 256, 64, 2>(a, stream);
-  if (a.H <= 2048) return fwd<T, 256 / P, 256 / P, P>(a, stream);
-  if (a.H <= 4096) return fwd<T, 512 / P, 512 / P, P>(a, stream);
-  return fwd<T, 512, 512, 2>(a, stream);  // 1024 threads would have 128 registers each, too few
+  if (a.H <= 128) return fwd<T, PAST, 256, 16, 1>(a, stream);
+  if (a.H <= 256) return fwd<T, PAST, 256, 32, 1>(a, stream);
+  if (a.H <= 512) return fwd<T, PAST, 256, 64, 1>(a, stream);
+  if (a.H <= 1024) return fwd<T, PAST, 256, 64, 2>(a, stream);
+  if (a.H <= 2048) return fwd<T, PAST, 256 / P, 256 / P, P>(a, stream);
+  if (a.H <= 4096) return fwd<T, PAST, 512 / P, 512 / P, P>(a, stream);
+  return fwd<T, PAST, 512, 512, 2>(a, stream);  // 1024 threads would have 128 registers each, too few
 }
 
 // The backward's workgroups hold as many teams as fit 512 threads, one
 // workgroup a compute unit, so that few of them leave column sums (8192 x 4096
-// with 512 workgroups of one team: 100 us with the sums' reduction, with 256 of
-// two teams 94); up to 512 columns a wave needs fewer registers and twice as
+// through the caches, with 512 workgroups of one team: 100 us with the sums'
+// reduction, with 256 of two teams 94); up to 512 columns a wave needs fewer registers and twice as
 // many fit.
-template <typename T>
+template <typename T, bool PAST>
 hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
-  if (a.H <= 128) return bwd<T, 256, 16, 1>(a, stream);
-  if (a.H <= 256) return bwd<T, 256, 32, 1>(a, stream);
-  if (a.H <= 512) return bwd<T, 256, 64, 1>(a, stream);
-  if (a.H <= 1024) return bwd<T, 512, 64, 2>(a, stream);
-  if (a.H <= 2048) return bwd<T, 512, 256 / P, P>(a, stream);
-  if (a.H <= 4096) return bwd<T, 512, 512 / P, P>(a, stream);
-  return bwd<T, 512, 512, 2>(a, stream);
+  if (a.H <= 128) return bwd<T, PAST, 256, 16, 1>(a, stream);
+  if (a.H <= 256) return bwd<T, PAST, 256, 32, 1>(a, stream);
+  if (a.H <= 512) return bwd<T, PAST, 256, 64, 1>(a, stream);
+  if (a.H <= 1024) return bwd<T, PAST, 512, 64, 2>(a, stream);
+  if (a.H <= 2048) return bwd<T, PAST, 512, 256 / P, P>(a, stream);
+  if (a.H <= 4096) return bwd<T, PAST, 512, 512 / P, P>(a, stream);
+  return bwd<T, PAST, 512, 512, 2>(a, stream);
 }
 
 // Teams of a workgroup of the backward (as dispatched above), and the most
@@ -603,7 +609,9 @@ size_t block_norm_bwd_workspace(const BlockNormArgs& a) {
 
 hipError_t launch_block_norm_fwd(const BlockNormArgs& a, hipStream_t stream) {
   if (a.rows <= 0 || a.H <= 0 || a.H % 8 || a.H > kBnMaxH) return hipErrorInvalidValue;
-  return a.f32 ? forward<float>(a, stream) : forward<uint16_t>(a, stream);
+  if (stream_activation(a.rows, a.H, a.f32))
+    return a.f32 ? forward<float, true>(a, stream) : forward<uint16_t, true>(a, stream);
+  return a.f32 ? forward<float, false>(a, stream) : forward<uint16_t, false>(a, stream);
 }
 
 hipError_t launch_block_norm_bwd(const BlockNormArgs& a, hipStream_t stream) {
@@ -612,7 +620,9 @@ hipError_t launch_block_norm_bwd(const BlockNormArgs& a, hipStream_t stream) {
   const int64_t teams = teams_of(a.H, a.f32), most = bwd_blocks(a.rows, a.H, a.f32);
   b.rows_per_block = (int)((a.rows + most * teams - 1) / (most * teams) * teams);
   b.nblocks = (int)((a.rows + b.rows_per_block - 1) / b.rows_per_block);
-  const hipError_t e = a.f32 ? backward<float>(b, stream) : backward<uint16_t>(b, stream);
+  const bool past = stream_activation(a.rows, a.H, a.f32);
+  const hipError_t e = past ? (a.f32 ? backward<float, true>(b, stream) : backward<uint16_t, true>(b, stream))
+                            : (a.f32 ? backward<float, false>(b, stream) : backward<uint16_t, false>(b, stream));
   const int sums = bn_slots(a).n;
   if (e != hipSuccess || sums == 0) return e;
   hipLaunchKernelGGL(bn_reduce_kernel, dim3((unsigned)((a.H + kRedCols - 1) / kRedCols)),

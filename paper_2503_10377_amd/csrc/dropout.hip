@@ -11,9 +11,9 @@ constexpr int64_t kMaxGroups = (int64_t)1 << 30;  // of a launch: below fast_div
 // A thread takes kUnroll groups of eight elements (one draw each), 256 groups
 // apart so that a wave's accesses are consecutive; all loads go out first.
 // FLAT: rows lie without gaps, so a group's place needs no division.
-// HBM-bound: 8192 x 4096 bf16 with a residual in 30.5 us, 6.6 TB/s out of
-// caches that hold part of it (39 us, 5.1 TB/s, on new data every time).
-template <typename T, bool FLAT, bool RES>
+// HBM-bound: 8192 x 4096 bf16 with a residual, on new data every time, in 34
+// us, 6.0 TB/s (read through the caches: 39).
+template <typename T, bool FLAT, bool RES, bool PAST>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, FastDiv per_row, uint32_t groups) {
   const Dropper drop(a.drop);
   const uint32_t cpr = (uint32_t)a.cols / 8;
@@ -33,8 +33,8 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, FastDi
       row[u] = r;
       col[u] = (int64_t)(g[u] - r * cpr) * 8;
     }
-    x[u].load(static_cast<const T*>(a.x) + row[u] * a.ldx + col[u]);
-    if constexpr (RES) res[u].load(static_cast<const T*>(a.res) + row[u] * a.ldres + col[u]);
+    x[u].template read<PAST>(static_cast<const T*>(a.x) + row[u] * a.ldx + col[u]);
+    if constexpr (RES) res[u].template read<PAST>(static_cast<const T*>(a.res) + row[u] * a.ldres + col[u]);
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, FastDi
   }
 }
 
-template <typename T>
+template <typename T, bool PAST>
 hipError_t launch(const DropoutArgs& a, hipStream_t stream) {
   const int64_t cpr = a.cols / 8, rows_per = kMaxGroups / cpr;
   const bool flat = a.ldx == a.cols && a.ldy == a.cols && (!a.res || a.ldres == a.cols);
@@ -67,13 +67,13 @@ hipError_t launch(const DropoutArgs& a, hipStream_t stream) {
     const uint32_t groups = (uint32_t)(b.rows * cpr);
     const dim3 grid((groups + kThreads * kUnroll - 1) / (kThreads * kUnroll)), block(kThreads);
     if (flat && a.res)
-      hipLaunchKernelGGL((dropout_kernel<T, true, true>), grid, block, 0, stream, b, div, groups);
+      hipLaunchKernelGGL((dropout_kernel<T, true, true, PAST>), grid, block, 0, stream, b, div, groups);
     else if (flat)
-      hipLaunchKernelGGL((dropout_kernel<T, true, false>), grid, block, 0, stream, b, div, groups);
+      hipLaunchKernelGGL((dropout_kernel<T, true, false, PAST>), grid, block, 0, stream, b, div, groups);
     else if (a.res)
-      hipLaunchKernelGGL((dropout_kernel<T, false, true>), grid, block, 0, stream, b, div, groups);
+      hipLaunchKernelGGL((dropout_kernel<T, false, true, PAST>), grid, block, 0, stream, b, div, groups);
     else
-      hipLaunchKernelGGL((dropout_kernel<T, false, false>), grid, block, 0, stream, b, div, groups);
+      hipLaunchKernelGGL((dropout_kernel<T, false, false, PAST>), grid, block, 0, stream, b, div, groups);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -84,7 +84,9 @@ hipError_t launch(const DropoutArgs& a, hipStream_t stream) {
 
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream) {
   if (a.rows <= 0 || a.cols <= 0 || a.cols % 8) return hipErrorInvalidValue;
-  return a.f32 ? launch<float>(a, stream) : launch<uint16_t>(a, stream);
+  if (stream_activation(a.rows, a.cols, a.f32))
+    return a.f32 ? launch<float, true>(a, stream) : launch<uint16_t, true>(a, stream);
+  return a.f32 ? launch<float, false>(a, stream) : launch<uint16_t, false>(a, stream);
 }
 
 }  // namespace sppo

@@ -278,10 +278,11 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs s, int spli
 // A workgroup takes kGroup sorted places and kSlab columns, each of its waves
 // kTile of the places; the workgroups of a group's columns come one after
 // another, so that whole rows are on their way at a time (8192 rows of 4096
-// columns, 3300 tokens: 34 us, 5.2 TB/s; with the places first 41).  After a
-// fill of the table it takes 44 us: the fill's last 256 MB are still in the
-// memory-side cache and leave it while the sums run (stores that go past that
-// cache make the fill 38 us longer).
+// columns, 3300 tokens, dy through the caches: 34 us, with the places first
+// 41).  A fill of the table leaves its last 256 MB in the memory-side cache,
+// from where they go to memory while the sums run: 30 us with dy past the
+// caches, 42 through them (stores of the fill that go past that cache make the
+// fill 38 us longer).
 //
 // A run of at most kTile rows belongs to the wave where it begins, which
 // follows it past its places, so it is summed at once.  Of a longer run the
@@ -304,7 +305,7 @@ struct SumArgs {
 // are read ahead, and where the sums add to the table so are its old rows, at
 // the places where runs begin (read where a run ends, each costs a trip to
 // memory).
-template <typename T, bool ADD>
+template <typename T, bool PAST, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) {
   // A wave's partial sums: of a long run that enters it and of one that leaves it.
   __shared__ __attribute__((aligned(16))) float part[4][2][kSlab];
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) 
   auto begins = [&](int u) { return u == first || key_at(u - 1) != key_at(u); };
   auto load = [&](int u, int slot) {
     if (u >= stop || !in) return;
-    x[slot].load(static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy + c);
+    x[slot].template read<PAST>(static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy + c);
     if constexpr (ADD)
       if (begins(u)) old[slot].load(a.dtable + (int64_t)key_at(u) * a.lddt + c);
   };
@@ -624,7 +625,7 @@ hipError_t forward(const EmbedArgs& a, hipStream_t stream) {
   return hipSuccess;
 }
 
-template <typename T>
+template <typename T, bool PAST>
 hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
   if (a.rows <= kDirectRows) {
     const int64_t slabs = (a.H + kSlab - 1) / kSlab, most = 4 * (int64_t)device_cus();
@@ -698,9 +699,9 @@ hipError_t backward(const EmbedArgs& a, hipStream_t stream) {
   SumArgs u{a.rows, s.key, s.row, reinterpret_cast<float*>(ws + p.part)};
   const dim3 grid((unsigned)(p.groups * ((a.H + kSlab - 1) / kSlab)));
   if (a.accumulate)
-    hipLaunchKernelGGL((embed_sum_kernel<T, true>), grid, dim3(256), 0, stream, a, u);
+    hipLaunchKernelGGL((embed_sum_kernel<T, PAST, true>), grid, dim3(256), 0, stream, a, u);
   else
-    hipLaunchKernelGGL((embed_sum_kernel<T, false>), grid, dim3(256), 0, stream, a, u);
+    hipLaunchKernelGGL((embed_sum_kernel<T, PAST, false>), grid, dim3(256), 0, stream, a, u);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(embed_join_kernel,
                      dim3((unsigned)p.groups, (unsigned)((a.H + kJoinCols - 1) / kJoinCols)), dim3(kJoinThreads), 0,
@@ -719,7 +720,9 @@ hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t stream) {
 
 hipError_t launch_embedding_bwd(const EmbedArgs& a, hipStream_t stream) {
   if (a.rows <= 0 || a.H <= 0 || a.H % 8) return hipErrorInvalidValue;
-  return a.f32 ? backward<float>(a, stream) : backward<uint16_t>(a, stream);
+  if (stream_activation(a.rows, a.H, a.f32))
+    return a.f32 ? backward<float, true>(a, stream) : backward<uint16_t, true>(a, stream);
+  return a.f32 ? backward<float, false>(a, stream) : backward<uint16_t, false>(a, stream);
 }
 
 }  // namespace sppo

@@ -55,7 +55,10 @@ __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
 }
 
 // Eight consecutive elements as they lie in memory, for activations of either
-// type: bf16 in one 16-byte piece, fp32 in two.
+// type: bf16 in one 16-byte piece, fp32 in two.  Of large activations (see
+// kStreamBytes) stream() reads what nobody reads again soon, so that it takes
+// no place in the caches from what is written for the next kernel, and
+// stream_out() writes what only a later kernel reads.
 template <typename T>
 struct Eight;
 template <>
@@ -63,9 +66,20 @@ struct Eight<uint16_t> {
   u32x4 v;
   __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void load(const uint16_t* p) { v = ld_global16(p); }
+  __device__ __forceinline__ void stream(const uint16_t* p) {
+    v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  }
+  template <bool PAST>
+  __device__ __forceinline__ void read(const uint16_t* p) {
+    if constexpr (PAST) stream(p);
+    else load(p);
+  }
   __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(v, f); }
   static __device__ __forceinline__ void store(uint16_t* p, const float (&f)[8]) {
     *reinterpret_cast<u32x4*>(p) = pack8(f);
+  }
+  static __device__ __forceinline__ void stream_out(uint16_t* p, const float (&f)[8]) {
+    __builtin_nontemporal_store(pack8(f), reinterpret_cast<u32x4*>(p));
   }
 };
 template <>
@@ -76,6 +90,15 @@ struct Eight<float> {
     v[0] = *reinterpret_cast<const f32x4*>(p);
     v[1] = *reinterpret_cast<const f32x4*>(p + 4);
   }
+  __device__ __forceinline__ void stream(const float* p) {
+    v[0] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+    v[1] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
+  }
+  template <bool PAST>
+  __device__ __forceinline__ void read(const float* p) {
+    if constexpr (PAST) stream(p);
+    else load(p);
+  }
   __device__ __forceinline__ void get(float (&f)[8]) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = v[e >> 2][e & 3];
@@ -83,6 +106,10 @@ struct Eight<float> {
   static __device__ __forceinline__ void store(float* p, const float (&f)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+  }
+  static __device__ __forceinline__ void stream_out(float* p, const float (&f)[8]) {
+    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(p));
+    __builtin_nontemporal_store(f32x4{f[4], f[5], f[6], f[7]}, reinterpret_cast<f32x4*>(p + 4));
   }
 };
 __device__ __forceinline__ void load8f(const float* p, float (&f)[8]) {

@@ -189,6 +189,20 @@ struct PackArgs {
 };
 hipError_t launch_pack_dqkv(const PackArgs& a, hipStream_t stream);
 
+// Activations of at least this size are read past the caches where they are
+// read once.  A call has three to six of them, so below it they fit the
+// memory-side cache's 256 MB beside what the next kernel reads, and come from
+// there: dropout between two LayerNorms, past and through the caches, at 16 MB
+// 30.8 and 29.7 us, at 32 MB 51 and 54; the block norm's backward between two
+// at 64 MB 144 and 156; the table gradient of 65521 x 1024 (128 MB) 94 and 114.
+// (Written past the caches for a next kernel that reads them, activations cost
+// it more than is gained: embedding 28 -> 19 us, with the LayerNorm behind it
+// 53 -> 59.)
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+inline bool stream_activation(int64_t rows, int64_t width, bool f32) {
+  return rows * width * (f32 ? 4 : 2) >= kStreamBytes;
+}
+
 // Dropout of a call's rows: threshold in [0, 65535] (0: none), the scale of
 // the kept elements, the global index of its first row.
 struct DropArgs {

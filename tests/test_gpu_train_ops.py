@@ -61,6 +61,8 @@ def drop_tol(x, keep, res, dtype):
     (2051, 40, 40, "bf16", False, 0.01, 0),
     (5, 64, 64, "bf16", True, 0.0, 0),                   # nothing dropped
     (5, 64, 64, "f32", False, 0.99998, 0),               # all but the highest draw dropped (T = 65535)
+    (4100, 4096, 4104, "bf16", True, 0.1, 0),            # read past the caches, strided and dense
+    (1030, 8192, 8192, "f32", False, 0.1, 0),
 ])
 def test_dropout(rows, W, ld, dtype, res, p, row0):
     announce(f"dropout rows={rows} W={W} ld={ld} {dtype} res={res} p={p} row0={row0}")
@@ -357,6 +359,7 @@ NORM_CASES = [
     (33, 256, 256, "f32", "none", "layer", "channel", True, 0.1, 1.0, 1.0),
     (1100, 768, 768, "bf16", "layer", "layer", "channel", True, 0.1, 1.0, 1.0),
     (515, 3000, 3008, "bf16", "layer", "layer", "channel", True, 0.1, 1.0, 1.0),
+    (4100, 4096, 4104, "bf16", "layer", "layer", "channel", True, 0.1, 1.0, 1.0),  # read past the caches
 ]
 
 
@@ -379,6 +382,54 @@ def test_block_norm(rows, H, ld, dtype, post, pre, gate, beta, p, alpha, scale):
         assert torch.equal(g[k], g3[k]), k
     if gate == "token":
         assert torch.equal(g["gate"], g2["gate"])
+
+
+@pytest.mark.parametrize("dtype,H", [("bf16", H) for H in (128, 256, 512, 1024, 2048, 8192)] +
+                         [("f32", H) for H in (128, 256, 512, 1024, 2048, 4096, 8192)])
+@pytest.mark.parametrize("post,gate", [("layer", "channel"), ("none", "token"), ("none", "none")])
+def test_block_norm_of_large_activations(dtype, H, post, gate):
+    """Activations of 32 MiB and more are read past the caches: the same bits
+    per row as the same rows in three smaller calls have."""
+    rows = 2 ** 25 // (H * DT[dtype].itemsize) + 3
+    announce(f"large block norm rows={rows} H={H} {dtype} post={post} gate={gate}")
+    g = torch.Generator(device="cuda").manual_seed(H)
+    x, b, dz, dh = (torch.randn(rows, H, generator=g, device="cuda").to(DT[dtype]) for _ in range(4))
+    par = {k: 0.5 + torch.rand(H, generator=g, device="cuda") for k in
+           ["pre_gamma", "pre_beta"] + (["post_gamma", "post_beta"] if post != "none" else [])}
+    token = 0.5 + torch.rand(rows, generator=g, device="cuda")
+    if gate == "channel":
+        par["gate"] = 0.5 + torch.rand(H, generator=g, device="cuda")
+
+    def run(c0, c1):
+        n = c1 - c0
+        mine = dict(par, gate=token[c0:c1]) if gate == "token" else par
+        bn = L.block_norm(H, dtype, post, "layer", gate, 1e-5, 1.0, 0.5, **mine)
+        names = ["pre_mean", "pre_rstd"] + (["post_mean", "post_rstd"] if post != "none" else [])
+        stats = {k: torch.empty(n, device="cuda") for k in names}
+        st, drop = L.block_norm_stats(**stats), L.drop_spec(0.1, 31, 2, c0)
+        h, z, dx, db = (torch.empty(n, H, device="cuda", dtype=DT[dtype]) for _ in range(4))
+        grads = {k: torch.empty_like(v) for k, v in mine.items()}
+        L.sppo_block_norm_fwd(bn, n, drop, x[c0:c1], H, b[c0:c1], H, h, H, z, H, st)
+        nb = L.sppo_block_norm_bwd_workspace(bn, n)
+        ws = torch.empty(max(nb // 4, 4), device="cuda")
+        L.sppo_block_norm_bwd(bn, n, drop, b[c0:c1], H, h, H, st, dz[c0:c1], H, dh[c0:c1], H, dx, H, db, H,
+                              L.block_norm_grads(**grads), ws, nb, 0)
+        torch.cuda.synchronize()
+        return [h, z, dx, db] + list(stats.values()) + ([grads["gate"]] if gate == "token" else []), grads, stats, h
+
+    whole, grads, stats, h = run(0, rows)
+    parts = [run(c0, c1)[0] for c0, c1 in ((0, 7), (7, rows // 2), (rows // 2, rows))]
+    for i, t in enumerate(whole):
+        assert torch.equal(t, torch.cat([q[i] for q in parts])), i
+    # the column sums, at the depth that bwd_check derives: of dz, and of dz
+    # times the normalised value, which rounds twice more and the product once
+    depth = -(-rows // 256) + 8 + 8 + 16 + 5 + 4
+    d = dz.double()
+    within(grads["pre_beta"], to_np(d.sum(0)), to_np((depth + 2) * U * d.abs().sum(0)), "pre_beta")
+    m, r = stats["pre_mean"].double()[:, None], stats["pre_rstd"].double()[:, None]
+    mag = d.abs() * (h.double().abs() + m.abs()) * r
+    within(grads["pre_gamma"], to_np((d * (h.double() - m) * r).sum(0)), to_np((depth + 5) * U * mag.sum(0)),
+           "pre_gamma")
 
 
 def test_block_norm_without_dh_and_with_frozen_parameters():
@@ -612,6 +663,8 @@ EMBED_CASES = [
     (1024, 520, 70, "bf16", "i64", "runs", 0.1, 1.0),
     (1000, 16, 300, "f32", "i32", "outside", 0.0, 1.0),
     (1025, 16, 4, "f32", "i64", "same", 0.0, 1.0),
+    (4100, 4096, 900, "bf16", "i64", "zipf", 0.1, 1.0),    # read past the caches
+    (33000, 256, 5000, "f32", "i64", "runs", 0.0, 1.0),
 ]
 
 
