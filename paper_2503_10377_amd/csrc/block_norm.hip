@@ -13,6 +13,17 @@ namespace {
 constexpr int kNone = 0, kLayer = 1, kRms = 2;
 constexpr int kChannel = 1, kToken = 2;
 
+// Has every cache line of the arguments fetched at once.  Their loads stand
+// where the values are needed, and each first touch of a line is a trip to
+// memory that the first rows would wait for, one after another: 0.4 us of a
+// call (backward of 5001 x 1024 bf16 17.1 -> 16.6; nothing for the smaller
+// arguments of dropout and the embedding).
+__device__ __forceinline__ void fetch_args(const BlockNormArgs& a) {
+  static_assert(sizeof(a) > 5 * 64 && sizeof(a) <= 6 * 64);
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&a);
+  asm volatile("" ::"s"(w[0]), "s"(w[16]), "s"(w[32]), "s"(w[48]), "s"(w[64]), "s"(w[80]));
+}
+
 // A team's exchange of two moments: each wave's sum and squares, its number of
 // columns and the inverse of that.
 struct alignas(16) Moments {
@@ -99,6 +110,7 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
 // busy for 58% of it.
 template <typename T, bool PAST, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
+  fetch_args(a);
   static_assert(TEAM == NT || TEAM <= 64, "");
   __shared__ Moments red[2][TEAM > 64 ? TEAM / 64 : 1];
   constexpr int TEAMS = NT / TEAM;
@@ -259,6 +271,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
 enum { kPlain = 0, kGated = 1, kNormed = 2 };
 template <typename T, bool PAST, int MODE, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
+  fetch_args(a);
   constexpr bool POST = MODE == kNormed;
   constexpr int TEAMS = NT / TEAM;
   // the team's exchanges alternate between two images, as in the forward
@@ -481,6 +494,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
 // all at once), then the groups are added pairwise.
 constexpr int kRedCols = 32, kRedGroups = 32, kRedThreads = kRedCols / 4 * kRedGroups;
 __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArgs a) {
+  fetch_args(a);
   __shared__ __attribute__((aligned(16))) float red[4][kRedGroups][kRedCols + 4];
   __shared__ float total[4][kRedCols];
   const int i = threadIdx.x / kRedThreads, th = threadIdx.x % kRedThreads;
