@@ -26,38 +26,53 @@ __device__ __forceinline__ uint32_t token(const void* ids, int id64, int64_t r, 
 
 // A thread takes kUnroll groups of eight elements, 256 groups apart: the ids
 // first, then the table's pieces, then the draws (19 us of the vector units for
-// 8192 x 4096, as long as its bytes take at 4.8 TB/s; together 21.5).
+// 8192 x 4096, as long as its bytes take at 4.8 TB/s; together 19.5, with
+// branches around the loads 21.7).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedArgs a, FastDiv per_row, uint32_t groups) {
   const Dropper drop(a.drop);
   const uint32_t cpr = (uint32_t)a.H / 8;
   const uint64_t g0 = (uint64_t)a.drop.row0 * cpr;
   const float scale = a.scale * drop.scale;  // finite: a row of zeros stays one
+  // No branches around the loads (a thread past the end takes the last group
+  // again, an id outside the table reads its row 0), so that none waits for
+  // another; the draws come before the pieces are waited for.
   Eight<T> x[kUnroll];
   uint32_t g[kUnroll], row[kUnroll], col[kUnroll], id[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    g[u] = blockIdx.x * (kThreads * kUnroll) + kThreads * u + threadIdx.x;
-    if (g[u] >= groups) continue;
+    const uint32_t i = blockIdx.x * (kThreads * kUnroll) + kThreads * u + threadIdx.x;
+    g[u] = i < groups ? i : groups - 1;
     row[u] = fast_div(g[u], per_row);
     col[u] = (g[u] - row[u] * cpr) * 8;
-    id[u] = token(a.ids, a.id64, row[u], a.V);
+  }
+  if (a.id64) {
+    int64_t v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = static_cast<const int64_t*>(a.ids)[row[u]];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) id[u] = (uint32_t)(v[u] >= 0 && v[u] < a.V ? v[u] : a.V);
+  } else {
+    int32_t v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) v[u] = static_cast<const int32_t*>(a.ids)[row[u]];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) id[u] = (uint32_t)(v[u] >= 0 && v[u] < a.V ? v[u] : a.V);
   }
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    if (g[u] >= groups) continue;
-    x[u].zero();
-    if (id[u] < a.V) x[u].load(static_cast<const T*>(a.table) + (int64_t)id[u] * a.ldt + col[u]);
-  }
+  for (int u = 0; u < kUnroll; ++u)
+    x[u].load(static_cast<const T*>(a.table) + (int64_t)(id[u] < a.V ? id[u] : 0) * a.ldt + col[u]);
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    if (g[u] >= groups) continue;
+    u32x4 w;
+    if (drop.t16) w = drop.draw(g0 + g[u]);
     float f[8];
     x[u].get(f);
-    drop.mask(g0 + g[u], f);
+    if (drop.t16) drop.keep(w, f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] *= scale;
-    Eight<T>::store(static_cast<T*>(a.y) + (int64_t)row[u] * a.ldy + col[u], f);
+    for (int e = 0; e < 8; ++e) f[e] = id[u] < a.V ? f[e] * scale : 0.f;
+    if (blockIdx.x * (kThreads * kUnroll) + kThreads * u + threadIdx.x < groups)
+      Eight<T>::store(static_cast<T*>(a.y) + (int64_t)row[u] * a.ldy + col[u], f);
   }
 }
 

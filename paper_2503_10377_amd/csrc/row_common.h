@@ -159,15 +159,18 @@ struct Dropper {
       : seed(d.seed), offset(d.offset), t16(d.threshold << 16), scale(d.threshold ? d.scale : 1.f) {
     if (d.offset_dev) offset += *d.offset_dev;
   }
-  // f: the elements 8 g .. 8 g + 7 of the whole sequence; the dropped ones
-  // become zero, the others are left for the caller to scale.
-  __device__ __forceinline__ void mask(uint64_t g, float (&f)[8]) const {
-    if (t16 == 0) return;
-    const u32x4 w = philox(g, offset, seed);
+  // The draw of the elements 8 g .. 8 g + 7 of the whole sequence, and with it:
+  // the dropped ones of f become zero, the others are left for the caller to
+  // scale.
+  __device__ __forceinline__ u32x4 draw(uint64_t g) const { return philox(g, offset, seed); }
+  __device__ __forceinline__ void keep(const u32x4& w, float (&f)[8]) const {
     const uint16_t t = (uint16_t)(t16 >> 16);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       f[e] = (e & 1 ? w[e >> 1] >= t16 : (uint16_t)w[e >> 1] >= t) ? f[e] : 0.f;
+  }
+  __device__ __forceinline__ void mask(uint64_t g, float (&f)[8]) const {
+    if (t16 != 0) keep(draw(g), f);
   }
   __device__ __forceinline__ void apply(uint64_t g, float (&f)[8]) const {
     mask(g, f);
