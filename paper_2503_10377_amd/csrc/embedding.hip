@@ -297,7 +297,7 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs s, int spli
 // 41).  A fill of the table leaves its last 256 MB in the memory-side cache,
 // from where they go to memory while the sums run: 30 us with dy past the
 // caches, 42 through them (stores of the fill that go past that cache make the
-// fill 38 us longer).
+// fill 38 us longer); 28 since the rows ahead are loaded without branches.
 //
 // A run of at most kTile rows belongs to the wave where it begins, which
 // follows it past its places, so it is summed at once.  Of a longer run the
@@ -377,12 +377,15 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) 
   const Dropper drop(a.drop);
   Eight<T> x[kAhead];
   Eight<float> old[ADD ? kAhead : 1];
-  auto begins = [&](int u) { return u == first || key_at(u - 1) != key_at(u); };
-  auto load = [&](int u, int slot) {
-    if (u >= stop || !in) return;
-    x[slot].template read<PAST>(static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy + c);
+  auto begins = [&](int u) { return (u == first) | (key_at(u - 1) != key_at(u)); };
+  const int width = a.H * (int)sizeof(T);
+  auto load = [&](int u, int slot) {  // (nothing past the last place)
+    const bool on = u < stop;
+    x[slot].template fetch<PAST>(row_buffer(static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy, on ? width : 0), c);
     if constexpr (ADD)
-      if (begins(u)) old[slot].load(a.dtable + (int64_t)key_at(u) * a.lddt + c);
+      old[slot].template fetch<false>(
+          row_buffer(a.dtable + (int64_t)key_at(u) * a.lddt, on & begins(u) ? 4 * a.H : 0), c);
+    __builtin_amdgcn_sched_barrier(0);  // in this order: a wait for one is a wait for all before it
   };
 #pragma unroll
   for (int v = 0; v < kAhead; ++v) load(first + v, v);
@@ -393,34 +396,36 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) 
 #pragma unroll
     for (int v = 0; v < kAhead; ++v) {
       const int u = j + v;
-      if (u >= stop) break;
-      float f[8];
-      x[v].get(f);
-      drop.apply((uint64_t)(a.drop.row0 + row_at(u)) * (a.H / 8) + c / 8, f);
-      if (begins(u)) {
+      const bool on = u < stop, last = u + 1 == stop;
+      if (on) {
+        float f[8];
+        x[v].get(f);
+        drop.apply((uint64_t)(a.drop.row0 + row_at(u)) * (a.H / 8) + c / 8, f);
+        if (begins(u)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = f[e];
-        if constexpr (ADD) old[v].get(base);
-      } else {
+          for (int e = 0; e < 8; ++e) acc[e] = f[e];
+          if constexpr (ADD) old[v].get(base);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += f[e];
+          for (int e = 0; e < 8; ++e) acc[e] += f[e];
+        }
       }
       load(u + kAhead, v);
-      const bool last = u + 1 == stop;
-      if (!last && !begins(u + 1)) continue;
-      float o[8];
+      if (on & (last | begins(u + 1))) {
+        float o[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = acc[e] * a.scale;
-      if (enter || (last && leave)) {
-        Eight<float>::store(&part[w][enter ? 0 : 1][8 * lane], o);
-      } else {
-        if constexpr (ADD) {
+        for (int e = 0; e < 8; ++e) o[e] = acc[e] * a.scale;
+        if (enter | (last & leave)) {
+          Eight<float>::store(&part[w][enter ? 0 : 1][8 * lane], o);
+        } else {
+          if constexpr (ADD) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += base[e];
+            for (int e = 0; e < 8; ++e) o[e] += base[e];
+          }
+          if (in) Eight<float>::store(a.dtable + (int64_t)key_at(u) * a.lddt + c, o);
         }
-        if (in) Eight<float>::store(a.dtable + (int64_t)key_at(u) * a.lddt + c, o);
+        enter = false;
       }
-      enter = false;
     }
   }
   __syncthreads();

@@ -54,6 +54,19 @@ __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
   return __builtin_bit_cast(u32x4, b);
 }
 
+// A row (the same for the whole wave) as a buffer of `bytes` bytes: lanes past
+// its end read zeros and store nothing, so loads of a ragged row, or of one
+// that isn't there (0 bytes), need no branch.  The compiler counts loads
+// between branches exactly, and waits for all that are on their way behind a
+// load that a branch may have passed by.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* p, int bytes) {
+  return uniform_rsrc(reinterpret_cast<uint64_t>(p), __builtin_amdgcn_readfirstlane(bytes));
+}
+template <bool PAST>
+__device__ __forceinline__ u32x4 load_row16(__amdgpu_buffer_rsrc_t row, int offset) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(row, offset, 0, PAST ? 2 : 0));
+}
+
 // Eight consecutive elements as they lie in memory, for activations of either
 // type: bf16 in one 16-byte piece, fp32 in two.  Of large activations (see
 // kStreamBytes) stream() reads what nobody reads again soon, so that it takes
@@ -73,6 +86,10 @@ struct Eight<uint16_t> {
   __device__ __forceinline__ void read(const uint16_t* p) {
     if constexpr (PAST) stream(p);
     else load(p);
+  }
+  template <bool PAST>
+  __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t row, int c) {
+    v = load_row16<PAST>(row, 2 * c);
   }
   __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(v, f); }
   static __device__ __forceinline__ void store(uint16_t* p, const float (&f)[8]) {
@@ -98,6 +115,11 @@ struct Eight<float> {
   __device__ __forceinline__ void read(const float* p) {
     if constexpr (PAST) stream(p);
     else load(p);
+  }
+  template <bool PAST>
+  __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t row, int c) {
+    v[0] = __builtin_bit_cast(f32x4, load_row16<PAST>(row, 4 * c));
+    v[1] = __builtin_bit_cast(f32x4, load_row16<PAST>(row, 4 * c + 16));
   }
   __device__ __forceinline__ void get(float (&f)[8]) const {
 #pragma unroll
