@@ -67,6 +67,19 @@ __device__ __forceinline__ u32x4 load_row16(__amdgpu_buffer_rsrc_t row, int offs
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(row, offset, 0, PAST ? 2 : 0));
 }
 
+__device__ __forceinline__ float load_row4(__amdgpu_buffer_rsrc_t row) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row, 0, 0, 0));
+}
+template <bool PAST>
+__device__ __forceinline__ void store_row16(__amdgpu_buffer_rsrc_t row, int offset, const u32x4& v) {
+  using raw = unsigned int __attribute__((ext_vector_type(4)));
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(raw, v), row, offset, 0, PAST ? 2 : 0);
+}
+// One float, from the lanes where `on`.
+__device__ __forceinline__ void store_row4(__amdgpu_buffer_rsrc_t row, bool on, float v) {
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), row, on ? 0 : 4, 0, 0);
+}
+
 // Eight consecutive elements as they lie in memory, for activations of either
 // type: bf16 in one 16-byte piece, fp32 in two.  Of large activations (see
 // kStreamBytes) stream() reads what nobody reads again soon, so that it takes
@@ -94,6 +107,10 @@ struct Eight<uint16_t> {
   __device__ __forceinline__ void get(float (&f)[8]) const { unpack8(v, f); }
   static __device__ __forceinline__ void store(uint16_t* p, const float (&f)[8]) {
     *reinterpret_cast<u32x4*>(p) = pack8(f);
+  }
+  template <bool PAST>
+  static __device__ __forceinline__ void put(__amdgpu_buffer_rsrc_t row, int c, const float (&f)[8]) {
+    store_row16<PAST>(row, 2 * c, pack8(f));
   }
   static __device__ __forceinline__ void stream_out(uint16_t* p, const float (&f)[8]) {
     __builtin_nontemporal_store(pack8(f), reinterpret_cast<u32x4*>(p));
@@ -128,6 +145,11 @@ struct Eight<float> {
   static __device__ __forceinline__ void store(float* p, const float (&f)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{f[4], f[5], f[6], f[7]};
+  }
+  template <bool PAST>
+  static __device__ __forceinline__ void put(__amdgpu_buffer_rsrc_t row, int c, const float (&f)[8]) {
+    store_row16<PAST>(row, 4 * c, __builtin_bit_cast(u32x4, f32x4{f[0], f[1], f[2], f[3]}));
+    store_row16<PAST>(row, 4 * c + 16, __builtin_bit_cast(u32x4, f32x4{f[4], f[5], f[6], f[7]}));
   }
   static __device__ __forceinline__ void stream_out(float* p, const float (&f)[8]) {
     __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4*>(p));
