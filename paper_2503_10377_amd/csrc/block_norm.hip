@@ -116,7 +116,11 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   constexpr int TEAMS = NT / TEAM;
   const int H = a.H, tid = threadIdx.x % TEAM;
   const int64_t step = (int64_t)gridDim.x * TEAMS;
-  int64_t row = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+  // A row that belongs to whole waves is read and written as a buffer, so that
+  // the next row's loads wait for none of this one's stores.
+  constexpr bool WAVE = TEAM >= 64;
+  const int team = WAVE ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : threadIdx.x / TEAM;
+  int64_t row = (int64_t)blockIdx.x * TEAMS + team;
   if (row >= a.rows) return;
   if constexpr (TEAM > 64) {
     init_moments<TEAM, PER>(red, H, tid);
@@ -124,9 +128,25 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   }
   const Dropper drop(a.drop);
   const bool post = a.post != kNone, pre = a.pre != kNone;
+  const bool token = a.gate_kind == kToken;
   const float inv_h = 1.f / H, scale = a.bscale * drop.scale;
+  const int width = H * (int)sizeof(T);
   Eight<T> xn[PER], bn[PER];
+  float gn = 1.f;  // the row's gate
   auto load = [&](int64_t r) {
+    if constexpr (WAVE) {
+      const int all = r < a.rows ? width : 0;
+      const auto b = row_buffer(static_cast<const T*>(a.b) + r * a.ldb, all);
+      const auto x = row_buffer(static_cast<const T*>(a.x) + r * a.ldx, all);
+#pragma unroll
+      for (int p = 0; p < PER; ++p) bn[p].template fetch<PAST>(b, 8 * (tid + TEAM * p));
+#pragma unroll
+      for (int p = 0; p < PER; ++p) xn[p].template fetch<PAST>(x, 8 * (tid + TEAM * p));
+      gn = load_row4(row_buffer(a.gate + r, token && r < a.rows ? 4 : 0));
+      return;
+    }
+    if (r >= a.rows) return;
+    if (token) gn = a.gate[r];
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
@@ -156,6 +176,21 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       if (pre && a.pre_beta) load8f(a.pre_beta + c, qb[p]);
     }
   }
+  auto put_stats = [&](int kind, float* means, float* rstds, float mean, float rstd) {
+    if constexpr (WAVE) {
+      store_row4(row_buffer(means + row, kind == kLayer ? 4 : 0), tid == 0, mean);
+      store_row4(row_buffer(rstds + row, kind != kNone ? 4 : 0), tid == 0, rstd);
+    } else if (tid == 0) {
+      if (kind == kLayer) means[row] = mean;
+      if (kind != kNone) rstds[row] = rstd;
+    }
+  };
+  auto put = [&](void* out, int64_t ld, bool on, int p, const float (&f)[8]) {
+    T* o = static_cast<T*>(out) + row * ld;
+    const int c = 8 * (tid + TEAM * p);
+    if constexpr (WAVE) Eight<T>::template put<false>(row_buffer(o, on ? width : 0), c, f);
+    else if (on && c < H) Eight<T>::store(o + c, f);
+  };
   int ph = 0;
   for (; row < a.rows; row += step) {
     Eight<T> xr[PER];
@@ -165,17 +200,15 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       xr[p] = xn[p];
       bn[p].get(v[p]);
     }
-    if (row + step < a.rows) load(row + step);
+    const float factor = token ? scale * gn : scale;
+    load(row + step);
     float mean = 0.f, rstd = 1.f;
     if (post) {
       row_moments<TEAM, PER>(v, H, tid, a.post == kRms, inv_h, a.eps, red[ph], mean, rstd);
       ph ^= 1;
-      if (tid == 0) {
-        if (a.post == kLayer) a.post_mean[row] = mean;
-        a.post_rstd[row] = rstd;
-      }
     }
-    const float shift = -mean * rstd, factor = a.gate_kind == kToken ? scale * a.gate[row] : scale;
+    put_stats(a.post, a.post_mean, a.post_rstd, mean, rstd);
+    const float shift = -mean * rstd;
     const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
@@ -188,25 +221,20 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
         xr[p].get(x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[p][e] = fmaf(a.alpha, x[e], v[p][e]);
-        Eight<T>::store(static_cast<T*>(a.h) + row * a.ldh + c, v[p]);
       }
+      put(a.h, a.ldh, true, p, v[p]);
     }
-    if (!pre) continue;
-    row_moments<TEAM, PER>(v, H, tid, a.pre == kRms, inv_h, a.eps, red[ph], mean, rstd);
-    ph ^= 1;
-    if (tid == 0) {
-      if (a.pre == kLayer) a.pre_mean[row] = mean;
-      a.pre_rstd[row] = rstd;
+    if (pre) {
+      row_moments<TEAM, PER>(v, H, tid, a.pre == kRms, inv_h, a.eps, red[ph], mean, rstd);
+      ph ^= 1;
     }
+    put_stats(a.pre, a.pre_mean, a.pre_rstd, mean, rstd);
     const float shift2 = -mean * rstd;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-      const int c = 8 * (tid + TEAM * p);
-      if (c < H) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift2), qg[p][e], qb[p][e]);
-        Eight<T>::store(static_cast<T*>(a.z) + row * a.ldz + c, v[p]);
-      }
+      for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift2), qg[p][e], qb[p][e]);
+      put(a.z, a.ldz, pre, p, v[p]);
     }
   }
 }
