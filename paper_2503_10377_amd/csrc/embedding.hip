@@ -67,10 +67,11 @@ __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedArgs a, FastDi
     u32x4 w;
     if (drop.t16) w = drop.draw(g0 + g[u]);
     float f[8];
+    if (id[u] >= a.V) x[u].zero();
     x[u].get(f);
     if (drop.t16) drop.keep(w, f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = id[u] < a.V ? f[e] * scale : 0.f;
+    for (int e = 0; e < 8; ++e) f[e] *= scale;
     if (blockIdx.x * (kThreads * kUnroll) + kThreads * u + threadIdx.x < groups)
       Eight<T>::store(static_cast<T*>(a.y) + (int64_t)row[u] * a.ldy + col[u], f);
   }
