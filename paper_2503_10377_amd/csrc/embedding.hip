@@ -17,12 +17,9 @@ namespace {
 constexpr int kThreads = 256, kUnroll = 4;
 constexpr int64_t kMaxGroups = (int64_t)1 << 30;  // of a launch: below fast_div's 2^31
 
-// The token of row r as an index below V, or V if it lies outside the table
-// (compared as 64-bit numbers: an id past 32 bits is outside).
-__device__ __forceinline__ uint32_t token(const void* ids, int id64, int64_t r, int64_t V) {
-  const int64_t id = id64 ? static_cast<const int64_t*>(ids)[r] : static_cast<const int32_t*>(ids)[r];
-  return (uint32_t)(id >= 0 && id < V ? id : V);
-}
+// A token as an index below V, or V if it lies outside the table (compared as
+// 64-bit numbers: an id past 32 bits is outside).
+__device__ __forceinline__ uint32_t inside(int64_t id, int64_t V) { return (uint32_t)(id >= 0 && id < V ? id : V); }
 
 // A thread takes kUnroll groups of eight elements, 256 groups apart: the ids
 // first, then the table's pieces, then the draws (19 us of the vector units for
@@ -51,13 +48,13 @@ __global__ __launch_bounds__(kThreads) void embed_fwd_kernel(EmbedArgs a, FastDi
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) v[u] = static_cast<const int64_t*>(a.ids)[row[u]];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) id[u] = (uint32_t)(v[u] >= 0 && v[u] < a.V ? v[u] : a.V);
+    for (int u = 0; u < kUnroll; ++u) id[u] = inside(v[u], a.V);
   } else {
     int32_t v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) v[u] = static_cast<const int32_t*>(a.ids)[row[u]];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) id[u] = (uint32_t)(v[u] >= 0 && v[u] < a.V ? v[u] : a.V);
+    for (int u = 0; u < kUnroll; ++u) id[u] = inside(v[u], a.V);
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u)
@@ -112,6 +109,7 @@ constexpr int kMaxDigitBits = 9, kMaxDigits = 1 << kMaxDigitBits;
 constexpr int kMaxSortTiles = 128;
 constexpr int kSortThreads = 512, kSortKeys = 2, kSortWaves = kSortThreads / 64;
 constexpr int kSortStep = kSortThreads * kSortKeys;  // keys a workgroup handles at a time
+constexpr int kScan = 32;                            // tiles whose counts are on their way at once
 
 struct SortArgs {
   int64_t n;
@@ -128,8 +126,35 @@ struct SortArgs {
   int64_t V;
 };
 
-__device__ __forceinline__ uint32_t sort_key(const SortArgs& s, int64_t i) {
-  return s.key ? s.key[i] : token(s.ids, s.id64, i, s.V);
+// Keys (and rows) i[u] of a pass, those from `end` on as the first one's:
+// without branches between the loads, so all are on their way at once.
+template <int N>
+__device__ __forceinline__ void sort_keys(const SortArgs& s, const int64_t (&i)[N], int64_t end, uint32_t (&key)[N],
+                                          uint32_t (&row)[N]) {
+  int64_t at[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) at[u] = i[u] < end ? i[u] : 0;
+  auto tokens = [&](auto* ids) {
+    int64_t id[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) id[u] = ids[at[u]];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      key[u] = inside(id[u], s.V);
+      row[u] = (uint32_t)at[u];
+    }
+  };
+  if (s.key) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      key[u] = s.key[at[u]];
+      row[u] = s.row[at[u]];
+    }
+  } else if (s.id64) {
+    tokens(static_cast<const int64_t*>(s.ids));
+  } else {
+    tokens(static_cast<const int32_t*>(s.ids));
+  }
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs s, ZeroArgs z) {
@@ -143,8 +168,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs s, Ze
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * s.per_tile;
   const int64_t i1 = i0 + s.per_tile < s.n ? i0 + s.per_tile : s.n;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
-    atomicAdd(&cnt[(sort_key(s, i) >> s.shift) & (digits - 1)], 1u);  // counts: any order gives the same
+  for (int64_t step = i0; step < i1; step += kSortStep) {
+    int64_t i[kSortKeys];
+    uint32_t key[kSortKeys], row[kSortKeys];
+#pragma unroll
+    for (int u = 0; u < kSortKeys; ++u) i[u] = step + kSortThreads * u + threadIdx.x;
+    sort_keys(s, i, i1, key, row);
+#pragma unroll
+    for (int u = 0; u < kSortKeys; ++u)
+      if (i[u] < i1) atomicAdd(&cnt[(key[u] >> s.shift) & (digits - 1)], 1u);  // counts: any order gives the same
+  }
   __syncthreads();
   for (int d = threadIdx.x; d < digits; d += kSortThreads) s.counts[(int64_t)blockIdx.x * digits + d] = cnt[d];
 }
@@ -180,11 +213,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, 
   // those of digit d in earlier tiles.
   uint32_t all = 0, before = 0;
   if (tid < digits) {
-#pragma unroll 8
-    for (int t = 0; t < s.tiles; ++t) {
-      const uint32_t c = s.counts[(int64_t)t * digits + tid];
-      all += c;
-      if (t < (int)blockIdx.x) before += c;
+    for (int t0 = 0; t0 < s.tiles; t0 += kScan) {
+      uint32_t c[kScan];
+#pragma unroll
+      for (int u = 0; u < kScan; ++u) c[u] = s.counts[(int64_t)(t0 + u < s.tiles ? t0 + u : t0) * digits + tid];
+#pragma unroll
+      for (int u = 0; u < kScan; ++u) {
+        all += t0 + u < s.tiles ? c[u] : 0;
+        before += t0 + u < (int)blockIdx.x ? c[u] : 0;
+      }
     }
   }
   uint32_t incl = all;
@@ -206,16 +243,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, 
       if (tid < digits) cnt[u][tid] = 0;
     __syncthreads();
     // a wave holds kSortKeys times 64 consecutive keys
+    int64_t i[kSortKeys];
     uint32_t key[kSortKeys], row[kSortKeys], rank[kSortKeys];
 #pragma unroll
-    for (int u = 0; u < kSortKeys; ++u) {
-      const int64_t i = step + (w * kSortKeys + u) * 64 + lane;
-      const bool in = i < i1;
-      key[u] = in ? sort_key(s, i) : 0;
-      row[u] = in ? (s.key ? s.row[i] : (uint32_t)i) : 0;
-      const uint32_t d = (key[u] >> s.shift) & (digits - 1);
-      rank[u] = wave_rank(d, s.bits, in, cnt[w]);
-    }
+    for (int u = 0; u < kSortKeys; ++u) i[u] = step + (w * kSortKeys + u) * 64 + lane;
+    sort_keys(s, i, i1, key, row);
+#pragma unroll
+    for (int u = 0; u < kSortKeys; ++u)
+      rank[u] = wave_rank((key[u] >> s.shift) & (digits - 1), s.bits, i[u] < i1, cnt[w]);
     __syncthreads();
     if (tid < digits) {
       uint32_t at = base[tid];
@@ -230,8 +265,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, 
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kSortKeys; ++u) {
-      const int64_t i = step + (w * kSortKeys + u) * 64 + lane;
-      if (i < i1) {
+      if (i[u] < i1) {
         const uint32_t at = cnt[w][(key[u] >> s.shift) & (digits - 1)] + rank[u];
         s.key_out[at] = key[u];
         s.row_out[at] = row[u];
@@ -246,7 +280,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortArgs s, 
 // which a workgroup holds in LDS.  n^2 comparisons of two instructions beat the
 // passes of the sort (four launches of 5 us) while launches and their gaps are
 // what costs: 11 us for 8192 rows.  With the sums over 512 columns 8192 rows
-// take 25 us this way and 30 by the sort, 16384 rows 41 and 33.
+// take 24 us this way, 9000 by the sort 30; 16384 rows 41 and 32.
 constexpr int kSmallKeys = 8192, kRankThreads = 1024, kRankWaves = kRankThreads / 64;
 
 // split: lanes that share a row's comparisons (1, 2 or 4); a workgroup ranks
@@ -261,7 +295,16 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(SortArgs s, int spli
     return;
   }
   const int n = (int)s.n, blocks = (n + 63) / 64, tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
-  for (int i = tid; i < 64 * blocks; i += kRankThreads) key[i] = i < n ? token(s.ids, s.id64, i, s.V) : 0xffffffffu;
+  for (int i0 = tid; i0 < 64 * blocks; i0 += 4 * kRankThreads) {
+    int64_t i[4];
+    uint32_t k[4], row[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) i[u] = i0 + kRankThreads * u;
+    sort_keys(s, i, n, k, row);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i[u] < 64 * blocks) key[i[u]] = i[u] < n ? k[u] : 0xffffffffu;
+  }
   if (tid < 64) place[tid] = 0;
   __syncthreads();
   const int rows = 64 / split, li = lane & (rows - 1), i = blockIdx.x * rows + li;
@@ -538,7 +581,7 @@ __global__ __launch_bounds__(256) void embed_direct_kernel(EmbedArgs a, int sums
     for (int u = 0; u < kDirectHeld; ++u) {
       const int r = 64 * u + lane;
       const int64_t id = ids[r < n ? r : 0];
-      held[u] = r < n && id >= 0 && id < a.V ? (uint32_t)id : V;
+      held[u] = r < n ? inside(id, a.V) : V;
     }
   };
   if (a.id64) hold(static_cast<const int64_t*>(a.ids));
