@@ -554,6 +554,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
 // 32 groups of rows, group t adding blocks t, t + 32, ... in order (the loads
 // all at once), then the groups are added pairwise.
 constexpr int kRedCols = 32, kRedGroups = 32, kRedThreads = kRedCols / 4 * kRedGroups;
+constexpr int kRedAhead = 8;  // 256 blocks at once
 __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArgs a) {
   fetch_args(a);
   __shared__ __attribute__((aligned(16))) float red[4][kRedGroups][kRedCols + 4];
@@ -563,11 +564,27 @@ __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArg
   const int c = blockIdx.x * kRedCols + lc, H = a.H;
   const Slots slots = bn_slots(a);
   const int64_t step = (int64_t)slots.n * H;
+  const bool post = a.post != kNone, chan = a.gate_kind == kChannel;
+  const int oc = blockIdx.x * kRedCols + threadIdx.x;
+  // what the gradients are made with, on its way before the sums
+  const int at = threadIdx.x < kRedCols && oc < H ? oc : 0;
+  const float gate = chan ? a.gate[at] : 1.f;
+  const float gamma = chan && post ? a.post_gamma[at] : 1.f;
+  const float beta = chan && post && a.post_beta ? a.post_beta[at] : 0.f;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (c < H) {
     const float* p = a.part + (int64_t)i * H + c;
-#pragma unroll 16
-    for (int b = t; b < a.nblocks; b += kRedGroups) s += *reinterpret_cast<const f32x4*>(p + b * step);
+    for (int b0 = t; b0 < a.nblocks; b0 += kRedAhead * kRedGroups) {
+      f32x4 v[kRedAhead];
+#pragma unroll
+      for (int u = 0; u < kRedAhead; ++u) {
+        const int b = b0 + kRedGroups * u;
+        v[u] = *reinterpret_cast<const f32x4*>(p + (b < a.nblocks ? b : b0) * step);
+      }
+#pragma unroll
+      for (int u = 0; u < kRedAhead; ++u)
+        if (b0 + kRedGroups * u < a.nblocks) s += v[u];
+    }
   }
   *reinterpret_cast<f32x4*>(&red[i][t][lc]) = s;
   __syncthreads();
@@ -583,24 +600,21 @@ __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArg
     total[i][th] = v[0];
   }
   __syncthreads();
-  const int oc = blockIdx.x * kRedCols + threadIdx.x;
   if (threadIdx.x >= kRedCols || oc >= H) return;
   float S[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) S[u] = slots.on[u] ? total[slots.at[u]][threadIdx.x] : 0.f;
-  const bool post = a.post != kNone, chan = a.gate_kind == kChannel;
   auto put = [&](float* dst, float x) {
     if (a.accumulate) dst[oc] += x;
     else dst[oc] = x;
   };
-  const float gate = chan ? a.gate[oc] : 1.f;
   if (slots.on[0]) put(a.d_pre_gamma, S[0]);
   if (slots.on[1]) put(a.d_pre_beta, S[1]);
   if (post && a.d_post_gamma) put(a.d_post_gamma, gate * S[2]);
   if (post && a.post_beta && a.d_post_beta) put(a.d_post_beta, gate * S[3]);
   if (chan && a.d_gate) {
-    float g = post ? a.post_gamma[oc] * S[2] : S[2];
-    if (post && a.post_beta) g += a.post_beta[oc] * S[3];
+    float g = gamma * S[2];
+    if (post && a.post_beta) g += beta * S[3];
     put(a.d_gate, g);
   }
 }
