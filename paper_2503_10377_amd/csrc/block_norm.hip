@@ -555,6 +555,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
 // all at once), then the groups are added pairwise.
 constexpr int kRedCols = 32, kRedGroups = 32, kRedThreads = kRedCols / 4 * kRedGroups;
 constexpr int kRedAhead = 8;  // 256 blocks at once
+template <bool ADD>
 __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArgs a) {
   fetch_args(a);
   __shared__ __attribute__((aligned(16))) float red[4][kRedGroups][kRedCols + 4];
@@ -566,11 +567,20 @@ __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArg
   const int64_t step = (int64_t)slots.n * H;
   const bool post = a.post != kNone, chan = a.gate_kind == kChannel;
   const int oc = blockIdx.x * kRedCols + threadIdx.x;
-  // what the gradients are made with, on its way before the sums
+  // what the gradients are made with and added to, on its way before the sums
   const int at = threadIdx.x < kRedCols && oc < H ? oc : 0;
   const float gate = chan ? a.gate[at] : 1.f;
   const float gamma = chan && post ? a.post_gamma[at] : 1.f;
   const float beta = chan && post && a.post_beta ? a.post_beta[at] : 0.f;
+  float* const out[5] = {slots.on[0] ? a.d_pre_gamma : nullptr, slots.on[1] ? a.d_pre_beta : nullptr,
+                         post ? a.d_post_gamma : nullptr, post && a.post_beta ? a.d_post_beta : nullptr,
+                         chan ? a.d_gate : nullptr};
+  float old[5];
+#pragma unroll
+  for (int u = 0; u < 5; ++u) {
+    old[u] = 0.f;
+    if (ADD && out[u]) old[u] = out[u][at];
+  }
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (c < H) {
     const float* p = a.part + (int64_t)i * H + c;
@@ -604,19 +614,10 @@ __global__ __launch_bounds__(4 * kRedThreads) void bn_reduce_kernel(BlockNormArg
   float S[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) S[u] = slots.on[u] ? total[slots.at[u]][threadIdx.x] : 0.f;
-  auto put = [&](float* dst, float x) {
-    if (a.accumulate) dst[oc] += x;
-    else dst[oc] = x;
-  };
-  if (slots.on[0]) put(a.d_pre_gamma, S[0]);
-  if (slots.on[1]) put(a.d_pre_beta, S[1]);
-  if (post && a.d_post_gamma) put(a.d_post_gamma, gate * S[2]);
-  if (post && a.post_beta && a.d_post_beta) put(a.d_post_beta, gate * S[3]);
-  if (chan && a.d_gate) {
-    float g = gamma * S[2];
-    if (post && a.post_beta) g += beta * S[3];
-    put(a.d_gate, g);
-  }
+  const float sums[5] = {S[0], S[1], gate * S[2], gate * S[3], fmaf(beta, S[3], gamma * S[2])};
+#pragma unroll
+  for (int u = 0; u < 5; ++u)
+    if (out[u]) out[u][oc] = ADD ? old[u] + sums[u] : sums[u];
 }
 
 template <typename T, bool PAST, int NT, int TEAM, int PER>
@@ -722,8 +723,11 @@ hipError_t launch_block_norm_bwd(const BlockNormArgs& a, hipStream_t stream) {
                             : (a.f32 ? backward<float, false>(b, stream) : backward<uint16_t, false>(b, stream));
   const int sums = bn_slots(a).n;
   if (e != hipSuccess || sums == 0) return e;
-  hipLaunchKernelGGL(bn_reduce_kernel, dim3((unsigned)((a.H + kRedCols - 1) / kRedCols)),
-                     dim3((unsigned)(sums * kRedThreads)), 0, stream, b);
+  const dim3 grid((unsigned)((a.H + kRedCols - 1) / kRedCols)), block((unsigned)(sums * kRedThreads));
+  if (a.accumulate)
+    hipLaunchKernelGGL(bn_reduce_kernel<true>, grid, block, 0, stream, b);
+  else
+    hipLaunchKernelGGL(bn_reduce_kernel<false>, grid, block, 0, stream, b);
   return hipGetLastError();
 }
 
