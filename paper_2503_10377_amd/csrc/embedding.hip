@@ -425,11 +425,13 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) 
   const int width = a.H * (int)sizeof(T);
   auto load = [&](int u, int slot) {  // (nothing past the last place)
     const bool on = u < stop;
-    x[slot].template fetch<PAST>(row_buffer(static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy, on ? width : 0), c);
+    const T* dy = static_cast<const T*>(a.dy) + (int64_t)row_at(u) * a.ldy;
+    x[slot].template fetch<PAST>(row_buffer(dy, on ? width : 0), c);
     // The table's old row in a branch: as an empty buffer for rows that begin no
     // run these loads made long runs 5 to 12% slower, short ones 0.5 to 2% faster.
     if constexpr (ADD)
-      if (on & begins(u)) old[slot].template fetch<false>(row_buffer(a.dtable + (int64_t)key_at(u) * a.lddt, 4 * a.H), c);
+      if (on & begins(u))
+        old[slot].template fetch<false>(row_buffer(a.dtable + (int64_t)key_at(u) * a.lddt, 4 * a.H), c);
     __builtin_amdgcn_sched_barrier(0);  // in this order: a wait for one is a wait for all before it
   };
 #pragma unroll
