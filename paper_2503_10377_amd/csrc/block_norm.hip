@@ -654,7 +654,9 @@ hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
 // bf16 rows take two groups of eight columns a thread where they can: what a
 // wave does once per row (its share of the sums, the statistics) is half as
 // much per element (forward of 8192 x 4096 with one: 88 us).  fp32 rows have
-// twice the bytes and twice the registers per element.
+// twice the bytes and twice the registers per element; rows of up to 6 x 512
+// columns take six waves (6553 x 2560: eight waves 59 us, six 54; for bf16 rows
+// two groups in four waves 28, one in six 36).
 template <typename T, bool PAST>
 hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
@@ -663,6 +665,8 @@ hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
   if (a.H <= 512) return fwd<T, PAST, 256, 64, 1>(a, stream);
   if (a.H <= 1024) return fwd<T, PAST, 256, 64, 2>(a, stream);
   if (a.H <= 2048) return fwd<T, PAST, 256 / P, 256 / P, P>(a, stream);
+  if constexpr (P == 1)
+    if (a.H <= 6 * 512) return fwd<T, PAST, 384, 384, 1>(a, stream);
   if (a.H <= 4096) return fwd<T, PAST, 512 / P, 512 / P, P>(a, stream);
   return fwd<T, PAST, 512, 512, 2>(a, stream);  // 1024 threads would have 128 registers each, too few
 }
@@ -672,6 +676,11 @@ hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
 // through the caches, with 512 workgroups of one team: 100 us with the sums'
 // reduction, with 256 of two teams 94); up to 512 columns a wave needs fewer registers and twice as
 // many fit.
+// Widths that would leave waves of such a team half empty take one group a
+// thread and, with fewer registers, 768 threads (with LayerNorms, gate and
+// dropout, two groups in 512 threads against this: 13107 x 1280 bf16 55 and 46
+// us, 6553 x 2560 54 and 47, 3276 x 5120 53 and 49.5; 6553 x 2560 fp32 102 and
+// 97; 8192 x 2048, where no wave is empty, even).
 template <typename T, bool PAST>
 hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
@@ -679,7 +688,12 @@ hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
   if (a.H <= 256) return bwd<T, PAST, 256, 32, 1>(a, stream);
   if (a.H <= 512) return bwd<T, PAST, 256, 64, 1>(a, stream);
   if (a.H <= 1024) return bwd<T, PAST, 512, 64, 2>(a, stream);
+  if constexpr (P == 2) {
+    if (a.H <= 3 * 512) return bwd<T, PAST, 768, 192, 1>(a, stream);
+    if (a.H > 8 * 512 && a.H <= 12 * 512) return bwd<T, PAST, 768, 768, 1>(a, stream);
+  }
   if (a.H <= 2048) return bwd<T, PAST, 512, 256 / P, P>(a, stream);
+  if (a.H <= 6 * 512) return bwd<T, PAST, 768, 384, 1>(a, stream);
   if (a.H <= 4096) return bwd<T, PAST, 512, 512 / P, P>(a, stream);
   return bwd<T, PAST, 512, 512, 2>(a, stream);
 }
@@ -690,6 +704,7 @@ int teams_of(int H, int f32) {
   if (H <= 512) return H <= 128 ? 16 : H <= 256 ? 8 : 4;
   if (H <= 1024) return 8;
   if (H <= 2048) return f32 ? 2 : 4;
+  if (H <= 6 * 512) return 2;
   return H <= 4096 && !f32 ? 2 : 1;
 }
 int64_t bwd_blocks(int64_t rows, int H, int f32) {

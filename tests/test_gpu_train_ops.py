@@ -384,8 +384,8 @@ def test_block_norm(rows, H, ld, dtype, post, pre, gate, beta, p, alpha, scale):
         assert torch.equal(g["gate"], g2["gate"])
 
 
-@pytest.mark.parametrize("dtype,H", [("bf16", H) for H in (128, 256, 512, 1024, 2048, 8192)] +
-                         [("f32", H) for H in (128, 256, 512, 1024, 2048, 4096, 8192)])
+@pytest.mark.parametrize("dtype,H", [("bf16", H) for H in (128, 256, 512, 1024, 1536, 2048, 2560, 5120, 8192)] +
+                         [("f32", H) for H in (128, 256, 512, 1024, 2048, 2560, 4096, 8192)])
 @pytest.mark.parametrize("post,gate", [("layer", "channel"), ("none", "token"), ("none", "none")])
 def test_block_norm_of_large_activations(dtype, H, post, gate):
     """Activations of 32 MiB and more are read past the caches: the same bits
