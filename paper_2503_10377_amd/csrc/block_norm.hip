@@ -209,14 +209,13 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       ph ^= 1;
     }
     put_stats(a.post, a.post_mean, a.post_rstd, mean, rstd);
-    const float shift = -mean * rstd;
     const uint64_t g0 = (uint64_t)(a.drop.row0 + row) * (H / 8);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
       const int c = 8 * (tid + TEAM * p);
       if (c < H) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[p][e] = factor * fmaf(fmaf(v[p][e], rstd, shift), pg[p][e], pb[p][e]);
+        for (int e = 0; e < 8; ++e) v[p][e] = factor * fmaf((v[p][e] - mean) * rstd, pg[p][e], pb[p][e]);
         drop.mask(g0 + c / 8, v[p]);
         float x[8];
         xr[p].get(x);
@@ -230,11 +229,10 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       ph ^= 1;
     }
     put_stats(a.pre, a.pre_mean, a.pre_rstd, mean, rstd);
-    const float shift2 = -mean * rstd;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[p][e] = fmaf(fmaf(v[p][e], rstd, shift2), qg[p][e], qb[p][e]);
+      for (int e = 0; e < 8; ++e) v[p][e] = fmaf((v[p][e] - mean) * rstd, qg[p][e], qb[p][e]);
       put(a.z, a.ldz, pre, p, v[p]);
     }
   }
@@ -400,7 +398,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
       zr[p] = zn[p];
       dn[p].get(D[p]);
     }
-    const float rstd1 = st[0], shift1 = -st[1] * rstd1, rstd = st[2], shift = -st[3] * rstd;
+    const float rstd1 = st[0], mean1 = st[1], rstd = st[2], mean = st[3];
     const float k = a.gate_kind == kToken ? st[4] : 1.f;
     if (AHEAD && (WAVE || row + TEAMS < r1)) load(row + TEAMS);
     if (pre) {
@@ -413,7 +411,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           zr[p].get(zv);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float xh = fmaf(hv[e], rstd1, shift1), g = zv[e] * qg[p][e];
+            const float xh = (hv[e] - mean1) * rstd1, g = zv[e] * qg[p][e];
             s[0] += g;
             s[1] += g * xh;
             sum[0][p][e] += zv[e] * xh;
@@ -432,7 +430,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           zr[p].get(zv);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            D[p][e] += rstd1 * (fmaf(zv[e], qg[p][e], -m1) - fmaf(hv[e], rstd1, shift1) * m2);
+            D[p][e] += rstd1 * (fmaf(zv[e], qg[p][e], -m1) - (hv[e] - mean1) * rstd1 * m2);
         }
       }
     }
@@ -473,7 +471,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           br[p].get(bv);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float m = D[p][e], bh = fmaf(bv[e], rstd, shift), w = m * pg[p][e];
+            const float m = D[p][e], bh = (bv[e] - mean) * rstd, w = m * pg[p][e];
             const float mb = POST || m != 0.f ? bh : 0.f;  // a dropped element is zero whatever b holds
             s[0] += w;
             s[1] += w * mb;
@@ -502,7 +500,7 @@ __global__ __launch_bounds__(NT) void bn_bwd_kernel(BlockNormArgs a) {
           float bv[8];
           br[p].get(bv);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) D[p][e] = kr * (D[p][e] - m1 - fmaf(bv[e], rstd, shift) * m2);
+          for (int e = 0; e < 8; ++e) D[p][e] = kr * (D[p][e] - m1 - (bv[e] - mean) * rstd * m2);
         } else if constexpr (MODE == kGated) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) D[p][e] *= k;

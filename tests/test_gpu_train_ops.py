@@ -493,6 +493,56 @@ def test_block_norm_offset_rows():
     fwd_check(c, h, z)
 
 
+def near_back_error(v, e_v, g, e_g, kind, mean, rstd):
+    """back_error for a normalised value (v - mean) rstd whose roundings are
+    relative to |v - mean|, however far the mean lies."""
+    vh = np.abs(v - mean[:, None]) * rstd[:, None]
+    m1 = rowmean(np.abs(g)) if kind == "layer" else 0.0
+    e1 = rowmean(e_g) + 44 * U * m1 if kind == "layer" else 0.0
+    m2 = rowmean(np.abs(g) * vh)
+    e2 = rowmean(e_g * vh) + 48 * U * m2
+    return rstd[:, None] * (e_g + e1 + vh * e2 + 8 * U * (np.abs(g) + m1 + vh * m2)), vh
+
+
+@pytest.mark.parametrize("rows,H,dtype,gate,mean", [
+    (17, 64, "f32", "channel", 10000.0), (40, 200, "f32", "token", 10000.0), (33, 512, "f32", "none", 10000.0),
+    (50, 1024, "f32", "channel", 10000.0), (17, 2048, "f32", "token", 1000.0), (9, 2560, "f32", "channel", 10000.0),
+    (20, 8192, "f32", "channel", 10000.0), (40, 1536, "bf16", "channel", 64.0), (12, 5120, "bf16", "token", 64.0),
+])
+def test_block_norm_backward_of_offset_rows(rows, H, dtype, gate, mean, monkeypatch):
+    """Rows whose mean is far larger than their deviation: with the statistics
+    as inputs, v - mean loses nothing, so the bounds know no mean."""
+    announce(f"block norm backward, large mean rows={rows} H={H} {dtype} {gate} mean={mean}")
+    c = Case(rows, H, H, dtype, "layer", "layer", gate, True, 0.1, seed=13)
+    c.x = (c.x.float() * 0.5 + mean).to(DT[dtype])
+    c.b = (c.b.float() / 1.5 + mean).to(DT[dtype])
+    h, _ = c.forward()
+    dz, dh = randn(rows, H, H, dtype, 67).cuda(), randn(rows, H, H, dtype, 68).cuda()
+    dx, db, g = run_bwd(c, h, dz, dh)
+    monkeypatch.setattr(sys.modules[__name__], "back_error", near_back_error)
+    bwd_check(c, h, dz, dh, dx, db, g)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H", [64, 256, 512, 1024, 2048, 4096, 8192])
+def test_block_norm_of_constant_rows_is_beta(H, dtype):
+    """Rows of one whole number, whose mean is exact at these widths: nothing is
+    left of v - mean, and the norm gives its beta, rounded once."""
+    announce(f"block norm of constant rows H={H} {dtype}")
+    rows = 5
+    v = torch.tensor([1000.0, 0.0, -3.0, 129024.0, 1.0])[:, None].expand(rows, H).to(DT[dtype]).contiguous().cuda()
+    zero = torch.zeros_like(v)
+    gamma, beta = torch.full((H,), 1.5, device="cuda"), torch.linspace(-1, 1, H, device="cuda")
+    out, other = torch.empty_like(v), torch.empty_like(v)
+    s = [torch.empty(rows, device="cuda") for _ in range(2)]
+    L.sppo_block_norm_fwd(L.block_norm(H, dtype, post="layer", post_gamma=gamma, post_beta=beta), rows, None, zero, H,
+                          v, H, out, H, None, 0, L.block_norm_stats(post_mean=s[0], post_rstd=s[1]))
+    assert torch.equal(out, beta.to(DT[dtype]).expand(rows, H))
+    L.sppo_block_norm_fwd(L.block_norm(H, dtype, pre="layer", pre_gamma=gamma, pre_beta=beta), rows, None, v, H,
+                          zero, H, other, H, out, H, L.block_norm_stats(pre_mean=s[0], pre_rstd=s[1]))
+    assert torch.equal(other, v) and torch.equal(out, beta.to(DT[dtype]).expand(rows, H))
+
+
 def test_block_norm_gates_only_what_is_kept():
     """No norm after the branch: NaN in dropped places of the branch reaches
     neither h nor the gate's gradient."""
