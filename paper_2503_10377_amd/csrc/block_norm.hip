@@ -104,7 +104,9 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
 // narrow rows a half or a quarter of one).  A team takes rows in turn, so the
 // parameters stay in its registers (read per row they would be 2.5 times the
 // activations' bytes, out of L2), with a channel's gate folded into the norm
-// after the branch: gate n = bh (gate gamma) + gate beta.  The next row's x and
+// after the branch: gate n = bh (gate gamma) + gate beta.  (Not an infinite
+// one, which would leave 0 inf and inf - inf of sums that are neither: its sign
+// is folded, and the sum multiplied after that.)  The next row's x and
 // b are on their way while a row is worked on.  HBM-bound: 8192 x 4096 bf16
 // with both LayerNorms, gate and dropout in 46 us, 5.8 TB/s (52.7 us and 5.1
 // TB/s on new data every time), the vector units busy for 66% of it.
@@ -159,6 +161,7 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   };
   load(row);  // on its way before the parameters
   float pg[PER][8], pb[PER][8], qg[PER][8], qb[PER][8];
+  uint32_t endless = 0;  // bit 8 p + e: the channel's gate is infinite
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int c = 8 * (tid + TEAM * p);
@@ -171,12 +174,19 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
         float g[8];
         load8f(a.gate + c, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pg[p][e] *= g[e], pb[p][e] *= g[e];
+        for (int e = 0; e < 8; ++e) {
+          if (__builtin_isinf(g[e])) {
+            g[e] = copysignf(1.f, g[e]);
+            endless |= 1u << (8 * p + e);
+          }
+          pg[p][e] *= g[e], pb[p][e] *= g[e];
+        }
       }
       if (pre) load8f(a.pre_gamma + c, qg[p]);
       if (pre && a.pre_beta) load8f(a.pre_beta + c, qb[p]);
     }
   }
+  const bool any_endless = __ballot(endless != 0) != 0;
   auto put_stats = [&](int kind, float* means, float* rstds, float mean, float rstd) {
     if constexpr (WAVE) {
       store_row4(row_buffer(means + row, kind == kLayer ? 4 : 0), tid == 0, mean);
@@ -216,6 +226,11 @@ __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
       if (c < H) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[p][e] = factor * fmaf((v[p][e] - mean) * rstd, pg[p][e], pb[p][e]);
+        if (any_endless) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (endless >> (8 * p + e) & 1) v[p][e] *= __builtin_inff();
+        }
         drop.mask(g0 + c / 8, v[p]);
         float x[8];
         xr[p].get(x);

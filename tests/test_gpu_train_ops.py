@@ -575,6 +575,42 @@ def test_block_norm_drops_what_an_infinite_gate_makes():
     assert not np.isfinite(to_np(h)[3][~dropped]).any()
 
 
+@pytest.mark.parametrize("rows,H,dtype,post,beta", [
+    (5, 64, "f32", "none", False), (7, 256, "bf16", "layer", True), (9, 512, "bf16", "none", False),
+    (6, 1024, "f32", "rms", False), (4, 2048, "bf16", "layer", False), (8, 4096, "bf16", "rms", True),
+    (3, 8192, "f32", "layer", True), (3, 8192, "bf16", "none", False),
+])
+def test_block_norm_with_infinite_channel_gates(rows, H, dtype, post, beta):
+    """gate n is an infinity of n's sign where a channel's gate is one (NaN
+    where n is zero), a dropped element is alpha x, other channels keep their
+    bits.  n is known to 1e-5 of its terms, far below the 1e-2 asked for; alpha x
+    rounds once before the output does."""
+    announce(f"block norm, infinite channel gates rows={rows} H={H} {dtype} {post} beta={beta}")
+    c = Case(rows, H, H, dtype, post, "none", "channel", beta, 0.3, 0.75, 0.5, seed=17)
+    cols = [0, 5, 9, H - 1]
+    c.b[0, 5] = 0.0
+    h, _ = c.forward()
+    bad = torch.tensor([np.inf, -np.inf, -np.inf, np.inf])
+    c.par["gate"][cols] = bad
+    c.dpar["gate"][cols] = bad.cuda()
+    c.npar["gate"] = to_np(c.par["gate"])
+    h2, _ = c.forward()
+    rest = torch.ones(H, dtype=torch.bool)
+    rest[cols] = False
+    assert torch.equal(h[:, rest.cuda()], h2[:, rest.cuda()])
+    n = to_np(c.b)
+    if post != "none":
+        st = c.np_stats()
+        n = O._hat(n, st["post_mean"], st["post_rstd"]) * c.npar["post_gamma"] + c.npar.get("post_beta", 0.0)
+    with np.errstate(invalid="ignore"):
+        ref = 0.75 * to_np(c.x) + 0.5 * O.drop(c.npar["gate"] * n, c.keep)
+    ref, n, keep = ref[:, cols], n[:, cols], c.keep[:, cols]
+    sure = (keep == 0) | (np.abs(n) > 1e-2) | ((n == 0) & (post == "none"))
+    assert sure.mean() > 0.5 and np.isinf(ref[sure]).any()
+    within(h2[:, cols][torch.from_numpy(sure).cuda()], ref[sure],
+           (HALF[dtype] + 2 * U) * np.abs(np.nan_to_num(ref[sure], posinf=0, neginf=0)), "h")
+
+
 def test_block_norm_gradient_matches_differences():
     """The fp32 backward along random directions of every input against
     central differences of the kernel's own forward, e = 2^-6: the forward's
