@@ -514,8 +514,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, SumArgs s) 
 // The long runs across groups: the one that begins in this group and leaves
 // it, if there is one, from the group's second partial sum and the following
 // groups' first ones, in kJoinGroups rows of groups in turn and then in row
-// order.  Most workgroups find none and end after one trip to memory.
-constexpr int kJoinCols = 256, kJoinGroups = 4;
+// order.  A row of groups takes kJoinRun partial sums in turn, kJoinRun of those
+// sums in turn and then these, so that a token in all of 2^28 rows is the end of
+// 64 + 64 + 256 additions and not of 2^20.  Most workgroups find none and end
+// after one trip to memory.
+constexpr int kJoinCols = 256, kJoinGroups = 4, kJoinRun = 64;
 constexpr int kJoinThreads = kJoinCols / 4 * kJoinGroups;
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, SumArgs s) {
   __shared__ __attribute__((aligned(16))) float red[kJoinGroups][kJoinCols];
@@ -546,9 +549,19 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedArgs a, S
   const int c = blockIdx.y * kJoinCols + lc;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   if (c < a.H) {
+    for (int64_t u = t + grp; u <= end;) {
+      f32x4 mid = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < kJoinRun && u <= end; ++i) {
+        const int64_t left = (end - u) / kJoinGroups + 1;
+        const int n = left < kJoinRun ? (int)left : kJoinRun;
+        f32x4 run = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int64_t u = t + grp; u <= end; u += kJoinGroups)
-      sum += *reinterpret_cast<const f32x4*>(s.part + (u * 2 + (u == t ? 1 : 0)) * a.H + c);
+        for (int k = 0; k < n; ++k, u += kJoinGroups)
+          run += *reinterpret_cast<const f32x4*>(s.part + (u * 2 + (u == t ? 1 : 0)) * a.H + c);
+        mid += run;
+      }
+      sum += mid;
+    }
   }
   *reinterpret_cast<f32x4*>(&red[grp][lc]) = sum;
   __syncthreads();

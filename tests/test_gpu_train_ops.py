@@ -798,6 +798,23 @@ def test_embedding(rows, H, V, dtype, idt, kind, p, scale):
     assert torch.equal(acc[:, H:].cpu(), base[:, H:])
 
 
+def test_embedding_gradient_of_one_token_in_all_rows():
+    """2^21 rows of one token, columns of one value each: equal partial sums of
+    one sign, whose roundings in a plain chain add up (400 to 1400 u here).  16
+    rows, 4 waves, then 64, 64 and 2 sums in turn, 4 chains and the scale."""
+    rows, H, V = 2 ** 21, 8, 3
+    announce(f"embedding gradient, rows={rows} of one token")
+    vals = torch.tensor([1.2345678, 1.7, 1.1, 1.9999, 1.3, 1.45, -1.7, -1.3])
+    dy = vals.expand(rows, H).contiguous().cuda()
+    ids = torch.ones(rows, dtype=torch.int32, device="cuda")
+    ws = torch.empty(L.sppo_embedding_bwd_workspace(rows, H), dtype=torch.uint8, device="cuda")
+    dt = torch.full((V, H), 7.0, device="cuda")
+    L.sppo_embedding_bwd(rows, H, V, ids, dy, H, 1.0, None, dt, H, ws, ws.numel(), 0, "f32", "i32")
+    ref = to_np(vals) * rows
+    within(dt[1], ref, (16 + 4 + 64 + 64 + 2 + 4 + 1) * U * np.abs(ref), "dtable")
+    assert torch.all(dt[::2] == 0)
+
+
 def test_embedding_rows_outside_read_nothing():
     """NaN in the rows of dy whose ids lie outside reaches no gradient, and a
     table of NaN no output row of such an id."""
