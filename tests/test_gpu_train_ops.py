@@ -481,6 +481,62 @@ def test_block_norm_in_place():
         assert torch.equal(dh, dx) and torch.equal(dz, db)
 
 
+FWD_ALIASES = [("x", None), ("b", None), ("x", "b"), (None, "b")]                    # h and z over
+BWD_ALIASES = [("dh", None), ("dz", None), (None, "b"), (None, "dz"), (None, "h"),   # dx and db over
+               ("dh", "b"), ("dh", "dz"), ("dh", "h"), ("dz", "b"), ("dz", "h")]
+
+
+@pytest.mark.parametrize("rows,H,dtype", [
+    (9000, 120, "bf16"), (9000, 200, "f32"), (5000, 512, "bf16"), (9000, 1024, "f32"), (3000, 1536, "bf16"),
+    (3000, 2048, "bf16"), (2000, 2560, "f32"), (1500, 4096, "f32"), (5000, 4096, "bf16"), (900, 5120, "bf16"),
+    (700, 8192, "f32"), (2100, 8192, "f32"),
+])
+@pytest.mark.parametrize("post,gate", [("layer", "token"), ("none", "channel"), ("none", "none")])
+def test_block_norm_over_its_inputs(rows, H, dtype, post, gate):
+    """Every output that may be the buffer of an input, in every layout of a
+    row, with more rows than there are teams: the bits of separate buffers."""
+    announce(f"block norm over its inputs rows={rows} H={H} {dtype} post={post} gate={gate}")
+    g = torch.Generator(device="cuda").manual_seed(H)
+    src = {k: torch.randn(rows, H, generator=g, device="cuda").to(DT[dtype]) for k in ("x", "b", "dz", "dh")}
+    rand = lambda n: 0.5 + torch.rand(n, generator=g, device="cuda")  # noqa: E731
+    par = {k: rand(H) for k in ["pre_gamma", "pre_beta"] + (["post_gamma", "post_beta"] if post != "none" else [])}
+    if gate != "none":
+        par["gate"] = rand(rows if gate == "token" else H)
+    bn = L.block_norm(H, dtype, post, "layer", gate, 1e-5, 0.9, 0.5, **par)
+    st = {k: torch.empty(rows, device="cuda") for k in ("post_mean", "post_rstd", "pre_mean", "pre_rstd")}
+    cst, drop = L.block_norm_stats(**st), L.drop_spec(0.1, 33, 1, 70)
+    nb = L.sppo_block_norm_bwd_workspace(bn, rows)
+    ws = torch.empty(nb // 4, device="cuda")
+
+    def fwd(h_over, z_over):
+        t = {k: src[k].clone() for k in ("x", "b")}
+        h = t[h_over] if h_over else torch.empty_like(t["x"])
+        z = t[z_over] if z_over else torch.empty_like(t["x"])
+        L.sppo_block_norm_fwd(bn, rows, drop, t["x"], H, t["b"], H, h, H, z, H, cst)
+        return [h, z] + [v.clone() for v in st.values()]
+
+    def bwd(dx_over, db_over):
+        t = {k: src[k].clone() for k in ("b", "h", "dz", "dh")}
+        dx = t[dx_over] if dx_over else torch.empty_like(t["b"])
+        db = t[db_over] if db_over else torch.empty_like(t["b"])
+        grads = {k: torch.empty_like(v) for k, v in par.items()}
+        L.sppo_block_norm_bwd(bn, rows, drop, t["b"], H, t["h"], H, cst, t["dz"], H, t["dh"], H, dx, H, db, H,
+                              L.block_norm_grads(**grads), ws, nb, 0)
+        return [dx, db] + list(grads.values())
+
+    for v in st.values():
+        v.zero_()
+    base = fwd(None, None)
+    src["h"] = base[0]
+    for pair in FWD_ALIASES:
+        for i, (u, v) in enumerate(zip(base, fwd(*pair))):
+            assert torch.equal(u, v), (pair, i)
+    base = bwd(None, None)
+    for pair in BWD_ALIASES:
+        for i, (u, v) in enumerate(zip(base, bwd(*pair))):
+            assert torch.equal(u, v), (pair, i)
+
+
 def test_block_norm_offset_rows():
     """Rows of mean 1000 and deviation 1 (and one constant row): the squares
     are taken around the mean, so nothing cancels."""
