@@ -5,6 +5,8 @@
 // Done by separate kernels, n and h would travel to memory and back.  One row
 // is held by a team of threads in registers (TEAM threads, PER groups of
 // eight columns each); both norms' sums stay within the team.
+#include <atomic>
+
 #include "row_common.h"
 
 namespace sppo {
@@ -640,12 +642,20 @@ hipError_t fwd(const BlockNormArgs& a, hipStream_t stream) {
   const int64_t teams = NT / TEAM, all = (a.rows + teams - 1) / teams;
   // As many workgroups as are resident at once: more would begin when the first
   // have taken all of their rows (8192 x 4096: 768 of them 52.8 us, 1024 57.1).
-  static const int resident = [] {
-    int n = 0;
+  // Asked for until it is known: a query that fails is the call's error, and the
+  // next call asks again.
+  static std::atomic<int> known{0};
+  int resident = known.load(std::memory_order_relaxed);
+  if (resident == 0) {
     const hipError_t e =
-        hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, bn_fwd_kernel<T, PAST, NT, TEAM, PER>, NT, 0);
-    return e == hipSuccess && n > 0 ? n : 1;
-  }();
+        hipOccupancyMaxActiveBlocksPerMultiprocessor(&resident, bn_fwd_kernel<T, PAST, NT, TEAM, PER>, NT, 0);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();  // reported here, not by the next launch
+      return e;
+    }
+    if (resident < 1) return hipErrorLaunchOutOfResources;
+    known.store(resident, std::memory_order_relaxed);
+  }
   const int64_t most = (int64_t)device_cus() * resident;
   hipLaunchKernelGGL((bn_fwd_kernel<T, PAST, NT, TEAM, PER>), dim3((unsigned)(all < most ? all : most)), dim3(NT), 0,
                      stream, a);
