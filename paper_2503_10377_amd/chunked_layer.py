@@ -67,8 +67,10 @@ class BlockEnds:
     def __init__(self, norm="none", gate=False, residual_scale=1.0, branch_scale=1.0, dropout=0.0):
         if norm not in L.NORMS:
             raise ValueError(f"unknown norm {norm!r}")
-        if not 0.0 <= dropout < 1.0:
-            raise ValueError("dropout must be in [0, 1)")
+        if not 0.0 <= dropout < 1.0 or L.drop_threshold(dropout) > 65535:
+            raise ValueError("dropout must be in [0, 1) and not round to 1 in units of 1/65536")
+        if not L.scale_ok(residual_scale, float("inf")) or not L.scale_ok(branch_scale):
+            raise ValueError("the scales must be finite, the branch's below 2^112")
         self.norm, self.gate = norm, bool(gate)
         self.residual_scale, self.branch_scale, self.dropout = residual_scale, branch_scale, dropout
 
@@ -100,6 +102,8 @@ class ChunkedLayer:
             raise ValueError("the layer needs Hq*D and (Hq+2Hkv)*D multiples of 256 and Hq*D <= 8192")
         if vocab is not None and not 0 < vocab < 2 ** 31:
             raise ValueError("vocab must be in [1, 2^31)")
+        if vocab is not None and not L.scale_ok(embed_scale):
+            raise ValueError("embed_scale must be finite and below 2^112")
         self.S, self.N, self.Hq, self.Hkv, self.D, self.H, self.Wt = S, n_chunks, Hq, Hkv, D, H, wt
         self.eps = eps
         self.device = device

@@ -526,6 +526,17 @@ def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
+def drop_threshold(p) -> int:
+    """T of a dropout with probability p (a C float): sppo_drop needs T < 65536."""
+    return int(ctypes.c_float(p).value * 65536.0 + 0.5)
+
+
+def scale_ok(scale, bound=2.0 ** 112) -> bool:
+    """Whether a call takes this scale (a C float); by default one of a branch or
+    an embedding, finite after a dropout's factor, which is at most 65536."""
+    return abs(ctypes.c_float(scale).value) < bound
+
+
 def drop_spec(p, seed, offset=0, row0=0, offset_dev=None) -> sppo_drop:
     """The dropout of a call whose first row is the sequence's row ``row0``;
     offset_dev: a device uint64 (int64 tensor) added to ``offset``."""

@@ -265,3 +265,29 @@ def test_embedding_refuses_bad_workspaces():
     refused(BAD, call, A, ws, 2)
     sizes = [L.sppo_embedding_bwd_workspace(r, 256) for r in range(1, 5000)]
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+@pytest.mark.parametrize("change", [
+    dict(dropout=0.999999), dict(dropout=-0.1), dict(dropout=float("nan")), dict(residual_scale=float("inf")),
+    dict(residual_scale=float("nan")), dict(branch_scale=float("nan")), dict(branch_scale=-(2.0 ** 112)),
+    dict(branch_scale=1e39), dict(residual_scale=1e39),
+])
+def test_block_ends_refuse_what_the_calls_would(change):
+    """What sppo_drop and sppo_block_norm refuse is refused before a walk begins."""
+    from paper_2503_10377_amd.chunked_layer import BlockEnds
+    with pytest.raises(ValueError):
+        BlockEnds(**change)
+
+
+def test_block_ends_take_what_the_calls_take():
+    from paper_2503_10377_amd.chunked_layer import BlockEnds
+    for kw in (dict(dropout=65535 / 65536), dict(branch_scale=2.0 ** 111), dict(residual_scale=-3e38), dict()):
+        BlockEnds(**kw)
+    assert [L.drop_threshold(p) for p in (0.0, 0.5, 65535 / 65536)] == [O.threshold(p) for p in (0.0, 0.5, 65535 / 65536)]
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 2.0 ** 112])
+def test_layer_refuses_an_embedding_scale_that_the_call_would(scale):
+    from paper_2503_10377_amd.chunked_layer import ChunkedLayer
+    with pytest.raises(ValueError):
+        ChunkedLayer(256, 1, 2, 2, 128, vocab=10, embed_scale=scale, device="cpu")
