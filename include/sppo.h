@@ -512,8 +512,11 @@ sppo_status sppo_dropout(sppo_dtype dtype, int64_t rows, int32_t cols, const voi
  * RMSNorm (RMS: v rstd gamma + beta, rstd = 1/sqrt(mean(v^2) + eps)); beta
  * may be NULL (zero).  gate: fp32, one value per channel [H] (a parameter)
  * or per row [rows].  keep: the dropout above, W = H, or none.  H % 8 == 0,
- * H <= 8192.  Everything between the loads and the stores is fp32: z and
- * its statistics come from h before it is rounded. */
+ * H <= 8192, rows < 2^22 (UNSUPPORTED otherwise: the backward adds up to
+ * rows / 256 rows of a column sum in turn, in fp32; a longer sequence goes in
+ * calls of its parts, with drop's row0, and gradients that are added to).
+ * Everything between the loads and the stores is fp32: z and its statistics
+ * come from h before it is rounded. */
 typedef enum { SPPO_NORM_NONE = 0, SPPO_NORM_LAYER = 1, SPPO_NORM_RMS = 2 } sppo_norm;
 typedef enum { SPPO_GATE_NONE = 0, SPPO_GATE_CHANNEL = 1, SPPO_GATE_TOKEN = 2 } sppo_gate;
 typedef struct {
@@ -576,8 +579,9 @@ sppo_status sppo_block_norm_bwd(const sppo_block_norm* bn, int64_t rows, const s
                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /* y[r] = keep * (scale * table[ids[r]]), table [V, H] with row stride ldt,
- * |scale| < 2^112; ids [rows] of id_type.  An id outside [0, V) (padding, another rank's part
- * of a split vocabulary) gives a row of zeros, and nothing is read for it.
+ * |scale| < 2^112; ids [rows] of id_type.  An id outside [0, V) (padding,
+ * another rank's part of a split vocabulary) gives a row of zeros whatever the
+ * table holds (its row 0 may be read for it, and is not used).
  * drop: NULL for none (W = H).  rows <= 2^28, V < 2^31, H <= 2^20
  * and rows * H <= 2^38 (UNSUPPORTED otherwise; the gradient's too). */
 typedef enum { SPPO_I32 = 0, SPPO_I64 = 1 } sppo_id_type;
@@ -590,7 +594,8 @@ sppo_status sppo_embedding_fwd(sppo_dtype dtype, sppo_id_type id_type, int64_t r
  * accumulate 0 overwrites all V rows (rows without a token become zero), 1
  * adds to the rows that have tokens and leaves the others as they are.  The
  * sums run in a fixed order, so results are the same bits every time.  Ids
- * outside [0, V) contribute nothing.  workspace:
+ * outside [0, V) contribute nothing, and their rows of dy are not used.
+ * workspace:
  * sppo_embedding_bwd_workspace bytes (0 for invalid sizes; it does not
  * shrink as rows grow), 16-byte aligned. */
 size_t sppo_embedding_bwd_workspace(int64_t rows, int32_t H);

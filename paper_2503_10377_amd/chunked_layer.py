@@ -34,8 +34,13 @@ Two options put the training operators around the blocks:
           h = alpha x + s drop(gate1 N1(O W_o)),  z = LN2(h)
           y = alpha h + s drop(gate2 N2(gelu(a) W_2))
       with a norm after the branch (or none), a gate per channel (or none),
-      scales and dropout.  The masks are drawn again in the backward; b_i and
-      the norms' statistics are further planes where the backward needs them.
+      scales and dropout (one p for both branches and the embedding; norms before
+      a branch are LayerNorms).  The masks are drawn again in the backward; b_i
+      and the norms' statistics are further planes where the backward needs them.
+      The forward's z comes from h before it is rounded; the backward norms the
+      stored h again, whose z and statistics (they replace the kept m2, r2) serve
+      dW_1 and LN2's gradient, so this z differs from the forward's by what the
+      rounding of h to bf16 makes of it.
   vocab=V              the walk starts from tokens: x_i = drop(scale
       w_emb[tokens_i]), with the block ends' dropout if there are any, is
       looked up in the forward and again in the backward (it is no plane, so it

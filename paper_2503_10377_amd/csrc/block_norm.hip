@@ -110,8 +110,8 @@ __device__ __forceinline__ void row_moments(const float (&v)[PER][8], int H, int
 // one, which would leave 0 inf and inf - inf of sums that are neither: its sign
 // is folded, and the sum multiplied after that.)  The next row's x and
 // b are on their way while a row is worked on.  HBM-bound: 8192 x 4096 bf16
-// with both LayerNorms, gate and dropout in 46 us, 5.8 TB/s (52.7 us and 5.1
-// TB/s on new data every time), the vector units busy for 66% of it.
+// with both LayerNorms, gate and dropout in 46 us, 5.8 TB/s (52.9 us and 5.1
+// TB/s on new data every time), the vector units busy for 67% of it.
 template <typename T, bool PAST, int NT, int TEAM, int PER>
 __global__ __launch_bounds__(NT) void bn_fwd_kernel(BlockNormArgs a) {
   fetch_args(a);
@@ -307,7 +307,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int tid, float* red) {
 // A team takes rows in turn with the parameters in registers (gate and gamma
 // as one) and the next row's h, dz, dh, b and statistics on their way, and adds
 // its part of the column sums row by row.  8192 x 4096 bf16 with both
-// LayerNorms, gate and dropout: 79 us and 5.5 for the sums' reduction, 5.2 TB/s
+// LayerNorms, gate and dropout: 80 us and 5.7 for the sums' reduction, 5.2 TB/s
 // with the column sums' traffic (through the caches 87 and 7, dx alone 3 of
 // them).  MODE: what the branch needs beyond its mask (two waves a SIMD hold
 // all of it in registers; asking for four, with some of it in scratch memory,
@@ -678,8 +678,8 @@ hipError_t bwd(const BlockNormArgs& a, hipStream_t stream) {
 // wave does once per row (its share of the sums, the statistics) is half as
 // much per element (forward of 8192 x 4096 with one: 88 us).  fp32 rows have
 // twice the bytes and twice the registers per element; rows of up to 6 x 512
-// columns take six waves (6553 x 2560: eight waves 59 us, six 54; for bf16 rows
-// two groups in four waves 28, one in six 36).
+// columns take six waves (6553 x 2560 on new data: eight waves 60 us, six 57; for
+// bf16 rows two groups in four waves 32, one in six 44).
 template <typename T, bool PAST>
 hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;
@@ -701,9 +701,9 @@ hipError_t forward(const BlockNormArgs& a, hipStream_t stream) {
 // many fit.
 // Widths that would leave waves of such a team half empty take one group a
 // thread and, with fewer registers, 768 threads (with LayerNorms, gate and
-// dropout, two groups in 512 threads against this: 13107 x 1280 bf16 55 and 46
-// us, 6553 x 2560 54 and 47, 3276 x 5120 53 and 49.5; 6553 x 2560 fp32 102 and
-// 97; 8192 x 2048, where no wave is empty, even).
+// dropout on new data, two groups in 512 threads against this: 13107 x 1280 bf16
+// 63 and 55 us, 6553 x 2560 60.5 and 55, 3276 x 5120 59.7 and 57; 6553 x 2560
+// fp32 102 and 99).
 template <typename T, bool PAST>
 hipError_t backward(const BlockNormArgs& a, hipStream_t stream) {
   constexpr int P = sizeof(T) == 2 ? 2 : 1;

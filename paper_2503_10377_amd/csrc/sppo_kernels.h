@@ -245,8 +245,8 @@ hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
 // A block's end: n = N_post(b), h = alpha x + bscale keep (gate n), z =
 // N_pre(h), and its backward (norm and gate kinds as sppo_norm, sppo_gate).
 // The backward's workgroups take rows_per_block rows each and leave their
-// column sums in part [nblocks][slots][H], slots in the order of BnSlot of
-// those that are needed; a second kernel adds them in a fixed order.
+// column sums in part [nblocks][slots][H], those of the four that are needed in
+// their order (bn_slots in block_norm.hip); a second kernel adds them in a fixed order.
 struct BlockNormArgs {
   int64_t rows;
   int H;

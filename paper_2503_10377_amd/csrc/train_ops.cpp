@@ -75,8 +75,9 @@ sppo_status check_norm(const sppo_block_norm* bn, int64_t rows) {
   if (!aligned(bn->post_gamma, 4) || !aligned(bn->post_beta, 4) || !aligned(bn->gate, 4) ||
       !aligned(bn->pre_gamma, 4) || !aligned(bn->pre_beta, 4))
     return fail(SPPO_ERR_INVALID_ARG, "block norm: a misaligned parameter");
-  // a workgroup per row, of up to 1024 threads, and the grid's work items
-  if (rows > sppo::kMaxWorkItems / 1024) return fail(SPPO_ERR_UNSUPPORTED, "block norm: more than 2^22 - 1 rows");
+  // A thread of the backward adds up to rows / 256 rows (rows of one team's width
+  // and more) of a column in turn: 16384 here, 2^-10 of the terms' magnitudes.
+  if (rows >= (int64_t)1 << 22) return fail(SPPO_ERR_UNSUPPORTED, "block norm: more than 2^22 - 1 rows");
   return SPPO_OK;
 }
 
