@@ -1,0 +1,607 @@
+"""Timed cases of the operators that close a training step around the chunk
+walk: rotary positions on a chunk's queries and keys (and their inverse on the
+gradients), the cross-entropy of a chunk's logits with its gradient, the norm
+of all gradients with the factor that clips them, and the AdamW step over many
+tensors with states in 32 or in 8 bits.
+
+``own`` selects the side: False computes each operator from elementary torch
+operations in fp32 (angles and long sums in fp64), True makes the library's
+calls.  Sizes are those of the package's layer (32 heads of 128, hidden size
+4096, chunks of 8192 tokens, a vocabulary of 32768), of its tests, and generic
+ones between them.
+
+    rotary    (a, b) of a pair j -> amp (a cos - b sin, b cos + a sin), angle =
+              position * freq_j; pairs are (j, j + rot/2) (half) or (2j, 2j+1);
+              the inverse turns the other way.
+    loss      lse = log sum_c exp x_c;  loss = lse - (1-e) x_t - e/V sum_c x_c + z lse^2
+              dx_c = s ((1 + 2 z lse) exp(x_c - lse) - (1-e) [c = t] - e/V);
+              targets outside [0, V) give zeros.
+    norm      sqrt(sum g^2) over all tensors, and min(1, max_norm / norm).
+    adamw     g' = f g;  m' = b1 m + (1-b1) g';  v' = b2 v + (1-b2) g'^2
+              p' = p - lr (m' / (1-b1^t) / (sqrt(v' / (1-b2^t)) + eps) + wd p)
+              8-bit states: m and r = sqrt(v) as e4m3 with one power of two for
+              32 elements, rounded by chance: with Philox4x32-10, counter
+              (group of 4 elements, t), key seed; word j of an element j: low
+              half for m, high half for r.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+BF, F32, F64, I64 = torch.bfloat16, torch.float32, torch.float64, torch.int64
+DT = {"bf16": BF, "f32": F32}
+SIZE = {"bf16": 2, "f32": 4}
+IDS = {"i32": torch.int32, "i64": I64}
+B1, B2, EPS, LR, DECAY = 0.9, 0.95, 1e-8, 1e-4, 0.1
+
+
+# ------------------------------------------------------------------- the cases
+def _rotary(name, rows, hq, hk, D, rot, layout="half", dtype="bf16", kdtype="bf16", pos="row0", row0=0, inverse=0,
+            scaling="none", pad=0):
+    return {"name": name, "kind": "rotary", "rows": rows, "hq": hq, "hk": hk, "D": D, "rot": rot, "layout": layout,
+            "dtype": dtype, "kdtype": kdtype, "pos": pos, "row0": row0, "inverse": inverse, "scaling": scaling,
+            "pad": pad}
+
+
+def _loss(name, kind, rows, V, dtype="bf16", ids="i64", smooth=0.0, z=0.0, padded=0, dead=0, pad=0):
+    return {"name": name, "kind": kind, "rows": rows, "V": V, "dtype": dtype, "ids": ids, "smooth": smooth, "z": z,
+            "padded": padded, "dead": dead, "pad": pad}
+
+
+def _opt(name, kind, tensors, size, state="f32", param="bf16", grad="f32", step=1000, shift=0):
+    """tensors "layer": the weights and norms of one layer of hidden size
+    ``size``; a number: that many tensors of 1 to ``size`` elements."""
+    return {"name": name, "kind": kind, "tensors": tensors, "size": size, "state": state, "param": param,
+            "grad": grad, "step": step, "shift": shift}
+
+
+def listed():
+    return [
+        # One new token's queries and keys, its position given: launch latency.
+        _rotary("rotary_1_token", 1, 32, 8, 128, 128, pos="i64"),
+        # The last chunk of 8192 tokens of a 128K sequence, queries and keys.
+        _rotary("rotary_8k", 8192, 32, 32, 128, 128, row0=122880),
+        # The gradients of a ragged chunk far out in a stretched context: half of each head turned, pairs side by
+        # side, dQ in bf16 beside fp32 dK accumulators, rows with gaps.
+        _rotary("rotary_inverse_3001", 3001, 32, 8, 128, 64, "interleaved", kdtype="f32", row0=1000003, inverse=1,
+                scaling="yarn", pad=64),
+        # The logits of a chunk over the layer's vocabulary, loss and gradient in one call.
+        _loss("loss_8kx32768", "loss", 8192, 32768),
+        # A short fp32 check run over an odd vocabulary, with smoothing and the penalty on lse.
+        _loss("loss_f32_37x50001", "loss", 37, 50001, "f32", "i32", 0.1, 1e-4, padded=5, pad=7),
+        # The gradient alone from a kept lse, a long ragged row with masked columns at its end.
+        _loss("loss_bwd_301x200019", "loss_bwd", 301, 200019, padded=20, dead=19, pad=5),
+        # The gradients of the layer configuration.
+        _opt("norm_layer_4096", "norm", "layer", 4096),
+        # Many small and ragged bf16 gradients.
+        _opt("norm_300_ragged", "norm", "300", 40000, grad="bf16"),
+        # A small layer's update: few elements, launch latency.
+        _opt("adamw_layer_64", "adamw", "layer", 64, param="f32", step=3),
+        # The layer configuration's weights: bf16 beside fp32 masters, states in 32 bits.
+        _opt("adamw_layer_4096", "adamw", "layer", 4096),
+        # A layer of half that width with states in 8 bits and bf16 gradients.
+        _opt("adamw_8bit_layer_2048", "adamw", "layer", 2048, "e4m3", grad="bf16"),
+        # Many small and ragged fp32 tensors off the 16-byte grid.
+        _opt("adamw_300_ragged", "adamw", "300", 40000, param="f32", shift=1),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(("rotary", "rotary", "rotary", "loss", "loss", "loss_bwd", "norm", "adamw", "adamw", "adamw"))
+    dtype = rng.choice(("bf16", "bf16", "f32"))
+    limit = 3e9
+    if kind == "rotary":
+        D = rng.choice((64, 96, 128, 128, 192, 256))
+        c = _rotary(None, _log(rng, 1, 16384), rng.randint(1, 48), rng.randint(1, 16), D,
+                    rng.choice((D, D, D // 2, 24)), rng.choice(("half", "interleaved")), dtype,
+                    rng.choice((dtype, "f32")), rng.choice(("row0", "i32", "i64")), _log(rng, 1, 2000000),
+                    rng.choice((0, 1)), rng.choice(("none", "linear", "ntk", "yarn")), rng.choice((0, 8, 128)))
+    elif kind in ("loss", "loss_bwd"):
+        rows, V = _log(rng, 1, 8192), _log(rng, 100, 300000)
+        smooth = rng.choice((0.0, 0.0, 0.1))
+        c = _loss(None, kind, rows, V, dtype, rng.choice(("i32", "i64")), smooth, rng.choice((0.0, 1e-4)),
+                  rng.choice((0, rows // 5)), rng.choice((0, 17)) if smooth == 0.0 else 0, rng.choice((0, 3, 40)))
+    else:
+        layer = rng.random() < 0.5
+        state = rng.choice(("f32", "e4m3")) if kind == "adamw" else "f32"
+        c = _opt(None, kind, "layer" if layer else str(_log(rng, 1, 400)),
+                 64 * rng.randint(1, 40) if layer else _log(rng, 10, 200000), state, rng.choice(("bf16", "f32")),
+                 rng.choice(("bf16", "f32")), _log(rng, 1, 100000), rng.choice((0, 1)) if state == "f32" else 0)
+    del c["name"]
+    while "rows" in c and c["rows"] > 1 and work(c)["bytes"] > limit / 3:
+        c["rows"] = max(1, c["rows"] * 3 // 4)
+        if "padded" in c:
+            c["padded"] = min(c["padded"], c["rows"] // 5)
+    return c
+
+
+# ------------------------------------------------------------------- the inputs
+def _gen(seed, salt):
+    return torch.Generator(device="cuda").manual_seed(1000003 * seed + salt)
+
+
+def _randn(shape, g, dtype, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def _ld(case):
+    """Row stride of a case's logits, in whole groups of eight."""
+    return -(-(case["V"] + case["pad"]) // 8) * 8
+
+
+def _sizes(case):
+    """Element counts of the tensors, and whether each decays."""
+    h = case["size"]
+    if case["tensors"] == "layer":
+        return [(h * 3 * h, 1), (h * h, 1), (h * 4 * h, 1), (4 * h * h, 1)] + [(h, 0)] * 4
+    r = np.random.RandomState(int(case["tensors"]) * 7 + h)
+    n = np.exp(r.uniform(0.0, math.log(h), int(case["tensors"]))).astype(np.int64)
+    return [(int(max(1, k)), int(i % 3 != 0)) for i, k in enumerate(n)]
+
+
+def _places(case):
+    """(offset, elements, decays) of each tensor in flat buffers, each from a
+    multiple of 32 on, and the buffers' length."""
+    at, out = 0, []
+    for n, d in _sizes(case):
+        out.append((at, n, d))
+        at += -(-n // 32) * 32
+    return out, at
+
+
+def _inv_freq(case):
+    """fp64 angles per position and the amplitude, by the scaling's formula:
+    factor 8 from 4096 positions on."""
+    rot, kind, s, L = case["rot"], case["scaling"], 8.0, 4096.0
+    base = 10000.0 * s ** (rot / (rot - 2.0)) if kind == "ntk" else 10000.0
+    f = base ** (-2.0 * np.arange(rot // 2) / rot)
+    if kind == "linear":
+        f = f / s
+    if kind == "yarn":
+        keep = np.clip((L * f / (2.0 * math.pi) - 1.0) / (32.0 - 1.0), 0.0, 1.0)
+        f = (1.0 - keep) * f / s + keep * f
+    return f, 0.1 * math.log(s) + 1.0 if kind == "yarn" else 1.0
+
+
+def _encode8(x):
+    """The nearest e4m3 codes and the blocks' exponent bytes of fp32 x (a state
+    that earlier steps left; whole blocks)."""
+    k = _block_exp(x)
+    y = x * _pow2(-k).repeat_interleave(32)
+    return y.to(torch.float8_e4m3fn), (k + 127).to(torch.uint8)
+
+
+def prepare(case, seed):
+    kind = case["kind"]
+    st = {"case": case, "seed": 7919 * seed + 12345678901}
+    g = _gen(seed, 1)
+    if kind == "rotary":
+        rows, D = case["rows"], case["D"]
+        for n, h, dt in (("q", case["hq"], case["dtype"]), ("k", case["hk"], case["kdtype"])):
+            st[n] = _randn((rows, h * D + case["pad"]), g, DT[dt])[:, :h * D]
+            st["y" + n] = torch.empty(rows, h * D, dtype=DT[dt], device="cuda")
+        st["pos"] = None
+        if case["pos"] != "row0":
+            st["pos"] = torch.randint(0, case["row0"] + rows + 100000, (rows,), generator=g,
+                                      device="cuda").to(IDS[case["pos"]])
+        f, st["amp"] = _inv_freq(case)
+        st["freq"] = torch.from_numpy(f).cuda()
+    elif kind in ("loss", "loss_bwd"):
+        rows, V, dt = case["rows"], case["V"], DT[case["dtype"]]
+        # Tokens' frequencies fall as one over the rank, and the logits follow them.
+        bias = -torch.log(torch.arange(1, V + 1, device="cuda", dtype=F32))
+        x = torch.empty(rows, _ld(case), dtype=dt, device="cuda")[:, :V]
+        x.copy_(torch.randn(rows, V, generator=g, device="cuda") * 2.0 + bias)
+        if case["dead"]:
+            x[:, V - case["dead"]:] = -float("inf")
+        u = torch.rand(rows, generator=g, device="cuda", dtype=F64)
+        t = (torch.exp(u * math.log(V - case["dead"] + 1.0)).to(I64) - 1).clamp_(0, V - 1 - case["dead"])
+        if case["padded"]:
+            t[rows - case["padded"]:] = -1
+        st["x"], st["t"], st["scale"] = x, t.to(IDS[case["ids"]]), 1.0 / rows
+        st["dx"] = torch.empty(rows, _ld(case), dtype=dt, device="cuda")[:, :V]
+        if kind == "loss_bwd":
+            st["lse"] = torch.cat([torch.logsumexp(r.to(F64), 1) for r in x.split(128)]).to(F32)
+            st["dloss"] = torch.rand(rows, generator=g, device="cuda") + 0.5
+        else:
+            st["loss"], st["lse"] = (torch.empty(rows, device="cuda") for _ in range(2))
+    else:
+        places, n = _places(case)
+        live = torch.zeros(n, dtype=torch.bool, device="cuda")
+        wd = torch.zeros(n, device="cuda")
+        for at, k, d in places:
+            live[at:at + k] = True
+            wd[at:at + k] = DECAY * d
+        flat = lambda dt: torch.zeros(n + case["shift"], dtype=dt, device="cuda")[case["shift"]:]  # noqa: E731
+        # Gradients of unequal size from block to block, as from tensor to tensor.
+        size = torch.exp(_randn(-(-n // 256), g, F32)).repeat_interleave(256)[:n] * 1e-3
+        st["g"] = flat(DT[case["grad"]])
+        st["g"].copy_(_randn(n, g, F32) * size * live)
+        if kind == "norm":
+            st["max_norm"], st["out"] = 1.0, torch.empty(2, device="cuda")
+        else:
+            master = _randn(n, g, F32, 0.02) * live
+            m = _randn(n, g, F32, 0.3) * size * live
+            v = (size * (0.5 + torch.rand(n, generator=g, device="cuda")) * live) ** 2
+            st["master"] = flat(F32)
+            st["master"].copy_(master)
+            if case["param"] == "bf16":
+                st["param"] = flat(BF)
+                st["param"].copy_(master)
+            st["wd"] = wd
+            # What the gradients' norm left: the norm and the factor.
+            st["norm"] = torch.tensor([1.2734, 1.0 / 1.2734], device="cuda")
+            if case["state"] == "f32":
+                for name, x in (("m", m), ("v", v)):
+                    st[name] = flat(F32)
+                    st[name].copy_(x)
+            else:
+                st["m"], st["ms"] = _encode8(m)
+                st["v"], st["vs"] = _encode8(v.sqrt())
+    if own:
+        _plan(st)
+    return st
+
+
+# ------------------------------------------------------------------- plain form
+def _plain_rotary(st):
+    case = st["case"]
+    rows, D, rot = case["rows"], case["D"], case["rot"]
+    pos = st["pos"]
+    if pos is None:
+        pos = torch.arange(case["row0"], case["row0"] + rows, device="cuda")
+    ang = pos.to(F64)[:, None] * st["freq"]
+    cos, sin = ((st["amp"] * f(ang)).to(F32)[:, None, :] for f in (torch.cos, torch.sin))
+    if case["inverse"]:
+        sin = -sin
+
+    def turn(x, h):
+        y = x.to(F32).reshape(rows, h, D).clone()
+        if case["layout"] == "half":
+            a, b = y[..., :rot // 2], y[..., rot // 2:rot]
+        else:
+            a, b = y[..., 0:rot:2], y[..., 1:rot:2]
+        na, nb = a * cos - b * sin, b * cos + a * sin
+        a.copy_(na)
+        b.copy_(nb)
+        return y.reshape(rows, h * D).to(x.dtype)
+
+    return {"q": turn(st["q"], case["hq"]), "k": turn(st["k"], case["hk"])}
+
+
+def _plain_loss(st):
+    case = st["case"]
+    V, e, z = case["V"], case["smooth"], case["z"]
+    x = st["x"].to(F32)
+    t = st["t"].to(I64)
+    ok = ((t >= 0) & (t < V)).to(F32)
+    tc = t.clamp(0, V - 1)[:, None]
+    out = {}
+    if case["kind"] == "loss":
+        top = x.max(dim=1).values
+        part = torch.log(torch.exp(x - top[:, None]).sum(dim=1))
+        lse = top + part
+        xt = x.gather(1, tc)[:, 0]
+        loss = (top - xt) + part + z * lse * lse
+        if e:
+            loss = loss + e * (xt - x.sum(dim=1) / V)
+        out["loss"], out["lse"] = loss * ok, lse * ok
+        s = st["scale"] * ok
+    else:
+        lse = st["lse"]
+        s = st["scale"] * st["dloss"] * ok
+    p = torch.exp(x - lse[:, None]) * (s * (1.0 + 2.0 * z * lse))[:, None]
+    if e:
+        p = p - (s * (e / V))[:, None]
+    p.scatter_add_(1, tc, (-(1.0 - e) * s)[:, None])
+    out["dx"] = p.to(st["x"].dtype)
+    return out
+
+
+def _philox(n, c2, c3, seed):
+    """[n, 4] words (int64) of Philox4x32-10 at counters (0 .. n-1, c2, c3); the
+    64-bit products are formed from 16-bit halves."""
+    M = 0xFFFFFFFF
+    i = torch.arange(n, dtype=I64, device="cuda")
+    c = [i & M, i >> 32, torch.full_like(i, c2), torch.full_like(i, c3)]
+    k0, k1 = seed & M, seed >> 32 & M
+
+    def mul(a, x):
+        lo, hi = a * (x & 0xFFFF), a * (x >> 16)
+        t = hi + (lo >> 16)
+        return (t >> 16) & M, ((t & 0xFFFF) << 16) | (lo & 0xFFFF)
+
+    for _ in range(10):
+        h0, l0 = mul(0xD2511F53, c[0])
+        h1, l1 = mul(0xCD9E8D57, c[2])
+        c = [h1 ^ c[1] ^ k0, l1, h0 ^ c[3] ^ k1, l0]
+        k0, k1 = (k0 + 0x9E3779B9) & M, (k1 + 0xBB67AE85) & M
+    return torch.stack(c, dim=1)
+
+
+def _pow2(k):
+    """2^k of int32 k in [-126, 127]."""
+    return ((k + 127) << 23).view(F32)
+
+
+def _block_exp(x):
+    """Exponents k of blocks of 32, with max |x| <= 448 2^k: int32 [n / 32]."""
+    a = x.abs().reshape(-1, 32).max(dim=1).values.view(torch.int32)
+    return ((a + 0x1FFFFF) // 0x800000 - 135).clamp(min=-126)
+
+
+def _round8(x, bits, positive):
+    """fp32 x (whole blocks) to e4m3 under a block's power of two, up with the
+    probability of what is cut off: (codes, exponent bytes)."""
+    k = _block_exp(x)
+    y = x.abs() * _pow2(-k).repeat_interleave(32)
+    low = (y < 2.0 ** -6) * 2.0 ** -6  # steps of 2^-9 below the normal numbers
+    t = ((y + low).view(torch.int32) + (bits << 4).to(torch.int32)) & -0x100000
+    t = t.view(F32) - low
+    if positive:
+        t = torch.where((x > 0) & (t == 0), 2.0 ** -9, t)
+    return torch.where(x < 0, -t, t).to(torch.float8_e4m3fn), (k + 127).to(torch.uint8)
+
+
+def _value8(code, exp):
+    return code.to(F32) * _pow2(exp.to(torch.int32) - 127).repeat_interleave(32)
+
+
+def _e8m0(b):
+    """Exponent bytes as the powers of two that they stand for."""
+    return b.view(torch.float8_e8m0fnu)
+
+
+def _state(st):
+    case = st["case"]
+    out = {"master": st["master"], "m": st["m"], "v": st["v"]}
+    if case["param"] == "bf16":
+        out["param"] = st["param"]
+    if case["state"] == "e4m3":
+        out["ms"], out["vs"] = _e8m0(st["ms"]), _e8m0(st["vs"])
+    return out
+
+
+def _plain_adamw(st):
+    case = st["case"]
+    t = case["step"]
+    g = st["g"].to(F32) * st["norm"][1]
+    if case["state"] == "f32":
+        m, v = st["m"], st["v"]
+    else:
+        m, r = _value8(st["m"], st["ms"]), _value8(st["v"], st["vs"])
+        v = r * r
+    m = B1 * m + (1.0 - B1) * g
+    v = B2 * v + (1.0 - B2) * (g * g)
+    r = torch.sqrt(v)
+    p = st["master"]
+    step = (m * (1.0 / (1.0 - B1 ** t))) / (r * (1.0 / math.sqrt(1.0 - B2 ** t)) + EPS)
+    p.sub_(LR * (step + st["wd"] * p))
+    if case["state"] == "f32":
+        st["m"].copy_(m)
+        st["v"].copy_(v)
+    else:
+        w = _philox(m.numel() // 4, t & 0xFFFFFFFF, t >> 32, st["seed"]).reshape(-1)
+        for (name, exp), x, b in ((("m", "ms"), m, w & 0xFFFF), (("v", "vs"), r, w >> 16)):
+            code, k = _round8(x, b, name == "v")
+            st[name].copy_(code)
+            st[exp].copy_(k)
+    if case["param"] == "bf16":
+        st["param"].copy_(p)
+    return _state(st)
+
+
+def _run_plain(st):
+    kind = st["case"]["kind"]
+    if kind == "rotary":
+        return _plain_rotary(st)
+    if kind in ("loss", "loss_bwd"):
+        return _plain_loss(st)
+    if kind == "norm":
+        n = torch.sqrt(st["g"].to(F64).square().sum())
+        return {"norm": torch.stack([n, (st["max_norm"] / n).clamp(max=1.0)]).to(F32)}
+    return _plain_adamw(st)
+
+
+# ------------------------------------------------------------------- the library's calls
+def _plan(st):
+    """What a program sets up once: the descriptions of its tensors, the table of
+    angles, the list of its parameters and the workspace."""
+    from paper_2503_10377_amd import sppo as L
+
+    case = st["case"]
+    kind = case["kind"]
+    st["L"] = L
+    if kind == "rotary":
+        freqs, amp = L.sppo_rotary_freqs(case["rot"], 10000.0, case["scaling"], factor=8.0, original_len=4096)
+        st["table"] = torch.from_numpy(np.array(freqs, dtype=np.uint64).view(np.int64)).cuda()
+        st["spec"] = L.rotary(case["rot"], st["table"], case["layout"], amp, row0=case["row0"], positions=st["pos"],
+                              id_type=case["pos"] if case["pos"] != "row0" else "i64")
+        D = case["D"]
+        st["both"] = L.rotary_tensors([
+            L.rotary_tensor(h, D, st[n], st[n].stride(0), D, st["y" + n], h * D, D, dtype=dt)
+            for n, h, dt in (("q", case["hq"], case["dtype"]), ("k", case["hk"], case["kdtype"]))])
+    elif kind in ("loss", "loss_bwd"):
+        st["spec"] = L.cross_entropy(case["V"], case["dtype"], case["ids"], label_smoothing=case["smooth"],
+                                     z_loss=case["z"], scale=st["scale"])
+    else:
+        places, _ = _places(case)
+        tensors = []
+        for at, n, d in places:
+            kw = dict(grad=st["g"][at:], grad_dtype=case["grad"])
+            if kind == "adamw":
+                kw.update(m=st["m"][at:], v=st["v"][at:], weight_decay=DECAY * d, param_dtype=case["param"])
+                if case["param"] == "bf16":
+                    kw.update(param=st["param"][at:], master=st["master"][at:])
+                else:
+                    kw.update(param=st["master"][at:])
+                if case["state"] == "e4m3":
+                    kw.update(m_scale=st["ms"][at // 32:], v_scale=st["vs"][at // 32:])
+            tensors.append(L.opt_tensor(n, **kw))
+        st["list"] = L.opt_list(tensors, case["state"] if kind == "adamw" else "none")
+        if kind == "norm":
+            st["ws_bytes"] = L.sppo_grad_norm_workspace(st["list"])
+            st["ws"] = torch.empty(st["ws_bytes"], dtype=torch.uint8, device="cuda")
+        else:
+            st["spec"] = L.adamw(LR, B1, B2, EPS, case["step"], norm=st["norm"], seed=st["seed"])
+
+
+def _run_own(st):
+    case, L = st["case"], st["L"]
+    kind = case["kind"]
+    if kind == "rotary":
+        L.sppo_rotary_apply(st["spec"], case["rows"], st["both"], inverse=case["inverse"])
+        return {"q": st["yq"], "k": st["yk"]}
+    if kind == "loss":
+        L.sppo_cross_entropy(st["spec"], case["rows"], st["x"], _ld(case), st["t"], st["loss"], st["lse"], st["dx"],
+                             _ld(case))
+        return {"loss": st["loss"], "lse": st["lse"], "dx": st["dx"]}
+    if kind == "loss_bwd":
+        L.sppo_cross_entropy_bwd(st["spec"], case["rows"], st["x"], _ld(case), st["t"], st["lse"], st["dloss"],
+                                 st["dx"], _ld(case))
+        return {"dx": st["dx"]}
+    if kind == "norm":
+        L.sppo_grad_norm(st["list"], st["max_norm"], st["out"], st["ws"], st["ws_bytes"])
+        return {"norm": st["out"]}
+    L.sppo_adamw_step(st["list"], st["spec"])
+    return _state(st)
+
+
+def run(state):
+    return _run_own(state) if own else _run_plain(state)
+
+
+# ------------------------------------------------------------------- work
+def work(case):
+    """Bytes: each input read once, each output written once (the logits of rows
+    without a target are not needed).  Flops: those of the formulas; an
+    exponential or a root counts as one."""
+    kind = case["kind"]
+    if kind == "rotary":
+        el = case["hq"] * SIZE[case["dtype"]] + case["hk"] * SIZE[case["kdtype"]]
+        heads = case["hq"] + case["hk"]
+        return {"bytes": 2 * case["rows"] * case["D"] * el, "flops": 3 * case["rows"] * heads * case["rot"]}
+    if kind in ("loss", "loss_bwd"):
+        n, el = case["rows"] * case["V"], SIZE[case["dtype"]]
+        live = (case["rows"] - case["padded"]) * case["V"]
+        return {"bytes": (n + live) * el + 16 * case["rows"], "flops": live * (7 if kind == "loss" else 4)}
+    n = sum(k for k, _ in _sizes(case))
+    g = SIZE[case["grad"]]
+    if kind == "norm":
+        return {"bytes": n * g, "flops": 2 * n}
+    state = 16 if case["state"] == "f32" else 4 + 0.125
+    return {"bytes": n * (g + 8 + state + (2 if case["param"] == "bf16" else 0)), "flops": 16 * n}
+
+
+# ------------------------------------------------------------------- 64-bit values
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "rotary":
+        return _exact_rotary(case, st)
+    if kind in ("loss", "loss_bwd"):
+        return _exact_loss(case, st)
+    if kind == "norm":
+        n = torch.linalg.vector_norm(st["g"].double())
+        return {"norm": torch.stack([n, torch.minimum(torch.ones_like(n), st["max_norm"] / n)])}
+    return _exact_adamw(case, st)
+
+
+def _exact_rotary(case, st):
+    """As products with complex numbers of length amp; the turns are reduced to
+    a fraction of one before they become an angle."""
+    rows, D, rot = case["rows"], case["D"], case["rot"]
+    ld = np.longdouble
+    pos = np.arange(rows) + case["row0"] if st["pos"] is None else st["pos"].cpu().numpy()
+    f, amp = _inv_freq(case)
+    turns = pos.astype(ld)[:, None] * (f.astype(ld) / (2 * ld("3.14159265358979323846264338327950288")))
+    turns = (turns - np.floor(turns)).astype(np.float64) * (-1.0 if case["inverse"] else 1.0)
+    w = torch.polar(torch.tensor(amp, dtype=F64), torch.from_numpy(2 * np.pi * turns)).cuda()[:, None, :]
+    out = {}
+    for n, h in (("q", case["hq"]), ("k", case["hk"])):
+        y = st[n].double().reshape(rows, h, D).contiguous()
+        if case["layout"] == "half":
+            c = torch.complex(y[..., :rot // 2].contiguous(), y[..., rot // 2:rot].contiguous()) * w
+            y[..., :rot] = torch.cat([c.real, c.imag], dim=-1)
+        else:
+            c = torch.complex(y[..., 0:rot:2].contiguous(), y[..., 1:rot:2].contiguous()) * w
+            y[..., :rot] = torch.stack([c.real, c.imag], dim=-1).reshape(rows, h, rot)
+        out[n] = y.reshape(rows, h * D)
+    return out
+
+
+def _exact_loss(case, st):
+    rows, V, e, z = case["rows"], case["V"], case["smooth"], case["z"]
+    dx = torch.empty(rows, V, dtype=F64, device="cuda")
+    loss, lses = torch.zeros(rows, dtype=F64, device="cuda"), torch.zeros(rows, dtype=F64, device="cuda")
+    for at in range(0, rows, 1024):
+        r = slice(at, min(rows, at + 1024))
+        x, t = st["x"][r].double(), st["t"][r].long()
+        ok = (t >= 0) & (t < V)
+        lse = torch.logsumexp(x, dim=1) if case["kind"] == "loss" else st["lse"][r].double()
+        q = torch.full((len(t), V), e / V, dtype=F64, device="cuda")  # what the target's distribution is
+        q[ok, t[ok]] += 1.0 - e
+        s = st["scale"] if case["kind"] == "loss" else (st["scale"] * st["dloss"][r].double())[:, None]
+        d = s * ((1.0 + 2.0 * z * lse[:, None]) * torch.exp(x - lse[:, None]) - q)
+        dx[r] = torch.where(ok[:, None], d, torch.zeros((), dtype=F64, device="cuda"))
+        if case["kind"] == "loss":
+            seen = torch.where(q > 0, q * x, torch.zeros((), dtype=F64, device="cuda")).sum(dim=1)
+            loss[r] = torch.where(ok, lse - seen + z * lse ** 2, torch.zeros_like(lse))
+            lses[r] = torch.where(ok, lse, torch.zeros_like(lse))
+    return {"loss": loss, "lse": lses, "dx": dx} if case["kind"] == "loss" else {"dx": dx}
+
+
+def _draws64(n, t, seed):
+    """uint32 words [n] of Philox4x32-10, four to a counter, in NumPy."""
+    mask, sh = np.uint64(0xFFFFFFFF), np.uint64(32)
+    x0 = np.arange(n // 4, dtype=np.uint64)
+    x1, x2, x3 = x0 >> sh, np.full_like(x0, t & 0xFFFFFFFF), np.full_like(x0, t >> 32)
+    x0 = x0 & mask
+    ka, kb = seed & 0xFFFFFFFF, seed >> 32
+    for _ in range(10):
+        pa, pb = x0 * np.uint64(0xD2511F53), x2 * np.uint64(0xCD9E8D57)
+        x0, x1, x2, x3 = (pb >> sh) ^ x1 ^ np.uint64(ka), pb & mask, (pa >> sh) ^ x3 ^ np.uint64(kb), pa & mask
+        ka, kb = (ka + 0x9E3779B9) % 2 ** 32, (kb + 0xBB67AE85) % 2 ** 32
+    return np.stack([x0, x1, x2, x3], axis=1).reshape(-1).astype(np.int64)
+
+
+def _exact_round8(x, u, positive):
+    """Values under the blocks' powers of two, and those powers, of fp64 x."""
+    a = x.abs().reshape(-1, 32).amax(dim=1)
+    k = torch.ceil(torch.log2(a.clamp(min=2.0 ** -130) / 448.0)).clamp(min=-126)
+    y = x.abs() / torch.exp2(k).repeat_interleave(32)
+    e = torch.floor(torch.log2(y.clamp(min=2.0 ** -6)))
+    q = torch.exp2(e - 3)
+    y = torch.floor(y / q + u / 65536.0) * q
+    if positive:
+        y = torch.where((x > 0) & (y == 0), torch.full_like(y, 2.0 ** -9), y)
+    return y * torch.sign(x), torch.exp2(k)
+
+
+def _exact_adamw(case, st):
+    t = case["step"]
+    g = st["g"].double() * float(st["norm"][1])
+    m, v, p = st["m"].to(F32).double(), st["v"].to(F32).double(), st["master"].double()
+    if case["state"] == "e4m3":
+        two = torch.tensor(2.0, dtype=F64, device="cuda")
+        m = m * (two ** (st["ms"].double() - 127)).repeat_interleave(32)
+        v = (v * (two ** (st["vs"].double() - 127)).repeat_interleave(32)) ** 2
+    m = m + (1.0 - B1) * (g - m)
+    v = v + (1.0 - B2) * (g ** 2 - v)
+    mh, vh = m / (1.0 - B1 ** t), v / (1.0 - B2 ** t)
+    p = p - LR * mh / (vh ** 0.5 + EPS) - LR * st["wd"].double() * p
+    out = {"master": p, "m": m, "v": v}
+    if case["param"] == "bf16":
+        out["param"] = p
+    if case["state"] == "e4m3":
+        w = torch.from_numpy(_draws64(m.numel(), t, st["seed"])).cuda()
+        out["m"], out["ms"] = _exact_round8(m, (w & 0xFFFF).double(), False)
+        out["v"], out["vs"] = _exact_round8(v ** 0.5, (w >> 16).double(), True)
+    return out
