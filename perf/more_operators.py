@@ -431,6 +431,8 @@ def _plan(st):
     elif kind in ("loss", "loss_bwd"):
         st["spec"] = L.cross_entropy(case["V"], case["dtype"], case["ids"], label_smoothing=case["smooth"],
                                      z_loss=case["z"], scale=st["scale"])
+        st["ws_bytes"] = L.sppo_cross_entropy_workspace(st["spec"], case["rows"])
+        st["ws"] = torch.empty(max(16, st["ws_bytes"]), dtype=torch.uint8, device="cuda")
     else:
         places, _ = _places(case)
         tensors = []
@@ -461,7 +463,7 @@ def _run_own(st):
         return {"q": st["yq"], "k": st["yk"]}
     if kind == "loss":
         L.sppo_cross_entropy(st["spec"], case["rows"], st["x"], _ld(case), st["t"], st["loss"], st["lse"], st["dx"],
-                             _ld(case))
+                             _ld(case), st["ws"], st["ws_bytes"])
         return {"loss": st["loss"], "lse": st["lse"], "dx": st["dx"]}
     if kind == "loss_bwd":
         L.sppo_cross_entropy_bwd(st["spec"], case["rows"], st["x"], _ld(case), st["t"], st["lse"], st["dloss"],
