@@ -604,6 +604,194 @@ sppo_status sppo_embedding_bwd(sppo_dtype dtype, sppo_id_type id_type, int64_t r
                                float* dtable, int64_t lddt, int32_t accumulate, void* workspace,
                                size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * What closes a training step: positions in the attention, the loss, and the
+ * update of the parameters.  Context-free calls under the rules of the ones
+ * above: validated on the host, nothing enqueued on failure, no allocation,
+ * no synchronisation, the message in sppo_last_error(NULL).
+ * ---------------------------------------------------------------------- */
+
+/* Rotary positions.  The first `rot` elements of a head are rot / 2 pairs:
+ * (j, j + rot/2) in the HALF layout, (2j, 2j + 1) in INTERLEAVED.  A pair
+ * (a, b) of a row at position t becomes
+ *   amp (a cos w - b sin w,  b cos w + a sin w),  w = 2 pi t freqs[j] / 2^64
+ * (inverse: -w, which with the same amp is the gradient); the elements from
+ * rot on are copied.  freqs (device, [rot/2]) are fractions of a turn per
+ * position in units of 2^-64, so that angles are exact modulo a turn: a
+ * frequency that is off by 2^-63 turns puts position t off by |t| 2^-63.
+ * positions: device [rows] of id_type, any values, or NULL for row0 + r.
+ * The arithmetic is fp32, one rounding to the output's type. */
+typedef enum { SPPO_ROTARY_HALF = 0, SPPO_ROTARY_INTERLEAVED = 1 } sppo_rotary_layout;
+typedef struct {
+  int32_t rot;              /* a multiple of 8, 8 <= rot                    */
+  sppo_rotary_layout layout;
+  const uint64_t* freqs;
+  float amp;                /* finite                                       */
+  sppo_id_type id_type;     /* of positions                                 */
+  const void* positions;
+  int64_t row0;
+} sppo_rotary;
+
+/* [rows, heads, head_dim] in memory: element (r, h, d) at r ld + h hs + d.
+ * head_dim a multiple of 8, rot <= head_dim <= 1024; ld and hs multiples of 8,
+ * with rows and heads apart from each other (hs >= head_dim and ld >= (heads
+ * - 1) hs + head_dim, or ld >= head_dim and hs >= (rows - 1) ld + head_dim);
+ * pointers 16-byte aligned.  y may be x with the same ld and hs; no other
+ * overlap, also not between tensors of a call. */
+typedef struct {
+  sppo_dtype dtype;
+  int32_t heads, head_dim;
+  const void* x;
+  int64_t ldx, hsx;
+  void* y;
+  int64_t ldy, hsy;
+} sppo_rotary_tensor;
+
+/* 1 to 4 tensors (queries and keys, or their gradients) of the same rows in
+ * one launch.  tensors: host array.  rows 0: nothing is done. */
+sppo_status sppo_rotary_apply(const sppo_rotary* spec, int64_t rows, int32_t inverse, int32_t n_tensors,
+                              const sppo_rotary_tensor* tensors, void* stream);
+
+/* The table of a rotary spec (a pure host function; freqs: host [rot/2], to be
+ * copied to the device) and its amplitude.  With f_j = base^(-2j/rot), L =
+ * original_len, s = factor:
+ *   NONE    f_j, amp 1
+ *   LINEAR  f_j / s, amp 1 (positions interpolated)
+ *   NTK     f_j with base s^(rot / (rot - 2)), amp 1
+ *   YARN    c f_j + (1 - c) f_j / s, c = clamp((L f_j / (2 pi) - beta_slow) /
+ *           (beta_fast - beta_slow), 0, 1), amp 0.1 ln s + 1 (Peng, Quesnelle,
+ *           Fan, Shippole, "YaRN", 2023)
+ *   GIVEN   inv_freq[j] (host [rot/2], finite), amp 1
+ * base > 1 (but for GIVEN), finite; s >= 1; YARN: L >= 1, beta_fast > beta_slow. */
+typedef enum {
+  SPPO_ROPE_NONE = 0,
+  SPPO_ROPE_LINEAR = 1,
+  SPPO_ROPE_NTK = 2,
+  SPPO_ROPE_YARN = 3,
+  SPPO_ROPE_GIVEN = 4
+} sppo_rope_scaling;
+typedef struct {
+  sppo_rope_scaling kind;
+  double base, factor;
+  double original_len, beta_fast, beta_slow;
+  const double* inv_freq;
+} sppo_rope;
+sppo_status sppo_rotary_freqs(int32_t rot, const sppo_rope* rope, uint64_t* freqs, float* amp);
+
+/* Cross-entropy of rows of logits x over V classes, and its gradient:
+ *   lse = log sum_c exp(x_c)
+ *   loss = lse - (1 - e) x_t - (e / V) sum_c x_c + z lse^2
+ *   dx_c = w ((1 + 2 z lse) exp(x_c - lse) - (1 - e) [c = t] - e / V)
+ * with t the row's target, e = label_smoothing, z = z_loss, w = scale, times
+ * *scale_dev (device fp32) where that is not NULL.  A row whose target is
+ * outside [0, V) (padding) has loss, lse and gradient zero whatever its logits
+ * hold.  Otherwise IEEE arithmetic holds: logits of -inf (masked classes) have
+ * probability zero, a target at one has an infinite loss, and a row of nothing
+ * but -inf has lse -inf and loss and gradient NaN.  With e > 0 a single -inf
+ * makes the loss +inf.  Everything between logits and outputs is fp32. */
+typedef struct {
+  int64_t V;                /* 1 <= V < 2^31 (UNSUPPORTED above)            */
+  sppo_dtype dtype;         /* of logits and dlogits                        */
+  sppo_id_type id_type;     /* of targets                                   */
+  float label_smoothing;    /* 0 <= e <= 1                                  */
+  float z_loss;             /* finite, >= 0                                 */
+  float scale;              /* finite                                       */
+  const float* scale_dev;
+} sppo_ce;
+
+/* Loss and gradient in one call.  logits [rows, V] with row stride ld (V <=
+ * ld, a multiple of 8, 16-byte aligned; V itself is any number), targets
+ * [rows], loss and lse fp32 [rows] (lse may be NULL), dlogits as logits, or
+ * NULL for the loss alone; it may be logits (with the same stride).  Columns
+ * from V on are neither used nor written.  rows 0: nothing is done; rows <
+ * 2^31.  workspace: sppo_cross_entropy_workspace bytes (0, and NULL, where rows
+ * are many or short; also 0 for an invalid ce), 16-byte aligned. */
+size_t sppo_cross_entropy_workspace(const sppo_ce* ce, int64_t rows);
+sppo_status sppo_cross_entropy(const sppo_ce* ce, int64_t rows, const void* logits, int64_t ld, const void* targets,
+                               float* loss, float* lse, void* dlogits, int64_t lddl, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* The gradient alone, from a kept lse; dloss: fp32 [rows], a factor beside the
+ * scale, or NULL.  dlogits may be logits (with the same stride). */
+sppo_status sppo_cross_entropy_bwd(const sppo_ce* ce, int64_t rows, const void* logits, int64_t ld,
+                                   const void* targets, const float* lse, const float* dloss, void* dlogits,
+                                   int64_t lddl, void* stream);
+
+/* The parameters of an update, as one list for all its calls.  State:
+ *   NONE  gradients only (for the norm)
+ *   F32   m and v fp32 [n]
+ *   E4M3  m and r = sqrt(v) in 8 bits: OCP e4m3 codes [n] under one power of two
+ *         2^(b - 127) for 32 elements, b in m_scale, v_scale [ceil(n/32)] (all
+ *         zeros is the state zero).  b is the least, from 1 on, with which the
+ *         block's largest magnitude is at most 448 2^(b - 127).
+ * A bf16 parameter has its fp32 master (which is what is updated, the parameter
+ * its rounding); an fp32 parameter has none.  Pointers are aligned to their
+ * element, with E4M3 to 16 bytes (the scales to 1).  n 0: skipped. */
+typedef enum { SPPO_STATE_NONE = 0, SPPO_STATE_F32 = 1, SPPO_STATE_E4M3 = 2 } sppo_opt_state;
+typedef struct {
+  int64_t n;
+  void* param;
+  const void* grad;
+  float* master;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  sppo_dtype param_dtype, grad_dtype;
+  float lr_scale;           /* a factor of the learning rate, finite        */
+  float weight_decay;       /* finite                                       */
+} sppo_opt_tensor;
+
+/* A list is made on the host (pure host functions), its table copied by the
+ * caller to device memory (16-byte aligned) whose address it writes into
+ * `table`; list and table live as long as their calls run.  INVALID_ARG where
+ * a buffer that is written overlaps another of the list (a tensor listed twice;
+ * gradients may be shared).  At most 2^20 tensors and 2^31 - 1 tiles of 4096
+ * elements (UNSUPPORTED above). */
+typedef struct {
+  const void* table;
+  int64_t tiles;
+  int32_t n_tensors;
+  sppo_opt_state state;
+} sppo_opt_list;
+size_t sppo_opt_list_bytes(int32_t n_tensors, const sppo_opt_tensor* tensors);
+sppo_status sppo_opt_list_make(int32_t n_tensors, const sppo_opt_tensor* tensors, sppo_opt_state state,
+                               void* host_table, size_t bytes, sppo_opt_list* list);
+
+/* out (device fp32 [2]) = { norm, min(1, max_norm / norm) }, norm = the root of
+ * the sum of the squares of all gradients, summed in fp64 in a fixed order (the
+ * same bits every time).  max_norm > 0; infinity: the factor is 1.  A norm of
+ * infinity or NaN has the factor 0.  steps: NULL, or a device int64 that is
+ * increased by one unless the norm is infinite or NaN.  workspace:
+ * sppo_grad_norm_workspace bytes, 16-byte aligned. */
+size_t sppo_grad_norm_workspace(const sppo_opt_list* list);
+sppo_status sppo_grad_norm(const sppo_opt_list* list, float max_norm, float* out, int64_t* steps, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* One AdamW update of the list's parameters:
+ *   g' = f g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
+ *   p -= lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)
+ * t = step, plus *step_dev where that is not NULL (t >= 1, checked only where
+ * the host knows it; below 1 on the device counts as 1); f = norm[1] and nothing
+ * at all is changed where norm[0] is infinite or NaN (norm: a grad_norm's out,
+ * NULL: f = 1); lr is multiplied by *lr_dev (device fp32) where that is not
+ * NULL, and by the tensor's lr_scale.  Arithmetic is fp32.
+ * With E4M3 the new m and r are rounded to the neighbour above with the
+ * probability of what lies between (in 2^-16), and a positive r never to zero:
+ * element e of a tensor whose blocks of 32 start at the list's block B takes
+ * word e % 4 of Philox4x32-10 (as the dropout's) with counter (8 B + e / 4 low,
+ * high, t low, high) and key seed, its low half for m, its high half for r.
+ * Values that are infinite or NaN are kept as NaN. */
+typedef struct {
+  double lr, beta1, beta2, eps;  /* finite; 0 <= beta < 1; eps >= 0         */
+  int64_t step;
+  const int64_t* step_dev;
+  const float* norm;
+  const float* lr_dev;
+  uint64_t seed;
+} sppo_adamw;
+sppo_status sppo_adamw_step(const sppo_opt_list* list, const sppo_adamw* adamw, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -323,4 +323,101 @@ size_t embedding_workspace(int64_t rows, int H);
 hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t stream);
 hipError_t launch_embedding_bwd(const EmbedArgs& a, hipStream_t stream);
 
+// Rotary positions of 1 to 4 tensors (rotary.hip).  A wave takes 64 kRotaryUnroll
+// (or 64) consecutive items of one row of one tensor, an item being a group of
+// rotated pairs or of copied elements of one head.
+constexpr int kRotaryMaxTensors = 4, kRotaryMaxDim = 1024;
+struct RotaryTensor {
+  const void* x;
+  void* y;
+  int64_t ldx, hsx, ldy, hsy;
+  int heads, D, f32;
+  // Set by the launcher: items of a head and of a row, the first wave of a row that takes this tensor.
+  int per, items, chunk0;
+  FastDiv per_head;  // division by per
+};
+struct RotaryArgs {
+  int64_t rows;
+  int rot, half, n;
+  const uint64_t* freqs;
+  float amp, sign;    // sign -1: the inverse
+  const void* pos;
+  int id64;
+  int64_t row0;
+  RotaryTensor t[kRotaryMaxTensors];
+};
+hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
+
+// Cross-entropy (cross_entropy.hip): loss, lse and gradient from the logits, or
+// with `lse_in` the gradient alone.
+struct CeArgs {
+  int64_t rows, V;
+  const void* x;
+  int64_t ldx;
+  const void* targets;
+  int id64;
+  float smooth, z, scale;
+  const float* scale_dev;
+  float* loss;
+  float* lse;
+  const float* lse_in;
+  const float* dloss;
+  void* dx;  // NULL: no gradient
+  int64_t lddx;
+  void* workspace;
+  int f32;
+};
+size_t cross_entropy_workspace(int64_t rows, int64_t V, bool f32);
+hipError_t launch_cross_entropy(const CeArgs& a, hipStream_t stream);
+hipError_t launch_cross_entropy_bwd(const CeArgs& a, hipStream_t stream);
+
+// The table of a parameter list, in device memory: n descriptions, then `tiles`
+// entries (tensor, tile of kOptTile elements in it).
+constexpr int kOptTile = 4096;
+enum { kOptVector = 1, kOptParamBf16 = 2, kOptGradBf16 = 4 };
+struct OptDesc {
+  void* param;
+  const void* grad;
+  float* master;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  int64_t n;
+  int64_t block0;  // blocks of 32 elements in the tensors before it
+  float lr_scale, weight_decay;
+  int32_t flags, pad[3];
+};
+static_assert(sizeof(OptDesc) == 96, "");
+struct OptTile {
+  uint32_t tensor, tile;
+};
+struct OptTable {
+  const OptDesc* desc;
+  const OptTile* tile;
+  int64_t tiles;
+};
+// Sum of squares (optimizer.hip) through `part`, kNormBlocks doubles.
+constexpr int kNormBlocks = 2048;
+hipError_t launch_grad_norm(const OptTable& t, float max_norm, float* out, int64_t* steps, double* part,
+                            hipStream_t stream);
+struct AdamArgs {
+  double beta1, beta2;
+  float lr, eps;
+  float im, ir;  // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t) where there is no step_dev
+  int64_t step;
+  const int64_t* step_dev;
+  const float* norm;
+  const float* lr_dev;
+  uint64_t seed;
+};
+// beta^t of beta in [0, 1), t >= 1, by squares: off by t 2^-53 of itself.
+__host__ __device__ inline double beta_power(double b, int64_t t) {
+  double r = 1.0;
+  for (uint64_t k = (uint64_t)t; k; k >>= 1, b *= b)
+    if (k & 1) r *= b;
+  return r;
+}
+hipError_t launch_adamw(const OptTable& t, int state, const AdamArgs& a, hipStream_t stream);
+
 }  // namespace sppo

@@ -113,6 +113,96 @@ class sppo_block_norm_grads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("post_gamma", "post_beta", "gate", "pre_gamma", "pre_beta")]
 
 
+class sppo_rotary(ctypes.Structure):
+    _fields_ = [
+        ("rot", ctypes.c_int32),
+        ("layout", ctypes.c_int),
+        ("freqs", ctypes.c_void_p),
+        ("amp", ctypes.c_float),
+        ("id_type", ctypes.c_int),
+        ("positions", ctypes.c_void_p),
+        ("row0", ctypes.c_int64),
+    ]
+
+
+class sppo_rotary_tensor(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int),
+        ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("x", ctypes.c_void_p),
+        ("ldx", ctypes.c_int64),
+        ("hsx", ctypes.c_int64),
+        ("y", ctypes.c_void_p),
+        ("ldy", ctypes.c_int64),
+        ("hsy", ctypes.c_int64),
+    ]
+
+
+class sppo_rope(ctypes.Structure):
+    _fields_ = [
+        ("kind", ctypes.c_int),
+        ("base", ctypes.c_double),
+        ("factor", ctypes.c_double),
+        ("original_len", ctypes.c_double),
+        ("beta_fast", ctypes.c_double),
+        ("beta_slow", ctypes.c_double),
+        ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+    ]
+
+
+class sppo_ce(ctypes.Structure):
+    _fields_ = [
+        ("V", ctypes.c_int64),
+        ("dtype", ctypes.c_int),
+        ("id_type", ctypes.c_int),
+        ("label_smoothing", ctypes.c_float),
+        ("z_loss", ctypes.c_float),
+        ("scale", ctypes.c_float),
+        ("scale_dev", ctypes.c_void_p),
+    ]
+
+
+class sppo_opt_tensor(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64),
+        ("param", ctypes.c_void_p),
+        ("grad", ctypes.c_void_p),
+        ("master", ctypes.c_void_p),
+        ("m", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("m_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("param_dtype", ctypes.c_int),
+        ("grad_dtype", ctypes.c_int),
+        ("lr_scale", ctypes.c_float),
+        ("weight_decay", ctypes.c_float),
+    ]
+
+
+class sppo_opt_list(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("tiles", ctypes.c_int64),
+        ("n_tensors", ctypes.c_int32),
+        ("state", ctypes.c_int),
+    ]
+
+
+class sppo_adamw(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("step_dev", ctypes.c_void_p),
+        ("norm", ctypes.c_void_p),
+        ("lr_dev", ctypes.c_void_p),
+        ("seed", ctypes.c_uint64),
+    ]
+
+
 KERNELS = ("fwd", "bwd_pre", "bwd_dkdv", "bwd_dq")
 
 
@@ -201,6 +291,22 @@ def lib() -> ctypes.CDLL:
             "sppo_embedding_bwd": ([ctypes.c_int, ctypes.c_int, ctypes.c_int64, I32, ctypes.c_int64, VP, VP,
                                     ctypes.c_int64, ctypes.c_float, ctypes.POINTER(sppo_drop), VP, ctypes.c_int64,
                                     I32, VP, ctypes.c_size_t, VP], ctypes.c_int),
+            "sppo_rotary_apply": ([ctypes.POINTER(sppo_rotary), ctypes.c_int64, I32, I32,
+                                   ctypes.POINTER(sppo_rotary_tensor), VP], ctypes.c_int),
+            "sppo_rotary_freqs": ([I32, ctypes.POINTER(sppo_rope), ctypes.POINTER(ctypes.c_uint64),
+                                   ctypes.POINTER(ctypes.c_float)], ctypes.c_int),
+            "sppo_cross_entropy_workspace": ([ctypes.POINTER(sppo_ce), ctypes.c_int64], ctypes.c_size_t),
+            "sppo_cross_entropy": ([ctypes.POINTER(sppo_ce), ctypes.c_int64, VP, ctypes.c_int64, VP, VP, VP, VP,
+                                    ctypes.c_int64, VP, ctypes.c_size_t, VP], ctypes.c_int),
+            "sppo_cross_entropy_bwd": ([ctypes.POINTER(sppo_ce), ctypes.c_int64, VP, ctypes.c_int64, VP, VP, VP, VP,
+                                        ctypes.c_int64, VP], ctypes.c_int),
+            "sppo_opt_list_bytes": ([I32, ctypes.POINTER(sppo_opt_tensor)], ctypes.c_size_t),
+            "sppo_opt_list_make": ([I32, ctypes.POINTER(sppo_opt_tensor), ctypes.c_int, VP, ctypes.c_size_t,
+                                    ctypes.POINTER(sppo_opt_list)], ctypes.c_int),
+            "sppo_grad_norm_workspace": ([ctypes.POINTER(sppo_opt_list)], ctypes.c_size_t),
+            "sppo_grad_norm": ([ctypes.POINTER(sppo_opt_list), ctypes.c_float, VP, VP, VP, ctypes.c_size_t, VP],
+                               ctypes.c_int),
+            "sppo_adamw_step": ([ctypes.POINTER(sppo_opt_list), ctypes.POINTER(sppo_adamw), VP], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -599,3 +705,119 @@ def sppo_embedding_bwd(rows, H, V, ids, dy, lddy, scale, drop, dtable, lddt, wor
     _context_free(lib().sppo_embedding_bwd(DTYPES.get(dtype, dtype), ID_TYPES.get(id_type, id_type), rows, H, V,
                                            _ptr(ids), _ptr(dy), lddy, scale, _ref(drop), _ptr(dtable), lddt,
                                            int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+# ------------------------------------------------------ closing a training step
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "given": 4}
+OPT_STATES = {"none": 0, "f32": 1, "e4m3": 2}
+
+
+def sppo_rotary_freqs(rot, base=10000.0, scaling="none", factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0,
+                      inv_freq=None):
+    """([rot / 2] integers of a rotary spec's table, to be put on the device as
+    64-bit numbers, and its amplitude)."""
+    n = max(int(rot) // 2, 1)
+    given = None
+    if inv_freq is not None:
+        if len(inv_freq) != int(rot) // 2:
+            raise ValueError("inv_freq needs one value per pair")
+        given = (ctypes.c_double * n)(*[float(f) for f in inv_freq])
+    r = sppo_rope(ROPE_SCALINGS.get(scaling, scaling), base, factor, original_len, beta_fast, beta_slow, given)
+    out, amp = (ctypes.c_uint64 * n)(), ctypes.c_float()
+    _context_free(lib().sppo_rotary_freqs(rot, ctypes.byref(r), out, ctypes.byref(amp)))
+    return list(out), amp.value
+
+
+def rotary(rot, freqs, layout="half", amp=1.0, row0=0, positions=None, id_type="i64") -> sppo_rotary:
+    """The description of a rotary call; freqs: the table as a device tensor.
+    Holds addresses only: the tensors must outlive its use."""
+    return sppo_rotary(rot, ROTARY_LAYOUTS.get(layout, layout), _ptr(freqs), amp, ID_TYPES.get(id_type, id_type),
+                       _ptr(positions), row0)
+
+
+def rotary_tensor(heads, head_dim, x, ldx, hsx, y, ldy, hsy, dtype="bf16") -> sppo_rotary_tensor:
+    return sppo_rotary_tensor(DTYPES.get(dtype, dtype), heads, head_dim, _ptr(x), ldx, hsx, _ptr(y), ldy, hsy)
+
+
+def rotary_tensors(tensors):
+    """The array that a rotary call takes, of rotary_tensor()s."""
+    return (sppo_rotary_tensor * len(tensors))(*tensors)
+
+
+def sppo_rotary_apply(spec, rows, tensors, inverse=0, stream=None):
+    _context_free(lib().sppo_rotary_apply(_ref(spec), rows, int(inverse), len(tensors), tensors, _stream(stream)))
+
+
+def cross_entropy(V, dtype="bf16", id_type="i64", label_smoothing=0.0, z_loss=0.0, scale=1.0,
+                  scale_dev=None) -> sppo_ce:
+    return sppo_ce(V, DTYPES.get(dtype, dtype), ID_TYPES.get(id_type, id_type), label_smoothing, z_loss, scale,
+                   _ptr(scale_dev))
+
+
+def sppo_cross_entropy_workspace(ce, rows) -> int:
+    return int(lib().sppo_cross_entropy_workspace(_ref(ce), rows))
+
+
+def sppo_cross_entropy(ce, rows, logits, ld, targets, loss, lse, dlogits, lddl, workspace=None, workspace_bytes=0,
+                       stream=None):
+    _context_free(lib().sppo_cross_entropy(_ref(ce), rows, _ptr(logits), ld, _ptr(targets), _ptr(loss), _ptr(lse),
+                                           _ptr(dlogits), lddl, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def sppo_cross_entropy_bwd(ce, rows, logits, ld, targets, lse, dloss, dlogits, lddl, stream=None):
+    _context_free(lib().sppo_cross_entropy_bwd(_ref(ce), rows, _ptr(logits), ld, _ptr(targets), _ptr(lse),
+                                               _ptr(dloss), _ptr(dlogits), lddl, _stream(stream)))
+
+
+def opt_tensor(n, grad=None, grad_dtype="f32", param=None, param_dtype="bf16", master=None, m=None, v=None,
+               m_scale=None, v_scale=None, lr_scale=1.0, weight_decay=0.0) -> sppo_opt_tensor:
+    """One parameter of an update.  Holds addresses only: the tensors must
+    outlive the list's use."""
+    return sppo_opt_tensor(n, _ptr(param), _ptr(grad), _ptr(master), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale),
+                           DTYPES.get(param_dtype, param_dtype), DTYPES.get(grad_dtype, grad_dtype), lr_scale,
+                           weight_decay)
+
+
+def sppo_opt_list_bytes(tensors) -> int:
+    arr = (sppo_opt_tensor * len(tensors))(*tensors)
+    return int(lib().sppo_opt_list_bytes(len(tensors), arr))
+
+
+def sppo_opt_list_make(tensors, state, host_table, nbytes) -> sppo_opt_list:
+    """The list of opt_tensor()s, its table written to host memory (an address
+    or a CPU tensor); its device address is the caller's to set."""
+    arr, out = (sppo_opt_tensor * len(tensors))(*tensors), sppo_opt_list()
+    _context_free(lib().sppo_opt_list_make(len(tensors), arr, OPT_STATES.get(state, state), _ptr(host_table), nbytes,
+                                           ctypes.byref(out)))
+    return out
+
+
+def opt_list(tensors, state="f32", device="cuda") -> sppo_opt_list:
+    """The list with its table on the device (a torch tensor that the list keeps)."""
+    import torch
+
+    nbytes = max(sppo_opt_list_bytes(tensors), 16)
+    host = torch.empty(nbytes, dtype=torch.uint8)
+    out = sppo_opt_list_make(tensors, state, host, nbytes)
+    out.device_table = host.to(device)
+    out.table = out.device_table.data_ptr()
+    return out
+
+
+def sppo_grad_norm_workspace(opt) -> int:
+    return int(lib().sppo_grad_norm_workspace(_ref(opt)))
+
+
+def sppo_grad_norm(opt, max_norm, out, workspace, workspace_bytes, steps=None, stream=None):
+    _context_free(lib().sppo_grad_norm(_ref(opt), max_norm, _ptr(out), _ptr(steps), _ptr(workspace), workspace_bytes,
+                                       _stream(stream)))
+
+
+def adamw(lr, beta1=0.9, beta2=0.95, eps=1e-8, step=1, step_dev=None, norm=None, lr_dev=None, seed=0) -> sppo_adamw:
+    """The settings of an update; step is the caller's to count on."""
+    return sppo_adamw(lr, beta1, beta2, eps, step, _ptr(step_dev), _ptr(norm), _ptr(lr_dev), seed)
+
+
+def sppo_adamw_step(opt, spec, stream=None):
+    _context_free(lib().sppo_adamw_step(_ref(opt), _ref(spec), _stream(stream)))
