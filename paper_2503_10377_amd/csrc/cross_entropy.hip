@@ -1,6 +1,8 @@
 // Cross-entropy of rows of logits and its gradient.
 //   lse = log sum exp x,  loss = lse - (1 - e) x_t - e/V sum x + z lse^2
 //   dx = w ((1 + 2 z lse) exp(x - lse) - (1 - e) [c = t] - e/V)
+#include <algorithm>
+
 #include "row_common.h"
 
 namespace sppo {
@@ -37,26 +39,51 @@ struct Running {
   }
 };
 
+// 16 bytes of a row as they lie in memory: N elements.
 template <typename T>
-__device__ __forceinline__ void load_group(const T* x, int64_t g, int64_t V, float fill, float (&f)[8]) {
-  Eight<T> v;
-  v.load(x + 8 * g);
-  v.get(f);
-  const int left = (int)min((int64_t)8, V - 8 * g);
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e >= left) f[e] = fill;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_group(T* y, int64_t g, int64_t V, const float (&f)[8]) {
-  if (8 * g + 8 <= V) {
-    Eight<T>::store(y + 8 * g, f);
-    return;
+struct Piece {
+  static constexpr int N = 16 / (int)sizeof(T);
+  u32x4 v;
+  template <bool PAST>
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t row, int piece) {
+    v = load_row16<PAST>(row, 16 * piece);
   }
+  __device__ __forceinline__ void get(float (&f)[N]) const {
+    if constexpr (N == 8) {
+      unpack8(v, f);
+    } else {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (8 * g + e < V) put_element(y, 8 * g + e, f[e]);
+      for (int e = 0; e < N; ++e) f[e] = __uint_as_float(v[e]);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&f)[N]) {
+    if constexpr (N == 8) {
+      v = pack8(f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = __float_as_uint(f[e]);
+    }
+  }
+  // The elements from `left` on become -inf.
+  __device__ __forceinline__ void cut(int left) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (N == 8) {
+        if (2 * e >= left) v[e] = 0xff80ff80u;
+        else if (2 * e + 1 >= left) v[e] = (v[e] & 0xffffu) | 0xff800000u;
+      } else {
+        if (e >= left) v[e] = 0xff800000u;
+      }
+    }
+  }
+};
+
+// Elements 0 .. left - 1 of a row's last piece.
+template <typename T>
+__device__ __forceinline__ void store_some(T* y, int left, const float (&f)[Piece<T>::N]) {
+#pragma unroll
+  for (int e = 0; e < Piece<T>::N; ++e)
+    if (e < left) put_element(y, e, f[e]);
 }
 
 // lse - (1 - e) x_t - e/V sum x + z lse^2 with lse = base + part, from the
@@ -82,140 +109,363 @@ struct RowGradient {
     sm = w * (a.smooth / (float)a.V);
     hit = w * (1.f - a.smooth);
   }
-  // Of the eight elements of group g; t is the target, -1 where there is none.
-  __device__ __forceinline__ void apply(float (&f)[8], int64_t g, int64_t t) const {
+  // Of the N elements of a piece of which element t, if it is one, is the target.
+  template <int N>
+  __device__ __forceinline__ void apply(float (&f)[N], int t) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = coef * exp_of(f[e] - base) - sm;
-    if (t >> 3 == g) {
+    for (int e = 0; e < N; ++e) f[e] = coef * exp_of(f[e] - base) - sm;
+    if ((uint32_t)t < (uint32_t)N) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] -= (t & 7) == e ? hit : 0.f;
+      for (int e = 0; e < N; ++e) f[e] -= t == e ? hit : 0.f;
     }
   }
 };
 
-constexpr int kThreads = 1024, kWavesCe = kThreads / 64;
+// Maximum over the wave, in every lane.
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  v = fmaxf(v, dpp<0x141>(v));
+  v = fmaxf(v, dpp<0x140>(v));
+  return max_groups(v);
+}
 
-// A row a workgroup: one pass for the maximum and the sum, a second one, from
-// the caches, for the gradient.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void ce_stream_kernel(CeArgs a) {
-  __shared__ float lm[kWavesCe], ls[kWavesCe], lx[kWavesCe];
-  const int64_t row = blockIdx.x;
-  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  T* dx = a.dx ? static_cast<T*>(a.dx) + row * a.lddx : nullptr;
-  const int64_t V = a.V, groups = (V + 7) / 8, t = target_of(a, row);
-  if (t < 0) {
-    if (threadIdx.x == 0) {
-      a.loss[row] = 0.f;
-      if (a.lse) a.lse[row] = 0.f;
-    }
-    const float zero[8] = {};
-    for (int64_t g = threadIdx.x; dx && g < groups; g += kThreads) store_group(dx, g, V, zero);
-    return;
-  }
-  const float xt = element(x, t);
-  Running r{-__builtin_inff(), 0.f};
-  float sum = 0.f;
-  for (int64_t g = threadIdx.x; g < groups; g += kThreads) {
-    float f[8];
-    load_group(x, g, V, -__builtin_inff(), f);
-    float top = f[0], s = 0.f;
+// The wave's Running of its lanes'.
+__device__ __forceinline__ Running wave_join(const Running& r) {
+  const float top = wave_max(r.m);
+  return {top, wave_sum(r.s == 0.f ? 0.f : r.s * exp_of(Running::base(r.m) - Running::base(top)))};
+}
+
+// K pieces of a row (or of n elements of one) a thread, TEAM apart: the maximum
+// and the sum under it, without another trip to memory for the gradient.
+template <typename T, int TEAM, int K>
+struct RowPart {
+  static constexpr int N = Piece<T>::N;
+  Piece<T> v[K];
+  // The last piece is read as a whole (a row's stride is in whole pieces), what
+  // is past n does not count.
+  template <bool PAST>
+  __device__ __forceinline__ void load(const T* x, int lane, int n) {
+    const int pieces = (n + N - 1) / N;
+    const __amdgpu_buffer_rsrc_t row = row_buffer(x, 16 * pieces);
 #pragma unroll
-    for (int e = 1; e < 8; ++e) top = fmaxf(top, f[e]);
-    const float b = Running::base(top);
+    for (int k = 0; k < K; ++k) v[k].template load<PAST>(row, lane + TEAM * k);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += exp_of(f[e] - b);
-    r.join(top, s);
-    if (a.smooth != 0.f) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += 8 * g + e < V ? f[e] : 0.f;
+    for (int k = 0; k < K; ++k) {
+      if (TEAM * (k + 1) < pieces) continue;  // whole for the team
+      const int left = n - N * (lane + TEAM * k);
+      if (left < N) v[k].cut(left);
     }
   }
+  // The compiler is not to keep what it unpacked in a pass for the next one,
+  // which would take twice the registers.
+  __device__ __forceinline__ void repack() {
+    if constexpr (N == 8) {
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) r.join(__shfl_xor(r.m, k), __shfl_xor(r.s, k));
-  sum = wave_sum(sum);
+      for (int k = 0; k < K; ++k) asm volatile("" : "+v"(v[k].v));
+    }
+  }
+  __device__ __forceinline__ Running running() {
+    Running r{-__builtin_inff(), 0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float f[N];
+      v[k].get(f);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) r.m = max3_nc(r.m, f[e], f[e + 1]);
+    }
+    repack();
+    const float b = Running::base(r.m);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float f[N];
+      v[k].get(f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) r.s += exp_of(f[e] - b);
+    }
+    repack();
+    return r;
+  }
+  __device__ __forceinline__ float sum(int lane, int n) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float f[N];
+      v[k].get(f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += N * (lane + TEAM * k) + e < n ? f[e] : 0.f;
+    }
+    repack();
+    return s;
+  }
+  // The gradient; t: the target's place among the n elements, outside: none.
+  template <bool PAST>
+  __device__ __forceinline__ void gradient(const RowGradient& g, T* dx, int lane, int n, int64_t t) {
+    const __amdgpu_buffer_rsrc_t out = row_buffer(dx, 16 * (n / N));  // pieces past it are not stored
+    const int at = t >= 0 && t < n ? (int)t : -N * TEAM * K;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int first = N * (lane + TEAM * k);
+      float f[N];
+      v[k].get(f);
+      g.apply(f, at - first);
+      v[k].set(f);
+      store_row16<PAST>(out, first * (int)sizeof(T), v[k].v);
+      if (TEAM * N * (k + 1) > n && n - first > 0 && n - first < N) store_some(dx + first, n - first, f);
+    }
+  }
+  static __device__ __forceinline__ void zero(T* dx, int lane, int n) {
+    for (int first = N * lane; first < n; first += N * TEAM) {
+      const float f[N] = {};
+      if (n - first < N) store_some(dx + first, n - first, f);
+      else *reinterpret_cast<u32x4*>(dx + first) = u32x4{0, 0, 0, 0};
+    }
+  }
+};
+
+// What the waves of a workgroup found, joined; in every thread.
+template <int WAVES>
+__device__ __forceinline__ void block_join(Running& r, float& sum) {
+  __shared__ float lds[3][WAVES];
   if ((threadIdx.x & 63) == 0) {
-    lm[threadIdx.x >> 6] = r.m;
-    ls[threadIdx.x >> 6] = r.s;
-    lx[threadIdx.x >> 6] = sum;
+    lds[0][threadIdx.x >> 6] = r.m;
+    lds[1][threadIdx.x >> 6] = r.s;
+    lds[2][threadIdx.x >> 6] = sum;
   }
   __syncthreads();
-  r = Running{lm[0], ls[0]};
-  sum = lx[0];
-  for (int k = 1; k < kWavesCe; ++k) {
-    r.join(lm[k], ls[k]);
-    sum += lx[k];
+  r = Running{lds[0][0], lds[1][0]};
+  sum = lds[2][0];
+#pragma unroll
+  for (int k = 1; k < WAVES; ++k) {
+    r.join(lds[0][k], lds[1][k]);
+    sum += lds[2][k];
   }
+}
+
+// loss and lse of a row, the latter returned.
+__device__ __forceinline__ float finish_row(const CeArgs& a, int64_t row, const Running& r, float xt, float sum,
+                                            bool write) {
   const float base = Running::base(r.m), part = logf(r.s), lse = base + part;
-  if (threadIdx.x == 0) {
+  if (write) {
     a.loss[row] = loss_of(a, base, part, xt, sum);
     if (a.lse) a.lse[row] = lse;
   }
-  if (!dx) return;
-  const RowGradient rg(a, r, lse, 1.f);
-  for (int64_t g = threadIdx.x; g < groups; g += kThreads) {
-    float f[8];
-    load_group(x, g, V, -__builtin_inff(), f);
-    rg.apply(f, g, t);
-    store_group(dx, g, V, f);
-  }
+  return lse;
+}
+__device__ __forceinline__ void finish_nothing(const CeArgs& a, int64_t row) {
+  a.loss[row] = 0.f;
+  if (a.lse) a.lse[row] = 0.f;
 }
 
-constexpr int kThreadsBwd = 256, kGroupsBwd = 4;
-
-// The gradient from a kept lse: kGroupsBwd groups a thread.
-template <typename T>
-__global__ __launch_bounds__(kThreadsBwd) void ce_bwd_kernel(CeArgs a, uint32_t parts, FastDiv by_parts) {
-  const uint32_t row = fast_div(blockIdx.x, by_parts), part = blockIdx.x - row * parts;
+// A row a team of threads, which keeps it in registers: one read, one write.
+// PAST: past the caches.
+template <typename T, int TEAM, int K, bool PAST>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void ce_row_kernel(CeArgs a) {
+  constexpr int ROWS = TEAM < 256 ? 256 / TEAM : 1;
+  const int lane = threadIdx.x % TEAM, V = (int)a.V;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
+  if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-  T* dx = static_cast<T*>(a.dx) + row * a.lddx;
-  const int64_t V = a.V, groups = (V + 7) / 8, t = target_of(a, row);
-  const RowGradient rg(a, Running{0.f, 0.f}, a.lse_in[row], a.dloss ? a.dloss[row] : 1.f);
-#pragma unroll
-  for (int u = 0; u < kGroupsBwd; ++u) {
-    const int64_t g = ((int64_t)part * kGroupsBwd + u) * kThreadsBwd + threadIdx.x;
-    if (g >= groups) continue;
-    float f[8] = {};
-    if (t >= 0) {
-      load_group(x, g, V, 0.f, f);
-      rg.apply(f, g, t);
-    }
-    store_group(dx, g, V, f);
+  T* dx = a.dx ? static_cast<T*>(a.dx) + row * a.lddx : nullptr;
+  const int64_t t = target_of(a, row);
+  if (t < 0) {
+    if (lane == 0) finish_nothing(a, row);
+    if (dx) RowPart<T, TEAM, K>::zero(dx, lane, V);
+    return;
   }
+  RowPart<T, TEAM, K> p;
+  p.template load<PAST>(x, lane, V);
+  const float xt = element(x, t);
+  Running r = wave_join(p.running());
+  float sum = a.smooth != 0.f ? wave_sum(p.sum(lane, V)) : 0.f;
+  if constexpr (TEAM > 64) block_join<TEAM / 64>(r, sum);
+  const float lse = finish_row(a, row, r, xt, sum, lane == 0);
+  if (dx) p.template gradient<PAST>(RowGradient(a, r, lse, 1.f), dx, lane, V, t);
 }
 
-}  // namespace
+// Long rows in parts of kPart bytes, a workgroup each: every part leaves its
+// maximum, the sum under it, its elements' sum and the target's element (which
+// the gradient may overwrite), and the gradient's kernel joins a row's.
+constexpr int kPartThreads = 256, kPartPieces = 4, kPart = 16 * kPartPieces * kPartThreads;
 
-size_t cross_entropy_workspace(int64_t, int64_t, bool) { return 0; }
-
-hipError_t launch_cross_entropy(const CeArgs& a, hipStream_t stream) {
-  if (a.rows <= 0 || a.rows > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)a.rows), block(kThreads);
-  if (a.f32) hipLaunchKernelGGL(ce_stream_kernel<float>, grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(ce_stream_kernel<uint16_t>, grid, block, 0, stream, a);
-  return hipGetLastError();
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void ce_part_kernel(CeArgs a, uint32_t parts, FastDiv by_parts) {
+  const uint32_t row = fast_div(blockIdx.x, by_parts), part = blockIdx.x - row * parts;
+  constexpr int E = kPart / (int)sizeof(T);
+  const int64_t t = target_of(a, row), c0 = (int64_t)part * E;
+  if (t < 0) return;
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx + c0;
+  const int n = (int)min((int64_t)E, a.V - c0);
+  RowPart<T, kPartThreads, kPartPieces> p;
+  p.template load<false>(x, threadIdx.x, n);
+  const float xt = t >= c0 && t < c0 + n ? element(x, t - c0) : 0.f;
+  Running r = wave_join(p.running());
+  float sum = a.smooth != 0.f ? wave_sum(p.sum(threadIdx.x, n)) : 0.f;
+  block_join<kPartThreads / 64>(r, sum);
+  if (threadIdx.x == 0) static_cast<f32x4*>(a.workspace)[blockIdx.x] = f32x4{r.m, r.s, sum, xt};
 }
 
-hipError_t launch_cross_entropy_bwd(const CeArgs& a, hipStream_t stream) {
-  const int64_t per = 8 * kGroupsBwd * kThreadsBwd, parts = (a.V + per - 1) / per;
-  const int64_t rows_per = ((int64_t)1 << 30) / parts;
-  const FastDiv by_parts = fast_divisor((uint32_t)parts);
+// The gradient from the parts, of which the first workgroup of a row makes loss
+// and lse too (the only one there is without a gradient).
+template <typename T, bool PAST>
+__global__ __launch_bounds__(kPartThreads) void ce_grad_kernel(CeArgs a, uint32_t parts, uint32_t grid_parts,
+                                                               FastDiv by_parts) {
+  const uint32_t row = fast_div(blockIdx.x, by_parts), part = blockIdx.x - row * grid_parts;
+  constexpr int E = kPart / (int)sizeof(T);
+  const int64_t t = target_of(a, row), c0 = (int64_t)part * E;
+  const int n = (int)min((int64_t)E, a.V - c0);
+  T* dx = a.dx ? static_cast<T*>(a.dx) + row * a.lddx + c0 : nullptr;
+  using Part = RowPart<T, kPartThreads, kPartPieces>;
+  if (t < 0) {
+    if (part == 0 && threadIdx.x == 0) finish_nothing(a, row);
+    if (dx) Part::zero(dx, threadIdx.x, n);
+    return;
+  }
+  Part p;
+  if (dx) p.template load<PAST>(static_cast<const T*>(a.x) + row * a.ldx + c0, threadIdx.x, n);
+  const f32x4* q = static_cast<const f32x4*>(a.workspace) + (int64_t)row * parts;
+  Running r{-__builtin_inff(), 0.f};
+  float sum = 0.f;
+  for (uint32_t i = threadIdx.x; i < parts; i += kPartThreads) {
+    r.join(q[i][0], q[i][1]);
+    sum += q[i][2];
+  }
+  r = wave_join(r);
+  sum = wave_sum(sum);
+  block_join<kPartThreads / 64>(r, sum);
+  const float lse = finish_row(a, row, r, q[t / E][3], sum, part == 0 && threadIdx.x == 0);
+  if (dx) p.template gradient<PAST>(RowGradient(a, r, lse, 1.f), dx, threadIdx.x, n, t - c0);
+}
+
+// The gradient from a kept lse: K x 64 pieces of a row a wave.
+template <typename T, int K, bool PAST>
+__global__ __launch_bounds__(256) void ce_bwd_kernel(CeArgs a, uint32_t parts, FastDiv by_parts) {
+  const uint32_t wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const uint32_t row = fast_div(wave, by_parts), part = wave - row * parts;
+  if (row >= a.rows) return;
+  constexpr int E = 64 * K * Piece<T>::N;
+  const int64_t t = target_of(a, row), c0 = (int64_t)part * E;
+  const int n = (int)min((int64_t)E, a.V - c0);
+  T* dx = static_cast<T*>(a.dx) + row * a.lddx + c0;
+  if (t < 0) return RowPart<T, 64, K>::zero(dx, lane, n);
+  RowPart<T, 64, K> p;
+  p.template load<PAST>(static_cast<const T*>(a.x) + row * a.ldx + c0, lane, n);
+  const RowGradient g(a, Running{0.f, 0.f}, a.lse_in[row], a.dloss ? a.dloss[row] : 1.f);
+  p.template gradient<PAST>(g, dx, lane, n, t - c0);
+}
+
+// Rows [r, r + n) of a call.
+CeArgs rows_from(const CeArgs& a, int64_t r, int64_t n) {
   const int el = a.f32 ? 4 : 2, id = a.id64 ? 8 : 4;
-  for (int64_t r = 0; r < a.rows; r += rows_per) {
-    CeArgs b = a;
-    b.rows = a.rows - r < rows_per ? a.rows - r : rows_per;
-    b.x = static_cast<const char*>(a.x) + r * a.ldx * el;
-    b.dx = static_cast<char*>(a.dx) + r * a.lddx * el;
-    b.targets = static_cast<const char*>(a.targets) + r * id;
-    b.lse_in = a.lse_in + r;
-    if (a.dloss) b.dloss = a.dloss + r;
-    const dim3 grid((uint32_t)(b.rows * parts)), block(kThreadsBwd);
-    if (a.f32) hipLaunchKernelGGL(ce_bwd_kernel<float>, grid, block, 0, stream, b, (uint32_t)parts, by_parts);
-    else hipLaunchKernelGGL(ce_bwd_kernel<uint16_t>, grid, block, 0, stream, b, (uint32_t)parts, by_parts);
+  CeArgs b = a;
+  b.rows = n;
+  b.x = static_cast<const char*>(a.x) + r * a.ldx * el;
+  if (a.dx) b.dx = static_cast<char*>(a.dx) + r * a.lddx * el;
+  b.targets = static_cast<const char*>(a.targets) + r * id;
+  if (a.loss) b.loss = a.loss + r;
+  if (a.lse) b.lse = a.lse + r;
+  if (a.lse_in) b.lse_in = a.lse_in + r;
+  if (a.dloss) b.dloss = a.dloss + r;
+  return b;
+}
+
+int64_t parts_of(int64_t V, bool f32) { return (V * (f32 ? 4 : 2) + kPart - 1) / kPart; }
+
+// Rows whose logits the gradient's kernel finds in the memory-side cache after
+// the parts' kernel.
+int64_t rows_at_once(int64_t rows, int64_t V, bool f32) {
+  const int64_t fit = ((int64_t)96 << 20) / (V * (f32 ? 4 : 2));
+  return std::min(rows, std::max<int64_t>(fit, 1));
+}
+
+constexpr int64_t kFewRows = 127;
+bool in_parts(int64_t rows, int64_t V, bool f32) {
+  if (V > (f32 ? 65536 : 131072)) return true;
+  return V > 32768 && rows <= kFewRows;
+}
+
+template <typename T, bool PAST>
+hipError_t launch_parts(const CeArgs& a, hipStream_t stream) {
+  const int64_t parts = parts_of(a.V, a.f32), step = rows_at_once(a.rows, a.V, a.f32), n = a.dx ? parts : 1;
+  const FastDiv by_parts = fast_divisor((uint32_t)parts), by_n = fast_divisor((uint32_t)n);
+  for (int64_t r = 0; r < a.rows; r += step) {
+    const CeArgs b = rows_from(a, r, std::min(step, a.rows - r));
+    hipLaunchKernelGGL(ce_part_kernel<T>, dim3((uint32_t)(b.rows * parts)), dim3(kPartThreads), 0, stream, b,
+                       (uint32_t)parts, by_parts);
+    hipLaunchKernelGGL((ce_grad_kernel<T, PAST>), dim3((uint32_t)(b.rows * n)), dim3(kPartThreads), 0, stream, b,
+                       (uint32_t)parts, (uint32_t)n, by_n);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+template <typename T, int TEAM, int K, bool PAST>
+hipError_t launch_row(const CeArgs& a, hipStream_t stream) {
+  constexpr int ROWS = TEAM < 256 ? 256 / TEAM : 1;
+  hipLaunchKernelGGL((ce_row_kernel<T, TEAM, K, PAST>), dim3((uint32_t)((a.rows + ROWS - 1) / ROWS)),
+                     dim3(TEAM * ROWS), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool PAST>
+hipError_t launch_loss(const CeArgs& a, hipStream_t stream) {
+  if (in_parts(a.rows, a.V, a.f32)) return launch_parts<T, PAST>(a, stream);
+  const int64_t pieces = (a.V + Piece<T>::N - 1) / Piece<T>::N;
+  if (pieces <= 64) return launch_row<T, 64, 1, PAST>(a, stream);
+  if (pieces <= 64 * 2) return launch_row<T, 64, 2, PAST>(a, stream);
+  if (pieces <= 64 * 4) return launch_row<T, 64, 4, PAST>(a, stream);
+  if (pieces <= 256 * 2) return launch_row<T, 256, 2, PAST>(a, stream);
+  if (pieces <= 256 * 4) return launch_row<T, 256, 4, PAST>(a, stream);
+  if (pieces <= 256 * 8) return launch_row<T, 256, 8, PAST>(a, stream);
+  if (pieces <= 512 * 8) return launch_row<T, 512, 8, PAST>(a, stream);
+  if (pieces <= 512 * 16) return launch_row<T, 512, 16, PAST>(a, stream);
+  return launch_row<T, 1024, 16, PAST>(a, stream);
+}
+
+template <typename T, int K, bool PAST>
+hipError_t launch_bwd(const CeArgs& a, hipStream_t stream) {
+  constexpr int E = 64 * K * Piece<T>::N;
+  const int64_t parts = (a.V + E - 1) / E, step = ((int64_t)1 << 30) / parts;
+  const FastDiv by_parts = fast_divisor((uint32_t)parts);
+  for (int64_t r = 0; r < a.rows; r += step) {
+    const CeArgs b = rows_from(a, r, std::min(step, a.rows - r));
+    const dim3 grid((uint32_t)((b.rows * parts + 3) / 4)), block(256);
+    hipLaunchKernelGGL((ce_bwd_kernel<T, K, PAST>), grid, block, 0, stream, b, (uint32_t)parts, by_parts);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// One piece a lane where that is the row, so that no lane of a short row's wave
+// computes on nothing.
+template <typename T, bool PAST>
+hipError_t launch_bwd(const CeArgs& a, hipStream_t stream) {
+  if (a.V <= 64 * Piece<T>::N) return launch_bwd<T, 1, PAST>(a, stream);
+  return launch_bwd<T, 4, PAST>(a, stream);
+}
+
+}  // namespace
+
+size_t cross_entropy_workspace(int64_t rows, int64_t V, bool f32) {
+  // Not less for more rows than for fewer.
+  if (rows > kFewRows && !in_parts(rows, V, f32)) rows = kFewRows;
+  if (rows <= 0 || !in_parts(rows, V, f32)) return 0;
+  return (size_t)(rows_at_once(rows, V, f32) * parts_of(V, f32)) * sizeof(f32x4);
+}
+
+hipError_t launch_cross_entropy(const CeArgs& a, hipStream_t stream) {
+  if (a.rows <= 0 || a.rows > INT32_MAX) return hipErrorInvalidValue;
+  if (stream_activation(a.rows, a.V, a.f32))
+    return a.f32 ? launch_loss<float, true>(a, stream) : launch_loss<uint16_t, true>(a, stream);
+  return a.f32 ? launch_loss<float, false>(a, stream) : launch_loss<uint16_t, false>(a, stream);
+}
+
+hipError_t launch_cross_entropy_bwd(const CeArgs& a, hipStream_t stream) {
+  if (stream_activation(a.rows, a.V, a.f32))
+    return a.f32 ? launch_bwd<float, true>(a, stream) : launch_bwd<uint16_t, true>(a, stream);
+  return a.f32 ? launch_bwd<float, false>(a, stream) : launch_bwd<uint16_t, false>(a, stream);
 }
 
 }  // namespace sppo
