@@ -6,14 +6,62 @@
 namespace sppo {
 namespace {
 
-constexpr int kThreads = 256, kGroups = kOptTile / (8 * kThreads);  // of eight elements a thread
+constexpr int kThreads = 256, kQuads = kOptTile / (4 * kThreads);  // of four elements a thread
 
-__device__ __forceinline__ float load1(const void* p, int64_t i, bool bf16) {
-  return bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(p)[i] << 16) : static_cast<const float*>(p)[i];
+// N consecutive elements of a tensor that is aligned to its element, in one
+// access; PAST: past the caches.
+template <typename T, int N>
+struct Vec;
+template <>
+struct Vec<float, 4> {
+  using V = f32x4_a4;
+  V v;
+  __device__ __forceinline__ void get(float (&f)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = v[e];
+  }
+  __device__ __forceinline__ void set(const float (&f)[4]) { v = V{f[0], f[1], f[2], f[3]}; }
+};
+template <>
+struct Vec<uint16_t, 4> {
+  using V = uint32_t __attribute__((ext_vector_type(2), aligned(2)));
+  V v;
+  __device__ __forceinline__ void get(float (&f)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+  }
+  __device__ __forceinline__ void set(const float (&f)[4]) {
+    const u32x2 p = pack_bf16x4(f[0], f[1], f[2], f[3]);
+    v = V{p[0], p[1]};
+  }
+};
+template <>
+struct Vec<uint16_t, 8> {
+  using V = uint32_t __attribute__((ext_vector_type(4), aligned(2)));
+  V v;
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+  }
+};
+template <bool PAST, typename T, int N>
+__device__ __forceinline__ void load_vec(Vec<T, N>& x, const T* p) {
+  const auto* q = reinterpret_cast<const typename Vec<T, N>::V*>(p);
+  x.v = PAST ? __builtin_nontemporal_load(q) : *q;
 }
-__device__ __forceinline__ void store_bf16(void* p, int64_t i, float v) {
-  static_cast<__bf16*>(p)[i] = (__bf16)v;
+template <bool PAST, typename T>
+__device__ __forceinline__ void store_quad(T* p, const float (&f)[4]) {
+  Vec<T, 4> x;
+  x.set(f);
+  auto* q = reinterpret_cast<typename Vec<T, 4>::V*>(p);
+  if constexpr (PAST) __builtin_nontemporal_store(x.v, q);
+  else *q = x.v;
 }
+
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *reinterpret_cast<__bf16*>(p) = (__bf16)v; }
 
 // --------------------------------------------------------------- sum of squares
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -29,28 +77,37 @@ __device__ __forceinline__ double block_sum64(double v, double* lds) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-template <typename T>
-__device__ __forceinline__ double square_groups(const T* g, int n) {
-  Eight<T> x[kGroups];
+// Of n <= kOptTile elements.  Squares of fp32 numbers are exact in fp64, and
+// their sum neither overflows nor loses small gradients.
+template <typename T, bool PAST>
+__device__ __forceinline__ double tile_squares(const T* g, int n) {
+  constexpr int N = 16 / (int)sizeof(T), K = kOptTile / (N * kThreads);
+  Vec<T, N> x[K];
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) {
-    const int e = 8 * (kThreads * u + threadIdx.x);
-    if (e + 8 <= n) x[u].stream(g + e);
-    else x[u].zero();
+  for (int u = 0; u < K; ++u) {
+    const int e = N * (kThreads * u + threadIdx.x);
+    if (e + N <= n) load_vec<PAST>(x[u], g + e);
   }
-  double s = 0.0;
+  double s[2] = {0.0, 0.0};
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) {
-    float f[8];
+  for (int u = 0; u < K; ++u) {
+    const int e = N * (kThreads * u + threadIdx.x);
+    if (e + N > n) continue;
+    float f[N];
     x[u].get(f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += (double)f[e] * f[e];
+    for (int i = 0; i < N; ++i) s[i & 1] += (double)f[i] * f[i];
   }
-  return s;
+  const int e = n / N * N + threadIdx.x;
+  if (e < n) {
+    const double f = load1(g + e);
+    s[0] += f * f;
+  }
+  return s[0] + s[1];
 }
 
-// Squares of fp32 numbers are exact in fp64 and their sum neither overflows nor
-// loses small gradients; workgroup b adds tiles b, b + gridDim, ... in order.
+// Workgroup b adds tiles b, b + gridDim, ... in order.
+template <bool PAST>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(OptTable t, double* part) {
   __shared__ double lds[4];
   double s = 0.0;
@@ -59,17 +116,8 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(OptTable t, double* par
     const OptDesc& d = t.desc[at.tensor];
     const int64_t e0 = (int64_t)at.tile * kOptTile;
     const int n = (int)min((int64_t)kOptTile, d.n - e0);
-    const bool bf = d.flags & kOptGradBf16;
-    int done = 0;
-    if (d.flags & kOptVector) {
-      s += bf ? square_groups(static_cast<const uint16_t*>(d.grad) + e0, n)
-              : square_groups(static_cast<const float*>(d.grad) + e0, n);
-      done = n & ~7;
-    }
-    for (int e = done + threadIdx.x; e < n; e += kThreads) {
-      const double g = load1(d.grad, e0 + e, bf);
-      s += g * g;
-    }
+    s += d.flags & kOptGradBf16 ? tile_squares<uint16_t, PAST>(static_cast<const uint16_t*>(d.grad) + e0, n)
+                                : tile_squares<float, PAST>(static_cast<const float*>(d.grad) + e0, n);
   }
   s = block_sum64(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -127,77 +175,57 @@ __device__ __forceinline__ void moments(const Coef& c, float g, float& m, float&
 }
 // The parameter from m and r = sqrt(v).
 __device__ __forceinline__ float stepped(const Coef& c, float p, float m, float r) {
-  const float q = m * c.im / (r * c.ir + c.eps);
+  const float q = m * c.im * __builtin_amdgcn_rcpf(r * c.ir + c.eps);
   return p - c.lr * (q + c.wd * p);
 }
 
-template <typename G, bool PBF>
-__device__ __forceinline__ void adam_groups(const Coef& c, const OptDesc& d, int64_t e0, int n) {
+// A tile with fp32 states: all loads first.
+template <typename G, bool PBF, bool PAST>
+__device__ __forceinline__ void adam_tile(const Coef& c, const OptDesc& d, int64_t e0, int n) {
   const G* g = static_cast<const G*>(d.grad) + e0;
   float* w = (PBF ? d.master : static_cast<float*>(d.param)) + e0;
   float* m = static_cast<float*>(d.m) + e0;
   float* v = static_cast<float*>(d.v) + e0;
-  Eight<G> xg[kGroups];
-  Eight<float> xw[kGroups], xm[kGroups], xv[kGroups];
+  uint16_t* p = static_cast<uint16_t*>(d.param) + e0;
+  Vec<G, 4> xg[kQuads];
+  Vec<float, 4> xw[kQuads], xm[kQuads], xv[kQuads];
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) {
-    const int e = 8 * (kThreads * u + threadIdx.x);
-    if (e + 8 > n) continue;
-    xg[u].load(g + e);
-    xw[u].load(w + e);
-    xm[u].load(m + e);
-    xv[u].load(v + e);
+  for (int u = 0; u < kQuads; ++u) {
+    const int e = 4 * (kThreads * u + threadIdx.x);
+    if (e + 4 > n) continue;
+    load_vec<PAST>(xg[u], g + e);
+    load_vec<PAST>(xw[u], w + e);
+    load_vec<PAST>(xm[u], m + e);
+    load_vec<PAST>(xv[u], v + e);
   }
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) {
-    const int e = 8 * (kThreads * u + threadIdx.x);
-    if (e + 8 > n) continue;
-    float fg[8], fw[8], fm[8], fv[8];
+  for (int u = 0; u < kQuads; ++u) {
+    const int e = 4 * (kThreads * u + threadIdx.x);
+    if (e + 4 > n) continue;
+    float fg[4], fw[4], fm[4], fv[4];
     xg[u].get(fg);
     xw[u].get(fw);
     xm[u].get(fm);
     xv[u].get(fv);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       moments(c, fg[i], fm[i], fv[i]);
       fw[i] = stepped(c, fw[i], fm[i], sqrtf(fv[i]));
     }
-    Eight<float>::store(m + e, fm);
-    Eight<float>::store(v + e, fv);
-    Eight<float>::store(w + e, fw);
-    if constexpr (PBF) Eight<uint16_t>::store(static_cast<uint16_t*>(d.param) + e0 + e, fw);
+    store_quad<PAST>(m + e, fm);
+    store_quad<PAST>(v + e, fv);
+    store_quad<PAST>(w + e, fw);
+    if constexpr (PBF) store_quad<PAST>(p + e, fw);
   }
-}
-
-__global__ __launch_bounds__(kThreads) void adam_f32_kernel(OptTable tab, AdamArgs a) {
-  const OptTile at = tab.tile[blockIdx.x];
-  const OptDesc& d = tab.desc[at.tensor];
-  const int64_t e0 = (int64_t)at.tile * kOptTile;
-  const int n = (int)min((int64_t)kOptTile, d.n - e0);
-  Coef c;
-  int64_t t;
-  if (!coefficients(a, d, c, t)) return;
-  const bool pbf = d.flags & kOptParamBf16, gbf = d.flags & kOptGradBf16;
-  int done = 0;
-  if (d.flags & kOptVector) {
-    if (gbf && pbf) adam_groups<uint16_t, true>(c, d, e0, n);
-    else if (gbf) adam_groups<uint16_t, false>(c, d, e0, n);
-    else if (pbf) adam_groups<float, true>(c, d, e0, n);
-    else adam_groups<float, false>(c, d, e0, n);
-    done = n & ~7;
-  }
-  float* w = pbf ? d.master : static_cast<float*>(d.param);
-  float* m = static_cast<float*>(d.m);
-  float* v = static_cast<float*>(d.v);
-  for (int i = done + threadIdx.x; i < n; i += kThreads) {
-    const int64_t e = e0 + i;
+  const int e = (n & ~3) + (int)threadIdx.x;
+  if (e < n) {
     float fm = m[e], fv = v[e];
-    moments(c, load1(d.grad, e, gbf), fm, fv);
+    moments(c, load1(g + e), fm, fv);
     const float fw = stepped(c, w[e], fm, sqrtf(fv));
     m[e] = fm;
     v[e] = fv;
     w[e] = fw;
-    if (pbf) store_bf16(d.param, e, fw);
+    if constexpr (PBF) store1(p + e, fw);
   }
 }
 
@@ -205,30 +233,32 @@ __global__ __launch_bounds__(kThreads) void adam_f32_kernel(OptTable tab, AdamAr
 // 2^k of k in [-126, 127]; a block's exponent byte 0 stands for zeros.
 __device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
-__device__ __forceinline__ void decode8(u32x2 codes, float scale, float (&f)[8]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i], false);
-    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i], true);
-    f[4 * i] = lo[0] * scale;
-    f[4 * i + 1] = lo[1] * scale;
-    f[4 * i + 2] = hi[0] * scale;
-    f[4 * i + 3] = hi[1] * scale;
-  }
+__device__ __forceinline__ void decode8(uint32_t codes, float scale, float (&f)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false);
+  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  f[0] = lo[0] * scale;
+  f[1] = lo[1] * scale;
+  f[2] = hi[0] * scale;
+  f[3] = hi[1] * scale;
+}
+__device__ __forceinline__ uint32_t encode8(const float (&f)[4]) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
 }
 
-// The exponent of a block of 32 (eight elements in each of four neighbouring
+// The exponent of a block of 32 (four elements in each of eight neighbouring
 // lanes): the least k >= -126 with the largest finite magnitude at most 448 2^k
 // (448 = 1.75 2^8: mantissas above .75 carry into the exponent).
-__device__ __forceinline__ int block_exponent(const float (&f)[8]) {
+__device__ __forceinline__ int block_exponent(const float (&f)[4]) {
   float a = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     const float x = fabsf(f[i]);
     a = fmaxf(a, x < __builtin_inff() ? x : 0.f);
   }
   a = fmaxf(a, dpp<0xB1>(a));
   a = fmaxf(a, dpp<0x4E>(a));
+  a = fmaxf(a, dpp<0x141>(a));
   return max((int)((__float_as_uint(a) + 0x1FFFFFu) >> 23) - 135, -126);
 }
 
@@ -241,61 +271,60 @@ __device__ __forceinline__ float round8(float y, uint32_t bits) {
   return y <= 448.f ? __uint_as_float(t) - low : __builtin_nanf("");
 }
 
-__device__ __forceinline__ u32x2 encode8(const float (&f)[8]) {
-  u32x2 r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], w, true);
-    r[i] = (uint32_t)w;
-  }
-  return r;
-}
-
-// The groups of a tile: elements from n on count as zeros and are not written,
-// so every lane takes part in its block's exponent.
-template <typename G, bool PBF>
-__device__ __forceinline__ void adam8_groups(const Coef& c, const OptDesc& d, int64_t e0, int n, int64_t t,
-                                             uint64_t seed) {
+// A tile with 8-bit states: elements from n on count as zeros and are not
+// written, so that every lane takes part in its block's exponent.
+template <typename G, bool PBF, bool PAST>
+__device__ __forceinline__ void adam8_tile(const Coef& c, const OptDesc& d, int64_t e0, int n, int64_t t,
+                                           uint64_t seed) {
   const G* g = static_cast<const G*>(d.grad) + e0;
   float* w = (PBF ? d.master : static_cast<float*>(d.param)) + e0;
   uint8_t* m = static_cast<uint8_t*>(d.m) + e0;
   uint8_t* v = static_cast<uint8_t*>(d.v) + e0;
+  uint16_t* p = static_cast<uint16_t*>(d.param) + e0;
+  uint8_t* ms = d.m_scale + e0 / 32;
+  uint8_t* vs = d.v_scale + e0 / 32;
+  const uint64_t group0 = 8 * (uint64_t)d.block0 + (uint64_t)e0 / 4;
+  Vec<G, 4> xg[kQuads];
+  Vec<float, 4> xw[kQuads];
+  uint32_t cm[kQuads], cv[kQuads], sm[kQuads], sv[kQuads];
 #pragma unroll
-  for (int u = 0; u < kGroups; ++u) {
-    const int e = 8 * (kThreads * u + threadIdx.x);
-    const bool whole = e + 8 <= n;
-    float fg[8] = {}, fw[8] = {}, fm[8] = {}, fr[8] = {};
-    const int64_t block = (e0 + e) / 32;
-    u32x2 cm = {0, 0}, cv = {0, 0};
-    float sm = 0.f, sv = 0.f;
+  for (int u = 0; u < kQuads; ++u) {
+    const int q = kThreads * u + threadIdx.x, e = 4 * q;
+    sm[u] = sv[u] = cm[u] = cv[u] = 0;
+    xg[u].v = {};
+    xw[u].v = {};
     if (e < n) {
-      sm = __uint_as_float((uint32_t)d.m_scale[block] << 23);
-      sv = __uint_as_float((uint32_t)d.v_scale[block] << 23);
+      sm[u] = ms[q / 8];
+      sv[u] = vs[q / 8];
     }
-    if (whole) {
-      Eight<G> xg;
-      Eight<float> xw;
-      xg.load(g + e);
-      xw.load(w + e);
-      xg.get(fg);
-      xw.get(fw);
-      cm = *reinterpret_cast<const u32x2*>(m + e);
-      cv = *reinterpret_cast<const u32x2*>(v + e);
-    } else {
+    if (e + 4 <= n) {
+      load_vec<PAST>(xg[u], g + e);
+      load_vec<PAST>(xw[u], w + e);
+      cm[u] = *reinterpret_cast<const uint32_t*>(m + e);
+      cv[u] = *reinterpret_cast<const uint32_t*>(v + e);
+    }
+  }
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+  for (int u = 0; u < kQuads; ++u) {
+    const int q = kThreads * u + threadIdx.x, e = 4 * q;
+    float fg[4], fw[4], fm[4], fr[4];
+    xg[u].get(fg);
+    xw[u].get(fw);
+    const bool whole = e + 4 <= n, some = e < n && !whole;
+    if (some) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
         if (e + i < n) {
-          fg[i] = load1(g, e + i, sizeof(G) == 2);
+          fg[i] = load1(g + e + i);
           fw[i] = w[e + i];
-          cm[i >> 2] |= (uint32_t)m[e + i] << (8 * (i & 3));
-          cv[i >> 2] |= (uint32_t)v[e + i] << (8 * (i & 3));
+          cm[u] |= (uint32_t)m[e + i] << (8 * i);
+          cv[u] |= (uint32_t)v[e + i] << (8 * i);
         }
     }
-    decode8(cm, sm, fm);
-    decode8(cv, sv, fr);
+    decode8(cm[u], __uint_as_float(sm[u] << 23), fm);
+    decode8(cv[u], __uint_as_float(sv[u] << 23), fr);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       float v2 = fr[i] * fr[i];
       moments(c, fg[i], fm[i], v2);
       fr[i] = sqrtf(v2);
@@ -303,39 +332,38 @@ __device__ __forceinline__ void adam8_groups(const Coef& c, const OptDesc& d, in
     }
     const int km = block_exponent(fm), kr = block_exponent(fr);
     const float im = pow2(-km), ir = pow2(-kr);
-    const uint64_t group = 8 * ((uint64_t)d.block0 + (uint64_t)block) + (uint64_t)((e & 31) >> 2);
-    const u32x4 d0 = philox(group, (uint64_t)t, seed), d1 = philox(group + 1, (uint64_t)t, seed);
+    const u32x4 draw = philox(group0 + q, (uint64_t)t, seed);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t word = i < 4 ? d0[i & 3] : d1[i & 3];
-      fm[i] = copysignf(round8(fabsf(fm[i]) * im, word & 0xFFFFu), fm[i]);
-      const float r = round8(fr[i] * ir, word >> 16);
+    for (int i = 0; i < 4; ++i) {
+      fm[i] = copysignf(round8(fabsf(fm[i]) * im, draw[i] & 0xFFFFu), fm[i]);
+      const float r = round8(fr[i] * ir, draw[i] >> 16);
       fr[i] = fr[i] > 0.f && r == 0.f ? 0.001953125f : r;
     }
-    const u32x2 em = encode8(fm), er = encode8(fr);
+    const uint32_t em = encode8(fm), er = encode8(fr);
     if (whole) {
-      Eight<float>::store(w + e, fw);
-      if constexpr (PBF) Eight<uint16_t>::store(static_cast<uint16_t*>(d.param) + e0 + e, fw);
-      *reinterpret_cast<u32x2*>(m + e) = em;
-      *reinterpret_cast<u32x2*>(v + e) = er;
-    } else {
+      store_quad<PAST>(w + e, fw);
+      if constexpr (PBF) store_quad<PAST>(p + e, fw);
+      *reinterpret_cast<uint32_t*>(m + e) = em;
+      *reinterpret_cast<uint32_t*>(v + e) = er;
+    } else if (some) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 4; ++i)
         if (e + i < n) {
           w[e + i] = fw[i];
-          if constexpr (PBF) store_bf16(d.param, e0 + e + i, fw[i]);
-          m[e + i] = (uint8_t)(em[i >> 2] >> (8 * (i & 3)));
-          v[e + i] = (uint8_t)(er[i >> 2] >> (8 * (i & 3)));
+          if constexpr (PBF) store1(p + e + i, fw[i]);
+          m[e + i] = (uint8_t)(em >> (8 * i));
+          v[e + i] = (uint8_t)(er >> (8 * i));
         }
     }
-    if (e < n && (e & 31) == 0) {
-      d.m_scale[block] = (uint8_t)(km + 127);
-      d.v_scale[block] = (uint8_t)(kr + 127);
+    if (e < n && (q & 7) == 0) {
+      ms[q / 8] = (uint8_t)(km + 127);
+      vs[q / 8] = (uint8_t)(kr + 127);
     }
   }
 }
 
-__global__ __launch_bounds__(kThreads) void adam_e4m3_kernel(OptTable tab, AdamArgs a) {
+template <bool SMALL, bool PAST>
+__global__ __launch_bounds__(kThreads) void adam_kernel(OptTable tab, AdamArgs a) {
   const OptTile at = tab.tile[blockIdx.x];
   const OptDesc& d = tab.desc[at.tensor];
   const int64_t e0 = (int64_t)at.tile * kOptTile;
@@ -344,10 +372,17 @@ __global__ __launch_bounds__(kThreads) void adam_e4m3_kernel(OptTable tab, AdamA
   int64_t t;
   if (!coefficients(a, d, c, t)) return;
   const bool pbf = d.flags & kOptParamBf16, gbf = d.flags & kOptGradBf16;
-  if (gbf && pbf) adam8_groups<uint16_t, true>(c, d, e0, n, t, a.seed);
-  else if (gbf) adam8_groups<uint16_t, false>(c, d, e0, n, t, a.seed);
-  else if (pbf) adam8_groups<float, true>(c, d, e0, n, t, a.seed);
-  else adam8_groups<float, false>(c, d, e0, n, t, a.seed);
+  if constexpr (SMALL) {
+    if (gbf && pbf) adam8_tile<uint16_t, true, PAST>(c, d, e0, n, t, a.seed);
+    else if (gbf) adam8_tile<uint16_t, false, PAST>(c, d, e0, n, t, a.seed);
+    else if (pbf) adam8_tile<float, true, PAST>(c, d, e0, n, t, a.seed);
+    else adam8_tile<float, false, PAST>(c, d, e0, n, t, a.seed);
+  } else {
+    if (gbf && pbf) adam_tile<uint16_t, true, PAST>(c, d, e0, n);
+    else if (gbf) adam_tile<uint16_t, false, PAST>(c, d, e0, n);
+    else if (pbf) adam_tile<float, true, PAST>(c, d, e0, n);
+    else adam_tile<float, false, PAST>(c, d, e0, n);
+  }
 }
 
 }  // namespace
@@ -356,7 +391,10 @@ hipError_t launch_grad_norm(const OptTable& t, float max_norm, float* out, int64
                             hipStream_t stream) {
   const int n = (int)(t.tiles < kNormBlocks ? t.tiles : kNormBlocks);
   if (n > 0) {
-    hipLaunchKernelGGL(sumsq_kernel, dim3(n), dim3(kThreads), 0, stream, t, part);
+    if (stream_activation(t.tiles, kOptTile, true))
+      hipLaunchKernelGGL(sumsq_kernel<true>, dim3(n), dim3(kThreads), 0, stream, t, part);
+    else
+      hipLaunchKernelGGL(sumsq_kernel<false>, dim3(n), dim3(kThreads), 0, stream, t, part);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -367,8 +405,11 @@ hipError_t launch_grad_norm(const OptTable& t, float max_norm, float* out, int64
 hipError_t launch_adamw(const OptTable& t, int state, const AdamArgs& a, hipStream_t stream) {
   if (t.tiles <= 0 || t.tiles > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((uint32_t)t.tiles), block(kThreads);
-  if (state == 2) hipLaunchKernelGGL(adam_e4m3_kernel, grid, block, 0, stream, t, a);
-  else hipLaunchKernelGGL(adam_f32_kernel, grid, block, 0, stream, t, a);
+  const bool past = stream_activation(t.tiles, kOptTile, true), small = state == 2;
+  if (small && past) hipLaunchKernelGGL((adam_kernel<true, true>), grid, block, 0, stream, t, a);
+  else if (small) hipLaunchKernelGGL((adam_kernel<true, false>), grid, block, 0, stream, t, a);
+  else if (past) hipLaunchKernelGGL((adam_kernel<false, true>), grid, block, 0, stream, t, a);
+  else hipLaunchKernelGGL((adam_kernel<false, false>), grid, block, 0, stream, t, a);
   return hipGetLastError();
 }
 
