@@ -241,34 +241,45 @@ __device__ __forceinline__ void decode8(uint32_t codes, float scale, float (&f)[
   f[2] = hi[0] * scale;
   f[3] = hi[1] * scale;
 }
-__device__ __forceinline__ uint32_t encode8(const float (&f)[4]) {
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
-}
-
 // The exponent of a block of 32 (four elements in each of eight neighbouring
 // lanes): the least k >= -126 with the largest finite magnitude at most 448 2^k
 // (448 = 1.75 2^8: mantissas above .75 carry into the exponent).
-__device__ __forceinline__ int block_exponent(const float (&f)[4]) {
-  float a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float x = fabsf(f[i]);
-    a = fmaxf(a, x < __builtin_inff() ? x : 0.f);
-  }
+__device__ __forceinline__ float block_max(const float (&f)[4]) {
+  float a = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));  // of what is no NaN
   a = fmaxf(a, dpp<0xB1>(a));
   a = fmaxf(a, dpp<0x4E>(a));
-  a = fmaxf(a, dpp<0x141>(a));
+  return fmaxf(a, dpp<0x141>(a));
+}
+__device__ __forceinline__ int block_exponent(const float (&f)[4]) {
+  float a = block_max(f);
+  if (__builtin_amdgcn_ballot_w64(a == __builtin_inff())) {  // some block of the wave: rare
+    float g[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g[i] = fabsf(f[i]) < __builtin_inff() ? f[i] : 0.f;
+    a = block_max(g);
+  }
   return max((int)((__float_as_uint(a) + 0x1FFFFFu) >> 23) - 135, -126);
 }
 
-// y >= 0, at most 448, cut to a multiple of its e4m3 step after 16 random bits
-// were added in what is cut off (20 bits of the mantissa; below 2^-6, where the
-// step stays 2^-9, of y + 2^-6).  Anything else becomes NaN.
-__device__ __forceinline__ float round8(float y, uint32_t bits) {
-  const float low = y < 0.015625f ? 0.015625f : 0.f;
-  const uint32_t t = (__float_as_uint(y + low) + (bits << 4)) & 0xFFF00000u;
-  return y <= 448.f ? __uint_as_float(t) - low : __builtin_nanf("");
+// Four values under their block's power of two (or NaN, infinite) to codes, up
+// with the probability of what is cut off: the conversion aligns the random
+// word's 32 bits with what is below a code's last bit, also below the normal
+// numbers, and carries.  HIGH: the draw's high halves, else the low ones.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t encode8(const float (&f)[4], const u32x4& draw) {
+  const auto bits = [&](int i) { return (int)(HIGH ? draw[i] & 0xFFFF0000u : draw[i] << 16); };
+  int w = __builtin_amdgcn_cvt_sr_fp8_f32(f[0], bits(0), 0, 0);
+  w = __builtin_amdgcn_cvt_sr_fp8_f32(f[1], bits(1), w, 1);
+  w = __builtin_amdgcn_cvt_sr_fp8_f32(f[2], bits(2), w, 2);
+  return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(f[3], bits(3), w, 3);
+}
+
+// sqrt(v), zero below the normal numbers: one step of Newton's on v rsq(v) (2 ulp)
+// leaves half an ulp and 2^-22 of one.
+__device__ __forceinline__ float root(float v) {
+  const float y = __builtin_amdgcn_rsqf(v), r = v * y;
+  const float s = __builtin_fmaf(__builtin_fmaf(-r, r, v), 0.5f * y, r);
+  return v < 1.17549435e-38f ? 0.f : s;
 }
 
 // A tile with 8-bit states: elements from n on count as zeros and are not
@@ -327,7 +338,7 @@ __device__ __forceinline__ void adam8_tile(const Coef& c, const OptDesc& d, int6
     for (int i = 0; i < 4; ++i) {
       float v2 = fr[i] * fr[i];
       moments(c, fg[i], fm[i], v2);
-      fr[i] = sqrtf(v2);
+      fr[i] = root(v2);
       fw[i] = stepped(c, fw[i], fm[i], fr[i]);
     }
     const int km = block_exponent(fm), kr = block_exponent(fr);
@@ -335,11 +346,10 @@ __device__ __forceinline__ void adam8_tile(const Coef& c, const OptDesc& d, int6
     const u32x4 draw = philox(group0 + q, (uint64_t)t, seed);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      fm[i] = copysignf(round8(fabsf(fm[i]) * im, draw[i] & 0xFFFFu), fm[i]);
-      const float r = round8(fr[i] * ir, draw[i] >> 16);
-      fr[i] = fr[i] > 0.f && r == 0.f ? 0.001953125f : r;
+      fm[i] *= im;
+      fr[i] = fr[i] == 0.f ? 0.f : max_nc(fr[i] * ir, 0.001953125f);  // 2^-9: not to zero
     }
-    const uint32_t em = encode8(fm), er = encode8(fr);
+    const uint32_t em = encode8<false>(fm, draw), er = encode8<true>(fr, draw);
     if (whole) {
       store_quad<PAST>(w + e, fw);
       if constexpr (PBF) store_quad<PAST>(p + e, fw);
