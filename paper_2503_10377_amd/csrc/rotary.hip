@@ -23,7 +23,7 @@ __device__ __forceinline__ void turn_cos_sin(uint32_t a, float& c, float& s) {
   s = q >= 2 ? -v : v;
 }
 
-// P consecutive elements as they lie in memory.
+// P consecutive elements as they lie in memory: 16 bytes, or four bf16.
 template <typename T, int P>
 struct Piece;
 template <>
@@ -44,130 +44,139 @@ struct Piece<uint16_t, 4> {
   }
   __device__ __forceinline__ void set(const float (&f)[4]) { v = pack_bf16x4(f[0], f[1], f[2], f[3]); }
 };
-template <int P>
-struct Piece<float, P> {
-  f32x4 v[P / 4];
-  __device__ __forceinline__ void get(float (&f)[P]) const {
+template <>
+struct Piece<float, 4> {
+  f32x4 v;
+  __device__ __forceinline__ void get(float (&f)[4]) const {
 #pragma unroll
-    for (int e = 0; e < P; ++e) f[e] = v[e >> 2][e & 3];
+    for (int e = 0; e < 4; ++e) f[e] = v[e];
   }
-  __device__ __forceinline__ void set(const float (&f)[P]) {
-#pragma unroll
-    for (int e = 0; e < P; ++e) v[e >> 2][e & 3] = f[e];
-  }
+  __device__ __forceinline__ void set(const float (&f)[4]) { v = f32x4{f[0], f[1], f[2], f[3]}; }
 };
 
-// The U x 64 items from `base` on of one row: G groups of P pairs a head, then
-// groups of 2 P copied elements; an item is two pieces of P elements.
-template <typename T, int P, bool HALF, int U>
-__device__ __forceinline__ void turn_items(const RotaryTensor& t, int rot, int64_t row, int base, int lane,
-                                           const float* cs, const float* sn) {
-  const int G = rot / 2 / P;
-  const T* x = static_cast<const T*>(t.x) + row * t.ldx;
-  T* y = static_cast<T*>(t.y) + row * t.ldy;
-  Piece<T, P> a[U], b[U];
-  int head[U], r[U], oa[U], ob[U];
+// N cosines or sines from LDS.
+template <int N>
+__device__ __forceinline__ void angles(const float* p, float (&c)[N]) {
+  typedef float V __attribute__((ext_vector_type(N < 4 ? N : 4)));
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int item = min(base + 64 * u + lane, t.items - 1);
-    head[u] = (int)fast_div((uint32_t)item, t.per_head);
-    r[u] = item - head[u] * t.per;
-    oa[u] = r[u] * (HALF ? P : 2 * P);
-    ob[u] = oa[u] + (HALF ? rot / 2 : P);
-    if (HALF && r[u] >= G) {
-      oa[u] = rot + (r[u] - G) * 2 * P;
-      ob[u] = oa[u] + P;
-    }
-    const T* h = x + head[u] * t.hsx;
-    a[u] = *reinterpret_cast<const Piece<T, P>*>(h + oa[u]);
-    b[u] = *reinterpret_cast<const Piece<T, P>*>(h + ob[u]);
-  }
+  for (int e = 0; e < N; e += 4) {
+    const V v = *reinterpret_cast<const V*>(p + e);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (base + 64 * u + lane >= t.items) continue;
-    if (r[u] < G) {
-      float f[P], g[P], c[P], s[P];
-      a[u].get(f);
-      b[u].get(g);
-#pragma unroll
-      for (int e = 0; e < P; e += 4) {
-        const f32x4 cv = *reinterpret_cast<const f32x4*>(cs + r[u] * P + e);
-        const f32x4 sv = *reinterpret_cast<const f32x4*>(sn + r[u] * P + e);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[e + i] = cv[i], s[e + i] = sv[i];
-      }
-      if constexpr (HALF) {
-#pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const float p = f[e], q = g[e];
-          f[e] = p * c[e] - q * s[e];
-          g[e] = q * c[e] + p * s[e];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < P / 2; ++e) {
-          const float p = f[2 * e], q = f[2 * e + 1], v = g[2 * e], w = g[2 * e + 1];
-          f[2 * e] = p * c[e] - q * s[e];
-          f[2 * e + 1] = q * c[e] + p * s[e];
-          g[2 * e] = v * c[P / 2 + e] - w * s[P / 2 + e];
-          g[2 * e + 1] = w * c[P / 2 + e] + v * s[P / 2 + e];
-        }
-      }
-      a[u].set(f);
-      b[u].set(g);
-    }
-    T* h = y + head[u] * t.hsy;
-    *reinterpret_cast<Piece<T, P>*>(h + oa[u]) = a[u];
-    *reinterpret_cast<Piece<T, P>*>(h + ob[u]) = b[u];
+    for (int i = 0; i < (N < 4 ? N : 4); ++i) c[e + i] = v[i];
   }
 }
 
-// A wave makes the cosines and sines of its row in LDS, a pair a lane, and
-// turns U x 64 items of one tensor with them.  The angle is position * freq
-// modulo 2^64, of which the upper half is used.
-template <int P, bool HALF, int U>
+// A piece with pairs side by side.
+template <int P>
+__device__ __forceinline__ void turn_pairs(float (&f)[P], const float* cs, const float* sn) {
+  float c[P / 2], s[P / 2];
+  angles(cs, c);
+  angles(sn, s);
+#pragma unroll
+  for (int e = 0; e < P / 2; ++e) {
+    const float a = f[2 * e], b = f[2 * e + 1];
+    f[2 * e] = a * c[e] - b * s[e];
+    f[2 * e + 1] = b * c[e] + a * s[e];
+  }
+}
+
+// The cosines and sines of a row's pairs in a wave's part of LDS, a pair a lane.
+// The angle is position * freq modulo 2^64, of which the upper half is used.
+__device__ __forceinline__ void make_table(const RotaryArgs& a, uint64_t pos, int lane, float* cs, float* sn) {
+  for (int j = lane; j < a.rot / 2; j += 64) {
+    float c, s;
+    turn_cos_sin((uint32_t)((pos * a.freqs[j]) >> 32), c, s);
+    cs[j] = a.amp * c;
+    sn[j] = a.amp * a.sign * s;
+  }
+  // Between the lanes of this wave only: its LDS accesses are served in order.
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// An item (64 of one row a wave) is two pieces of P elements of a head, half of
+// what is turned (or half of what is copied) apart, so that neighbouring lanes'
+// pieces lie side by side in either layout.  The loads go out before the table
+// is made.
+template <typename T, int P, bool HALF, bool PAST>
+__device__ __forceinline__ void turn_item(const RotaryArgs& a, const RotaryTensor& t, int64_t row, uint64_t pos,
+                                          int item, int lane, float* cs, float* sn) {
+  const int G = a.rot / 2 / P;  // items of a head that are turned
+  const int at = min(item, t.items - 1), head = (int)fast_div((uint32_t)at, t.per_head), r = at - head * t.per;
+  const bool turned = r < G;
+  const int oa = (turned ? 0 : a.rot - G * P) + r * P, ob = oa + (turned ? a.rot / 2 : (t.D - a.rot) / 2);
+  const T* x = static_cast<const T*>(t.x) + row * t.ldx + head * t.hsx;
+  T* y = static_cast<T*>(t.y) + row * t.ldy + head * t.hsy;
+  Piece<T, P> p, q;
+  const auto* px = reinterpret_cast<const decltype(p.v)*>(x + oa);
+  const auto* qx = reinterpret_cast<const decltype(q.v)*>(x + ob);
+  p.v = PAST ? __builtin_nontemporal_load(px) : *px;
+  q.v = PAST ? __builtin_nontemporal_load(qx) : *qx;
+  make_table(a, pos, lane, cs, sn);
+  if (item >= t.items) return;
+  if (turned) {
+    float f[P], g[P];
+    p.get(f);
+    q.get(g);
+    if constexpr (HALF) {
+      float c[P], s[P];
+      angles(cs + r * P, c);
+      angles(sn + r * P, s);
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        const float u = f[e], v = g[e];
+        f[e] = u * c[e] - v * s[e];
+        g[e] = v * c[e] + u * s[e];
+      }
+    } else {
+      const int j = r * P / 2;
+      turn_pairs(f, cs + j, sn + j);
+      turn_pairs(g, cs + a.rot / 4 + j, sn + a.rot / 4 + j);
+    }
+    p.set(f);
+    q.set(g);
+  }
+  *reinterpret_cast<decltype(p.v)*>(y + oa) = p.v;
+  *reinterpret_cast<decltype(q.v)*>(y + ob) = q.v;
+}
+
+// A wave turns 64 items of one tensor's row.
+template <int P, bool HALF, bool PAST>
 __global__ __launch_bounds__(64 * kWaves) void rotary_kernel(RotaryArgs a, uint32_t chunks, FastDiv by_chunks,
                                                              uint32_t waves) {
   extern __shared__ float tab[];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const uint32_t w = blockIdx.x * kWaves + wv;
-  const uint32_t at = __builtin_amdgcn_readfirstlane(w < waves ? w : waves - 1);
-  const uint32_t row = __builtin_amdgcn_readfirstlane(fast_div(at, by_chunks));
-  const int c = (int)(at - row * chunks), pairs = a.rot / 2;
+  const uint32_t w = __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + wv);
+  if (w >= waves) return;
+  const uint32_t row = __builtin_amdgcn_readfirstlane(fast_div(w, by_chunks));
+  const int c = (int)(w - row * chunks);
   uint64_t pos = (uint64_t)a.row0 + row;
   if (a.pos)
     pos = a.id64 ? (uint64_t) static_cast<const int64_t*>(a.pos)[row]
                  : (uint64_t)(int64_t) static_cast<const int32_t*>(a.pos)[row];
   float* cs = tab + wv * a.rot;
-  float* sn = cs + pairs;
-  for (int j = lane; j < pairs; j += 64) {
-    float co, si;
-    turn_cos_sin((uint32_t)((pos * a.freqs[j]) >> 32), co, si);
-    cs[j] = a.amp * co;
-    sn[j] = a.amp * a.sign * si;
-  }
-  __syncthreads();
-  if (w >= waves) return;
   int k = 0;
   while (k + 1 < a.n && c >= a.t[k + 1].chunk0) ++k;
   const RotaryTensor& t = a.t[k];
-  const int base = (c - t.chunk0) * 64 * U;
+  const int item = (c - t.chunk0) * 64 + lane;
   if (t.f32)
-    turn_items<float, P, HALF, U>(t, a.rot, row, base, lane, cs, sn);
+    turn_item<float, 4, HALF, PAST>(a, t, row, pos, item, lane, cs, cs + a.rot / 2);
   else
-    turn_items<uint16_t, P, HALF, U>(t, a.rot, row, base, lane, cs, sn);
+    turn_item<uint16_t, P, HALF, PAST>(a, t, row, pos, item, lane, cs, cs + a.rot / 2);
 }
 
-template <int P, int U>
+template <int P, bool PAST>
 hipError_t launch(RotaryArgs a, hipStream_t stream) {
   int64_t chunks = 0;
   for (int k = 0; k < a.n; ++k) {
     RotaryTensor& t = a.t[k];
-    t.per = a.rot / 2 / P + (t.x == t.y ? 0 : (t.D - a.rot) / (2 * P));  // in place nothing is copied
+    const int p = t.f32 ? 4 : P;
+    t.per = a.rot / 2 / p + (t.x == t.y ? 0 : (t.D - a.rot) / (2 * p));  // in place nothing is copied
     t.per_head = fast_divisor((uint32_t)t.per);
     t.items = t.heads * t.per;
     t.chunk0 = (int)chunks;
-    chunks += (t.items + 64 * U - 1) / (64 * U);
+    chunks += (t.items + 63) / 64;
   }
   // Waves of a launch index as numbers below 2^31 (fast_div).
   const int64_t rows_per = ((int64_t)1 << 30) / chunks;
@@ -186,10 +195,8 @@ hipError_t launch(RotaryArgs a, hipStream_t stream) {
     }
     const uint32_t waves = (uint32_t)(b.rows * chunks);
     const dim3 grid((waves + kWaves - 1) / kWaves), block(64 * kWaves);
-    if (a.half)
-      hipLaunchKernelGGL((rotary_kernel<P, true, U>), grid, block, lds, stream, b, (uint32_t)chunks, by_chunks, waves);
-    else
-      hipLaunchKernelGGL((rotary_kernel<P, false, U>), grid, block, lds, stream, b, (uint32_t)chunks, by_chunks, waves);
+    const auto kernel = a.half ? rotary_kernel<P, true, PAST> : rotary_kernel<P, false, PAST>;
+    hipLaunchKernelGGL(kernel, grid, block, lds, stream, b, (uint32_t)chunks, by_chunks, waves);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -199,9 +206,15 @@ hipError_t launch(RotaryArgs a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
-  bool wide = a.rot % 16 == 0;
-  for (int k = 0; k < a.n; ++k) wide = wide && a.t[k].D % 16 == 0;
-  return wide ? launch<8, 4>(a, stream) : launch<4, 4>(a, stream);
+  // Pieces of 16 bytes where bf16 tensors divide into pairs of them.
+  bool wide = true, past = false;
+  for (int k = 0; k < a.n; ++k) {
+    const RotaryTensor& t = a.t[k];
+    wide = wide && (t.f32 || (a.rot % 16 == 0 && t.D % 16 == 0));
+    past = past || stream_activation(a.rows, (int64_t)t.heads * t.D, t.f32);
+  }
+  if (past) return wide ? launch<8, true>(a, stream) : launch<4, true>(a, stream);
+  return wide ? launch<8, false>(a, stream) : launch<4, false>(a, stream);
 }
 
 }  // namespace sppo

@@ -323,16 +323,16 @@ size_t embedding_workspace(int64_t rows, int H);
 hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t stream);
 hipError_t launch_embedding_bwd(const EmbedArgs& a, hipStream_t stream);
 
-// Rotary positions of 1 to 4 tensors (rotary.hip).  A wave takes 64 kRotaryUnroll
-// (or 64) consecutive items of one row of one tensor, an item being a group of
-// rotated pairs or of copied elements of one head.
+// Rotary positions of 1 to 4 tensors (rotary.hip).  A wave takes 64 consecutive
+// items of one row of one tensor, an item being two pieces of a head that are
+// turned with each other's angles, or copied.
 constexpr int kRotaryMaxTensors = 4, kRotaryMaxDim = 1024;
 struct RotaryTensor {
   const void* x;
   void* y;
   int64_t ldx, hsx, ldy, hsy;
   int heads, D, f32;
-  // Set by the launcher: items of a head and of a row, the first wave of a row that takes this tensor.
+  // Set by the launcher: items of a head and of a row, the first of a row's waves that takes this tensor.
   int per, items, chunk0;
   FastDiv per_head;  // division by per
 };
