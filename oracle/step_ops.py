@@ -6,7 +6,8 @@ TEST INFRASTRUCTURE ONLY -- never imported by the product path.
 
 Pins (tests/test_step_ops_cpu.py): rotations keep lengths and depend on the
 difference of positions alone; the loss against a loop over classes, its
-gradient by central differences; AdamW against a scalar loop; the 8-bit format
+gradient by central differences; the layer's gradients by central differences
+of its mean loss; AdamW against a scalar loop; the 8-bit format
 against a table of its codes, its rounding by its mean over the draws.
 """
 from __future__ import annotations
@@ -15,7 +16,9 @@ import math
 
 import numpy as np
 
-from .train_ops import philox4x32
+from .causal_attention import attention_bwd, attention_fwd
+from .train_ops import block_norm_bwd, block_norm_fwd, philox4x32
+from .transformer_layer import gelu, gelu_grad, layer_norm, layer_norm_bwd
 
 
 def _f64(x):
@@ -149,3 +152,57 @@ def round8(x, scales, u, positive):
     code = np.where(bad, 127, code)
     sign = np.where(np.signbit(x), 128, 0)
     return (code + sign).astype(np.uint8), np.abs(share - 1.0)
+
+
+# -------------------------------------------------------------------- the layer
+def layer_step(x, p, hq, hkv, d, rope, targets, smooth=0.0, z=0.0, scale=1.0, ends=None, keep=(1.0, 1.0), eps=1e-5):
+    """A layer's forward and backward with rotary positions (rope: rot, layout,
+    freqs, amp, position0) and the loss of its output, unchunked, batch 1.
+    ends: as layer_with_ends takes them (None: plain adds).  Returns y, loss, dx
+    and the parameters' gradients by their names with a d in front."""
+    x = _f64(x)
+    S = len(x)
+    w = {k: _f64(v) for k, v in p.items()}
+    ends = ends or dict(norm="none", gate=False, alpha=1.0, scale=1.0)
+    cfg = [dict(post=ends["norm"], pre=pre, gate="channel" if ends["gate"] else "none", eps=eps, alpha=ends["alpha"],
+                scale=ends["scale"]) for pre in ("layer", "none")]
+    par = [dict(post_gamma=w.get(f"g_end{n}"), post_beta=w.get(f"b_end{n}"), gate=w.get(f"gate{n}"),
+                pre_gamma=w["g2"], pre_beta=w["b2"]) for n in (1, 2)]
+    keep = [np.ones(x.shape) * k for k in keep]
+    pos = np.arange(S) + rope["position0"]
+    turn = lambda t, inv: rotary(t[0], pos, rope["freqs"], rope["rot"], rope["layout"], rope["amp"], inv)[None]  # noqa: E731
+    u, m1, r1 = layer_norm(x, w["g1"], w["b1"], eps)
+    split = np.split(u @ w["w_qkv"], [hq * d, (hq + hkv) * d], axis=1)
+    q, k, v = (t.reshape(1, S, n, d) for t, n in zip(split, (hq, hkv, hkv)))
+    q, k = turn(q, False), turn(k, False)
+    sm = 1.0 / math.sqrt(d)
+    o4, lse = attention_fwd(q, k, v, sm)
+    o = o4.reshape(S, -1)
+    e1 = o @ w["w_o"]
+    f1 = block_norm_fwd(x, e1, cfg[0], par[0], keep[0])
+    a = f1["z"] @ w["w_1"]
+    g = gelu(a)
+    e2 = g @ w["w_2"]
+    f2 = block_norm_fwd(f1["h"], e2, cfg[1], par[1], keep[1])
+    y = f2["h"]
+    uf, mf, rf = layer_norm(y, w["gf"], w["bf"], eps)
+    loss, _, dl = cross_entropy(uf @ w["w_out"], targets, smooth, z, scale)
+    out = {"y": y, "loss": loss, "dw_out": uf.T @ dl}
+    dy, out["dgf"], out["dbf"] = layer_norm_bwd(y, w["gf"], mf, rf, dl @ w["w_out"].T)
+    b2 = block_norm_bwd(e2, None, f2, None, dy, cfg[1], par[1], keep[1])
+    out["dw_2"] = g.T @ b2["db"]
+    da = (b2["db"] @ w["w_2"].T) * gelu_grad(a)
+    out["dw_1"] = f1["z"].T @ da
+    b1 = block_norm_bwd(e1, f1["h"], f1, da @ w["w_1"].T, b2["dx"], cfg[0], par[0], keep[0])
+    out["dg2"], out["db2"] = b1["pre_gamma"], b1["pre_beta"]
+    out["dw_o"] = o.T @ b1["db"]
+    dq, dk, dv = attention_bwd(q, k, v, (b1["db"] @ w["w_o"].T).reshape(1, S, hq, d), sm, o4, lse)
+    dqkv = np.concatenate([t.reshape(S, -1) for t in (turn(dq, True), turn(dk, True), dv)], axis=1)
+    out["dw_qkv"] = u.T @ dqkv
+    dx, out["dg1"], out["db1"] = layer_norm_bwd(x, w["g1"], m1, r1, dqkv @ w["w_qkv"].T)
+    out["dx"] = b1["dx"] + dx
+    for n, b in ((1, b1), (2, b2)):
+        for ours, theirs in (("post_gamma", f"g_end{n}"), ("post_beta", f"b_end{n}"), ("gate", f"gate{n}")):
+            if theirs in p:
+                out["d" + theirs] = b[ours]
+    return out

@@ -47,11 +47,22 @@ Two options put the training operators around the blocks:
       does not travel), and dx_i becomes the table's gradient, added up over
       the reverse walk.
 
+Two more make the walk a whole training step's (optimizer.AdamW is its end):
+  rotary=Rotary(...)   the queries and keys are turned by their positions where
+      the projections left them (the K cache holds turned keys), and their
+      gradients are turned back, dK's rows in the fp32 accumulators once chunk
+      i's backward has made them final.
+  loss=Loss(classes)   dy comes from the loss: logits = LN_f(y) W_out and their
+      cross-entropy with targets, one chunk at a time at the head of its
+      backward, so that no more than a chunk's logits are ever held (their
+      gradient in their place).
+
 Only C-ABI calls and torch allocations happen here; every arithmetic step
 runs in the library's kernels.
 """
 from __future__ import annotations
 
+import numpy as np
 import torch
 
 from . import sppo as L
@@ -98,9 +109,43 @@ class BlockEnds:
         return names
 
 
+class Rotary:
+    """Positions in the attention: ``rot`` elements of a head are turned (all
+    where None), pairs (j, j + rot/2) ("half") or (2j, 2j + 1) ("interleaved");
+    the first row's position; the frequencies as sppo_rotary_freqs takes them
+    (base, scaling, factor, original_len, beta_fast, beta_slow, inv_freq)."""
+
+    def __init__(self, rot=None, layout="half", position0=0, **freqs):
+        if layout not in L.ROTARY_LAYOUTS:
+            raise ValueError(f"unknown layout {layout!r}")
+        if not 0 <= position0 < 2 ** 62:
+            raise ValueError("position0 must be in [0, 2^62)")
+        self.rot, self.layout, self.position0, self.freqs = rot, layout, position0, freqs
+
+    def table(self, head_dim, device):
+        """The device table of a head's frequencies and their amplitude."""
+        rot = head_dim if self.rot is None else self.rot
+        if rot > head_dim:
+            raise ValueError("rot is more than a head has")
+        freqs, amp = L.sppo_rotary_freqs(rot, **self.freqs)
+        return rot, torch.from_numpy(np.array(freqs, dtype=np.uint64).view(np.int64)).to(device), amp
+
+
+class Loss:
+    """The loss behind the layer: cross-entropy over ``classes`` (a multiple of
+    256, as the projection's gradient needs)."""
+
+    def __init__(self, classes, label_smoothing=0.0, z_loss=0.0):
+        if not 0 < classes < 2 ** 31 or classes % 256:
+            raise ValueError("classes must be a multiple of 256 below 2^31")
+        if not 0.0 <= label_smoothing <= 1.0 or not 0.0 <= z_loss < float("inf"):
+            raise ValueError("label_smoothing must be in [0, 1], z_loss finite and not negative")
+        self.classes, self.label_smoothing, self.z_loss = classes, label_smoothing, z_loss
+
+
 class ChunkedLayer:
     def __init__(self, S, n_chunks, Hq, Hkv, D, offsets=None, offload="none", device="cuda", eps=1e-5,
-                 host_ahead=2, fwd_slots=4, ends=None, vocab=None, embed_scale=1.0):
+                 host_ahead=2, fwd_slots=4, ends=None, vocab=None, embed_scale=1.0, rotary=None, loss=None):
         H = Hq * D
         wt = (Hq + 2 * Hkv) * D
         if H % 256 or wt % 256 or H > 8192:
@@ -113,6 +158,9 @@ class ChunkedLayer:
         self.eps = eps
         self.device = device
         self.ends, self.vocab, self.embed_scale = ends, vocab, embed_scale
+        self.rotary, self.loss = rotary, loss
+        if rotary is not None:
+            self.rot, self.rot_table, self.rot_amp = rotary.table(D, device)
         # bytes of a row of each plane: x, h, a bf16, mean/rstd of LN1, LN2 fp32;
         # with block ends their branches (bf16) and statistics
         self.row_bytes = dict(zip(PLANES, (2 * H, 2 * H, 8 * H, 4, 4, 4, 4)))
@@ -168,6 +216,16 @@ class ChunkedLayer:
                                   pre_gamma=self.dk, pre_beta=self.dk) for pre in ("layer", "none")]
             self.ends_ws_bytes = max(L.sppo_block_norm_bwd_workspace(b, sm) for b in probe)
             self.ends_ws = torch.empty(max(self.ends_ws_bytes, 16) // 4, dtype=f32, device=dev)
+        if self.loss is not None:
+            C = self.loss.classes
+            if sm * C >= 2 ** 31:
+                raise ValueError("a chunk's logits must be below 2^31 elements: smaller chunks")
+            self.wT["w_out"] = e(C, H)
+            self.logits, self.dy, self.none = e(sm, C), e(sm, H), torch.zeros(sm, H, dtype=bf, device=dev)
+            self.mf, self.rf = e(sm, dt=f32), e(sm, dt=f32)
+            ce = self._ce("i64", 1.0)
+            self.ce_ws_bytes = max(L.sppo_cross_entropy_workspace(ce, self.chunk_len(i)) for i in range(self.N))
+            self.ce_ws = torch.empty(max(self.ce_ws_bytes, 16) // 4, dtype=f32, device=dev)
         if self.vocab is not None:
             self.x, self.dx = e(sm, H), e(sm, H)
             self.emb_ws_bytes = L.sppo_embedding_bwd_workspace(sm, H)
@@ -181,6 +239,10 @@ class ChunkedLayer:
             more["dx"] = torch.empty(self.S, H, dtype=torch.bfloat16, device=dev)
         else:
             more["dw_emb"] = torch.empty(self.vocab, H, dtype=f32, device=dev)
+        if self.loss is not None:
+            more["loss"] = torch.empty(self.S, dtype=f32, device=dev)
+            more["dw_out"] = torch.empty(H, self.loss.classes, dtype=f32, device=dev)
+            more.update({k: torch.empty(H, dtype=f32, device=dev) for k in ("dgf", "dbf")})
         if self.ends is not None:
             for n in (1, 2):
                 more.update({"d" + k: torch.empty(H, dtype=f32, device=dev) for k in self.ends.params(n).values()})
@@ -266,8 +328,21 @@ class ChunkedLayer:
             g.update(pre_gamma=out["dg2"], pre_beta=out["db2"])
         return L.block_norm_grads(**g)
 
+    def _ce(self, id_type, scale):
+        """The loss's description; scale: a number, or a device fp32 tensor."""
+        dev = isinstance(scale, torch.Tensor)
+        return L.cross_entropy(self.loss.classes, "bf16", id_type, self.loss.label_smoothing, self.loss.z_loss,
+                               1.0 if dev else scale, scale if dev else None)
+
+    def _ids(self, t, what):
+        """The id type of [S] tokens or targets."""
+        if t.dtype not in (torch.int32, torch.int64) or t.shape != (self.S,) or not t.is_contiguous() \
+                or not t.is_cuda:
+            raise ValueError(f"{what} must be [{self.S}] contiguous int32 or int64 on the device")
+        return "i32" if t.dtype == torch.int32 else "i64"
+
     def step(self, inp, p, out, offload_chunks=None, lookahead=2, poison=False, stream=None, marks=None,
-             ops=None, seed=0, offset=0):
+             ops=None, seed=0, offset=0, loss_scale=None):
         """Forward and backward of the layer over all chunks.  inp: x, dy
         [S, H] bf16 (x's chunk rows are the x planes: offloading a chunk
         makes its rows of x dead, and the prefetch brings them back into the
@@ -280,24 +355,36 @@ class ChunkedLayer:
         vocab, inp holds tokens [S] (int32 or int64) instead of x, p w_emb
         [vocab, H] bf16, and out dw_emb instead of dx; with ends, p their
         parameters (BlockEnds.params) in fp32.  seed, offset: of the step's
-        dropout, which draws at offsets offset .. offset + DROP_STRIDE - 1."""
+        dropout, which draws at offsets offset .. offset + DROP_STRIDE - 1.
+        With a loss, inp holds targets [S] (int32 or int64; outside [0,
+        classes): no target) instead of dy, p w_out [H, classes] bf16 and the
+        last LayerNorm's gf, bf, and out their gradients and loss [S], the rows'
+        losses; loss_scale: the factor of their gradients, a number (1 / S where
+        None) or a device fp32 tensor of one."""
         s = torch.cuda.current_stream() if stream is None else stream
         H, Wt, HqD, HkvD = self.H, self.Wt, self.Hq * self.D, self.Hkv * self.D
         if offload_chunks is None:
             offload_chunks = [] if self.offload == L.SPPO_OFFLOAD_NONE else list(range(self.N - 1))
         offl = set(offload_chunks)
-        self.prepare(offl, lookahead)
-        arena, keep = self.arena, self.keep
-        arena.reset()
-        ends, dy = self.ends, inp["dy"]
+        ends, dy = self.ends, inp["dy"] if self.loss is None else None
         x = inp["x"] if self.vocab is None else None
         drop_p = ends.dropout if ends is not None else 0.0
         if x is None:
             tokens = inp["tokens"]
-            if tokens.dtype not in (torch.int32, torch.int64) or tokens.shape != (self.S,) \
-                    or not tokens.is_contiguous() or not tokens.is_cuda:
-                raise ValueError(f"tokens must be [{self.S}] contiguous int32 or int64 on the device")
-            id_type = "i32" if tokens.dtype == torch.int32 else "i64"
+            id_type = self._ids(tokens, "tokens")
+        if self.loss is not None:
+            targets = inp["targets"]
+            scale = 1.0 / self.S if loss_scale is None else loss_scale
+            if isinstance(scale, torch.Tensor):
+                if scale.dtype != torch.float32 or scale.numel() != 1 or not scale.is_cuda:
+                    raise ValueError("a loss_scale tensor must be one fp32 on the device")
+            elif not L.scale_ok(scale, float("inf")):
+                raise ValueError("loss_scale must be finite")
+            ce = self._ce(self._ids(targets, "targets"), scale)
+
+        self.prepare(offl, lookahead)
+        arena, keep = self.arena, self.keep
+        arena.reset()
 
         def mark(label):
             self.pacer.boundary(s)
@@ -331,9 +418,35 @@ class ChunkedLayer:
         end_bwd = timed("block_norm", L.sppo_block_norm_bwd)
         embed = timed("embedding", L.sppo_embedding_fwd)
         embed_bwd = timed("embedding", L.sppo_embedding_bwd)
+        rotate = timed("rotary", L.sppo_rotary_apply)
+        cross_entropy = timed("loss", L.sppo_cross_entropy)
         drop = lambda site, row0: L.drop_spec(drop_p, seed, offset + site, row0) if drop_p > 0 else None
         lookup = lambda n, c0: embed(n, H, self.vocab, tokens[c0:], p["w_emb"], H, self.embed_scale,
                                      drop(DROP_EMBED, c0), self.x, H, "bf16", id_type, s)
+        def turn(n, c0, q, k, inverse):
+            """q [n, HqD] and rows c0 on of k, in place; dK is in fp32."""
+            if self.rotary is None:
+                return
+            spec = L.rotary(self.rot, self.rot_table, self.rotary.layout, self.rot_amp, self.rotary.position0 + c0)
+            both = [L.rotary_tensor(h, self.D, t, h * self.D, self.D, t, h * self.D, self.D,
+                                    "f32" if t.dtype == torch.float32 else "bf16")
+                    for t, h in ((q, self.Hq), (k[c0:], self.Hkv))]
+            rotate(spec, n, L.rotary_tensors(both), inverse, s)
+
+        def head(n, c0, first):
+            """Chunk i's dy from its loss: logits = LN_f(y) W_out, their gradient
+            in their place."""
+            C, u, y, z = self.loss.classes, self.u[:n], out["y"][c0:c0 + n], self.logits[:n]
+            wacc, add = ("f32", 0) if first else ("acc_f32", 1)
+            ln_fwd(n, H, y, H, p["gf"], p["bf"], self.eps, u, H, self.mf, self.rf, s)
+            gemm("nt", n, C, H, u, H, self.wT["w_out"], H, z, C, stream=s)
+            cross_entropy(ce, n, z, C, targets[c0:], out["loss"][c0:], None, z, C, self.ce_ws, self.ce_ws_bytes, s)
+            gemm("nt", n, H, C, z, C, p["w_out"], C, self.du[:n], H, stream=s)
+            gemm("tn", H, C, n, u, H, z, C, out["dw_out"], C, wacc, stream=s)
+            ln_bwd(n, H, y, H, p["gf"], self.mf, self.rf, self.du[:n], H, self.none, H, self.dy, H, out["dgf"],
+                   out["dbf"], self.ws, self.ws_bytes, accumulate=add, stream=s)
+            return self.dy[:n]
+
         pairs = lambda a: self.chunk_len(a[1]) * self.offsets[a[1]] + self.chunk_len(a[1]) * (self.chunk_len(a[1]) + 1) // 2
         attn_fwd = timed("attn_fwd", L.sppo_attn_fwd_chunk, lambda a: 4 * self.D * self.Hq * pairs(a))
         attn_bwd = timed("attn_bwd", L.sppo_attn_bwd_chunk, lambda a: 10 * self.D * self.Hq * pairs(a))
@@ -343,6 +456,8 @@ class ChunkedLayer:
         transpose(p["w_o"], self.wT["w_o"], HqD, H, s)
         transpose(p["w_1"], self.wT["w_1"], H, 4 * H, s)
         transpose(p["w_2"], self.wT["w_2"], 4 * H, H, s)
+        if self.loss is not None:
+            transpose(p["w_out"], self.wT["w_out"], H, self.loss.classes, s)
         held, back = {}, {}  # chunk -> (region, views): not offloaded / prefetched
         for i in range(self.N):
             mark(("fwd", i))
@@ -356,6 +471,7 @@ class ChunkedLayer:
             gemm("nt", n, HqD, H, u, H, wq, H, v["q"], HqD, stream=s)
             gemm("nt", n, HkvD, H, u, H, wq[HqD:], H, self.k[c0:], HkvD, stream=s)
             gemm("nt", n, HkvD, H, u, H, wq[HqD + HkvD:], H, self.v[c0:], HkvD, stream=s)
+            turn(n, c0, v["q"], self.k, 0)
             attn_fwd(self.ctx, i, v["q"], self.k, self.v, v["o"], v["lse"], s)
             if ends is None:
                 gemm("nt", n, H, HqD, v["o"], HqD, self.wT["w_o"], HqD, v["h"], H, "add_bf16", v["x"], H, stream=s)
@@ -421,7 +537,7 @@ class ChunkedLayer:
             wacc = "f32" if first else "acc_f32"
             u, z, g = self.u[:n], self.z[:n], self.g[:n]
             da, dz, dh, dO = self.da[:n], self.dz[:n], self.dh[:n], self.dO[:n]
-            dyi = dy[c0:c0 + n]
+            dyi = dy[c0:c0 + n] if self.loss is None else head(n, c0, first)
             add = 0 if first else 1
             dres, dbr = dyi, dyi  # gradients of h (along the stream) and of the MLP's output
             if ends is not None:
@@ -453,6 +569,7 @@ class ChunkedLayer:
             attn_bwd(self.ctx, i, v["q"], self.k, self.v, v["o"], v["lse"], dO, self.dq[:n],
                                   self.dk, self.dv, s)
             # q, k, v = u W_qkv (chunk i's dK/dV rows are complete now)
+            turn(n, c0, self.dq[:n], self.dk, 1)
             dqkv = self.dqkv[:n]
             pack(n, HqD, HkvD, self.dq[:n], self.dk, self.dv, c0, dqkv, s)
             if x is None:

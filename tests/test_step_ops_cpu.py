@@ -77,6 +77,28 @@ def test_eight_bit_format_and_rounding():
     assert (codes == 1).all()
 
 
+def test_layer_step_gradients_by_differences():
+    r = np.random.RandomState(3)
+    hq, hkv, d, S, C = 2, 1, 8, 5, 11
+    H = hq * d
+    shapes = dict(w_qkv=(H, (hq + 2 * hkv) * d), w_o=(H, H), w_1=(H, 4 * H), w_2=(4 * H, H), w_out=(H, C), g1=H, b1=H,
+                  g2=H, b2=H, gf=H, bf=H)
+    p = {k: r.randn(*(v if isinstance(v, tuple) else (v,))) * (0.3 if k[0] == "w" else 1.0) for k, v in shapes.items()}
+    x, t = r.randn(S, H), np.array([3, -1, 10, 0, 3])
+    rope = dict(rot=8, layout="interleaved", freqs=O.rope_freqs(8)[0], amp=1.1, position0=7)
+    run = lambda x, p: O.layer_step(x, p, hq, hkv, d, rope, t, 0.1, 0.01, 0.2)  # noqa: E731
+    out = run(x, p)
+    f = lambda x, p: 0.2 * run(x, p)["loss"].sum()  # noqa: E731
+    for name in ["x", *p]:
+        v = x if name == "x" else p[name]
+        for i in r.choice(v.size, 4, replace=False):
+            h = np.zeros(v.size)
+            h[i] = 1e-5
+            h = h.reshape(v.shape)
+            d2 = (f(x + h, p) - f(x - h, p)) if name == "x" else (f(x, {**p, name: v + h}) - f(x, {**p, name: v - h}))
+            assert np.isclose(out["d" + name].ravel()[i], d2 / 2e-5, rtol=1e-5, atol=1e-8), (name, i)
+
+
 # --------------------------------------------------------------- host functions
 @pytest.mark.parametrize("rot", [8, 24, 128, 1024])
 @pytest.mark.parametrize("kw", [dict(), dict(base=500000.0), dict(scaling="linear", factor=4.0),
@@ -308,3 +330,28 @@ def test_struct_layouts_match_c():
     assert ctypes.sizeof(L.sppo_rope) == 56 and ctypes.sizeof(L.sppo_ce) == 40
     assert ctypes.sizeof(L.sppo_opt_tensor) == 80 and ctypes.sizeof(L.sppo_opt_list) == 24
     assert ctypes.sizeof(L.sppo_adamw) == 72
+
+
+def test_layer_refuses_before_the_device():
+    """What the layer's options say for themselves."""
+    from paper_2503_10377_amd.chunked_layer import Loss, Rotary
+    from paper_2503_10377_amd.optimizer import AdamW
+    import torch
+
+    for kw in (dict(layout="spiral"), dict(position0=-1), dict(position0=2 ** 62)):
+        with pytest.raises(ValueError):
+            Rotary(**kw)
+    with pytest.raises(ValueError):
+        Rotary(rot=128).table(64, "cpu")
+    with pytest.raises(L.SppoError):
+        Rotary(rot=20).table(64, "cpu")
+    rot, table, amp = Rotary(base=500000.0).table(64, "cpu")
+    assert rot == 64 and table.shape == (32,) and amp == 1.0
+    for a in ((0,), (100,), (2 ** 31,), (256, -0.1), (256, 0.0, -1.0), (256, 0.0, float("nan"))):
+        with pytest.raises(ValueError):
+            Loss(*a)
+    w = torch.zeros(4)
+    for params, grads, kw in (({}, {}, {}), ({"a": w}, {"b": w}, {}), ({"a": w}, {"a": w}, {}),
+                              ({"a": w}, {"a": w}, dict(state="f16")), ({"a": w}, {"a": w}, dict(max_norm=0.0))):
+        with pytest.raises(ValueError):
+            AdamW(params, grads, 1e-3, **kw)
