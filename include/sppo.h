@@ -637,7 +637,8 @@ typedef struct {
  * with rows and heads apart from each other (hs >= head_dim and ld >= (heads
  * - 1) hs + head_dim, or ld >= head_dim and hs >= (rows - 1) ld + head_dim);
  * pointers 16-byte aligned.  y may be x with the same ld and hs; no other
- * overlap, also not between tensors of a call. */
+ * overlap, also not between tensors of a call (INVALID_ARG where a y is another
+ * tensor's x or y). */
 typedef struct {
   sppo_dtype dtype;
   int32_t heads, head_dim;
@@ -746,7 +747,7 @@ typedef struct {
  * caller to device memory (16-byte aligned) whose address it writes into
  * `table`; list and table live as long as their calls run.  INVALID_ARG where
  * a buffer that is written overlaps another of the list (a tensor listed twice;
- * gradients may be shared).  At most 2^20 tensors and 2^31 - 1 tiles of 4096
+ * gradients may be shared).  At most 2^20 tensors and 2^24 - 1 tiles of 4096
  * elements (UNSUPPORTED above). */
 typedef struct {
   const void* table;
@@ -761,7 +762,7 @@ sppo_status sppo_opt_list_make(int32_t n_tensors, const sppo_opt_tensor* tensors
 /* out (device fp32 [2]) = { norm, min(1, max_norm / norm) }, norm = the root of
  * the sum of the squares of all gradients, summed in fp64 in a fixed order (the
  * same bits every time).  max_norm > 0; infinity: the factor is 1.  A norm of
- * infinity or NaN has the factor 0.  steps: NULL, or a device int64 that is
+ * infinity (or past fp32's range) or NaN has the factor 0.  steps: NULL, or a device int64 that is
  * increased by one unless the norm is infinite or NaN.  workspace:
  * sppo_grad_norm_workspace bytes, 16-byte aligned. */
 size_t sppo_grad_norm_workspace(const sppo_opt_list* list);
@@ -783,7 +784,8 @@ sppo_status sppo_grad_norm(const sppo_opt_list* list, float max_norm, float* out
  * high, t low, high) and key seed, its low half for m, its high half for r.
  * Values that are infinite or NaN are kept as NaN, a v below 2^-126 as zero. */
 typedef struct {
-  double lr, beta1, beta2, eps;  /* finite; 0 <= beta < 1; eps >= 0         */
+  double lr, beta1, beta2, eps;  /* lr finite; 0 <= beta < 1; eps > 0, a
+                                    normal fp32 number                      */
   int64_t step;
   const int64_t* step_dev;
   const float* norm;

@@ -138,7 +138,7 @@ class Loss:
     def __init__(self, classes, label_smoothing=0.0, z_loss=0.0):
         if not 0 < classes < 2 ** 31 or classes % 256:
             raise ValueError("classes must be a multiple of 256 below 2^31")
-        if not 0.0 <= label_smoothing <= 1.0 or not 0.0 <= z_loss < float("inf"):
+        if not 0.0 <= label_smoothing <= 1.0 or not z_loss >= 0.0 or not L.scale_ok(z_loss, float("inf")):
             raise ValueError("label_smoothing must be in [0, 1], z_loss finite and not negative")
         self.classes, self.label_smoothing, self.z_loss = classes, label_smoothing, z_loss
 

@@ -403,9 +403,15 @@ hipError_t launch_parts(const CeArgs& a, hipStream_t stream) {
 template <typename T, int TEAM, int K, bool PAST>
 hipError_t launch_row(const CeArgs& a, hipStream_t stream) {
   constexpr int ROWS = TEAM < 256 ? 256 / TEAM : 1;
-  hipLaunchKernelGGL((ce_row_kernel<T, TEAM, K, PAST>), dim3((uint32_t)((a.rows + ROWS - 1) / ROWS)),
-                     dim3(TEAM * ROWS), 0, stream, a);
-  return hipGetLastError();
+  constexpr int64_t step = kMaxWaves / (TEAM / 64);
+  for (int64_t r = 0; r < a.rows; r += step) {
+    const CeArgs b = rows_from(a, r, std::min(step, a.rows - r));
+    hipLaunchKernelGGL((ce_row_kernel<T, TEAM, K, PAST>), dim3((uint32_t)((b.rows + ROWS - 1) / ROWS)),
+                       dim3(TEAM * ROWS), 0, stream, b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, bool PAST>
@@ -426,7 +432,7 @@ hipError_t launch_loss(const CeArgs& a, hipStream_t stream) {
 template <typename T, int K, bool PAST>
 hipError_t launch_bwd(const CeArgs& a, hipStream_t stream) {
   constexpr int E = 64 * K * Piece<T>::N;
-  const int64_t parts = (a.V + E - 1) / E, step = ((int64_t)1 << 30) / parts;
+  const int64_t parts = (a.V + E - 1) / E, step = kMaxWaves / parts;
   const FastDiv by_parts = fast_divisor((uint32_t)parts);
   for (int64_t r = 0; r < a.rows; r += step) {
     const CeArgs b = rows_from(a, r, std::min(step, a.rows - r));

@@ -178,8 +178,7 @@ hipError_t launch(RotaryArgs a, hipStream_t stream) {
     t.chunk0 = (int)chunks;
     chunks += (t.items + 63) / 64;
   }
-  // Waves of a launch index as numbers below 2^31 (fast_div).
-  const int64_t rows_per = ((int64_t)1 << 30) / chunks;
+  const int64_t rows_per = kMaxWaves / chunks;
   const FastDiv by_chunks = fast_divisor((uint32_t)chunks);
   const size_t lds = (size_t)kWaves * a.rot * sizeof(float);
   const int64_t rows = a.rows;

@@ -323,6 +323,9 @@ size_t embedding_workspace(int64_t rows, int H);
 hipError_t launch_embedding_fwd(const EmbedArgs& a, hipStream_t stream);
 hipError_t launch_embedding_bwd(const EmbedArgs& a, hipStream_t stream);
 
+// Waves of a launch: a grid counts its threads in 32 bits.
+constexpr int64_t kMaxWaves = (int64_t)1 << 25;
+
 // Rotary positions of 1 to 4 tensors (rotary.hip).  A wave takes 64 consecutive
 // items of one row of one tensor, an item being two pieces of a head that are
 // turned with each other's angles, or copied.

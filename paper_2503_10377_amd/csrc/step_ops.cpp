@@ -85,7 +85,7 @@ sppo_status ce_args(const sppo_ce* ce, int64_t rows, const void* logits, int64_t
 
 // ---------------------------------------------------------------- parameters
 constexpr int32_t kMaxTensors = 1 << 20;
-constexpr int64_t kMaxTiles = INT32_MAX;
+constexpr int64_t kMaxTiles = ((int64_t)1 << 24) - 1;  // a workgroup of 256 each: 32 bits of threads
 
 int64_t tiles_of(int64_t n) { return n / sppo::kOptTile + (n % sppo::kOptTile != 0); }
 int64_t blocks_of(int64_t n) { return n / 32 + (n % 32 != 0); }
@@ -199,6 +199,9 @@ sppo_status sppo_rotary_apply(const sppo_rotary* spec, int64_t rows, int32_t inv
     o.y = t.y; o.ldy = t.ldy; o.hsy = t.hsy;
     o.heads = t.heads; o.D = t.head_dim;
     o.f32 = t.dtype == SPPO_F32;
+    for (int k = 0; k < i; ++k)
+      if (t.y == tensors[k].y || t.y == tensors[k].x || t.x == tensors[k].y)
+        return fail(SPPO_ERR_INVALID_ARG, "rotary: a tensor is written and used by another one of the call");
   }
   if (rows == 0) return SPPO_OK;
   a.rows = rows;
@@ -294,7 +297,7 @@ sppo_status sppo_opt_list_make(int32_t n_tensors, const sppo_opt_tensor* tensors
   for (int32_t i = 0; i < n_tensors; ++i)
     if (tensors[i].n < 0) return fail(SPPO_ERR_INVALID_ARG, "optimizer: a tensor of negative size");
   const int64_t tiles = count_tiles(n_tensors, tensors);
-  if (tiles < 0) return fail(SPPO_ERR_UNSUPPORTED, "optimizer: more than 2^20 tensors or 2^31 - 1 tiles");
+  if (tiles < 0) return fail(SPPO_ERR_UNSUPPORTED, "optimizer: more than 2^20 tensors or 2^24 - 1 tiles");
   if (!aligned(host_table, 8) || bytes < list_bytes(n_tensors, tiles))
     return fail(SPPO_ERR_INVALID_ARG, "optimizer: the table is misaligned or too small");
   try {
@@ -359,8 +362,9 @@ sppo_status sppo_adamw_step(const sppo_opt_list* list, const sppo_adamw* w, void
   if (st != SPPO_OK) return st;
   if (list->state == SPPO_STATE_NONE) return fail(SPPO_ERR_INVALID_ARG, "adamw: the list has gradients only");
   if (!w || !std::isfinite((float)w->lr) || !(w->beta1 >= 0.0) || !(w->beta1 < 1.0) || !(w->beta2 >= 0.0) ||
-      !(w->beta2 < 1.0) || !(w->eps >= 0.0) || !std::isfinite((float)w->eps))
-    return fail(SPPO_ERR_INVALID_ARG, "adamw: lr or eps not finite, eps negative, or a beta outside [0, 1)");
+      !(w->beta2 < 1.0) || !((float)w->eps > 0.f) || !std::isnormal((float)w->eps))
+    return fail(SPPO_ERR_INVALID_ARG,
+                "adamw: lr not finite, eps not positive and a normal number, or a beta outside [0, 1)");
   if (!w->step_dev && w->step < 1) return fail(SPPO_ERR_INVALID_ARG, "adamw: step below 1");
   if (!aligned(w->step_dev, 8) || !aligned(w->norm, 4) || !aligned(w->lr_dev, 4))
     return fail(SPPO_ERR_INVALID_ARG, "adamw: a misaligned pointer");

@@ -34,6 +34,8 @@ class AdamW:
             raise ValueError(f"unknown state {state!r}")
         if max_norm is not None and not max_norm > 0:
             raise ValueError("max_norm must be positive")
+        if not all(0.0 <= b < 1.0 for b in betas) or not eps > 0.0:
+            raise ValueError("betas must be in [0, 1), eps positive")
         device = next(iter(params.values())).device
         for name, p in params.items():
             g = grads[name]
@@ -75,6 +77,8 @@ class AdamW:
         dev = isinstance(lr, torch.Tensor)
         if dev and (lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self.device):
             raise ValueError("an lr tensor must be one fp32 on the parameters' device")
+        if not dev and not L.scale_ok(lr, float("inf")):
+            raise ValueError("lr must be finite")  # before the norm's call counts the step
         with torch.cuda.device(self.device):
             L.sppo_grad_norm(self.list, float("inf") if self.max_norm is None else self.max_norm, self.norm, self.ws,
                              self.ws_bytes, self.steps, stream)

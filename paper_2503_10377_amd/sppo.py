@@ -717,12 +717,12 @@ def sppo_rotary_freqs(rot, base=10000.0, scaling="none", factor=1.0, original_le
                       inv_freq=None):
     """([rot / 2] integers of a rotary spec's table, to be put on the device as
     64-bit numbers, and its amplitude)."""
-    n = max(int(rot) // 2, 1)
+    n = min(max(int(rot) // 2, 1), 512)  # more is refused
     given = None
     if inv_freq is not None:
         if len(inv_freq) != int(rot) // 2:
             raise ValueError("inv_freq needs one value per pair")
-        given = (ctypes.c_double * n)(*[float(f) for f in inv_freq])
+        given = (ctypes.c_double * len(inv_freq))(*[float(f) for f in inv_freq])
     r = sppo_rope(ROPE_SCALINGS.get(scaling, scaling), base, factor, original_len, beta_fast, beta_slow, given)
     out, amp = (ctypes.c_uint64 * n)(), ctypes.c_float()
     _context_free(lib().sppo_rotary_freqs(rot, ctypes.byref(r), out, ctypes.byref(amp)))

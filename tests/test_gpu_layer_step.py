@@ -25,6 +25,7 @@ from parity import to_np
 
 pytestmark = pytest.mark.gpu
 REL, MAXREL = 1.2e-2, 1.5e-2
+INF = float("inf")
 
 
 def announce(msg):
@@ -301,6 +302,7 @@ def test_optimizer_refuses():
     with pytest.raises(ValueError):
         AdamW(p, g, 1e-3, lr_scale={"v": 1.0})
     o = AdamW(p, g, 1e-3)
-    for lr in (torch.ones(1), torch.ones(2, device="cuda"), torch.ones(1, device="cuda").double()):
+    for lr in (torch.ones(1), torch.ones(2, device="cuda"), torch.ones(1, device="cuda").double(), INF, float("nan")):
         with pytest.raises(ValueError):
             o.step(lr)
+    assert o.steps.item() == 0

@@ -292,6 +292,77 @@ def test_cross_entropy_of_masked_logits(V, dtype):
     assert loss[1] == INF and loss[2] == INF and loss[5] == 0 and torch.isfinite(loss[0])
 
 
+@pytest.mark.parametrize("V,dtype", [(100, "bf16"), (50000, "f32"), (140000, "bf16")])
+def test_cross_entropy_of_infinite_logits(V, dtype):
+    """A logit of +inf: lse and the loss of any other target are +inf, its own
+    gradient is NaN, the others' is the formula's at probability zero."""
+    announce(f"cross entropy of +inf V={V} {dtype}")
+    ld = (V + 7) // 8 * 8
+    x, t = ce_inputs(2, V, ld, dtype, 3, scale=100.0)
+    x[:, V // 3] = INF
+    t[0], t[1] = 5, V // 3
+    loss, lse, dx = run_ce(L.cross_entropy(V, dtype, scale=2.0), 2, x.cuda(), ld, t.cuda(), dtype)
+    assert torch.all(lse == INF) and loss[0] == INF and torch.isnan(loss[1])
+    want = torch.zeros(2, V)
+    want[0, 5] = -2.0
+    want[:, V // 3] = NAN
+    within(dx[:, :V], to_np(want), 0.0, "dx")
+
+
+def test_calls_past_32_bit_offsets():
+    """Rows and elements whose offsets pass 2^32, in a buffer that is touched at
+    few places."""
+    announce("offsets past 2^32")
+    rows, ld = 4100, 1 << 20
+    buf = torch.empty(rows * ld, dtype=BF, device="cuda").view(rows, ld)
+    freqs, dev, amp = table(64)
+    x = randn((rows, 64), 1).to(BF)
+    buf[:, :64] = x.cuda()
+    L.sppo_rotary_apply(L.rotary(64, dev, "half", amp), rows,
+                        L.rotary_tensors([L.rotary_tensor(1, 64, buf, ld, 64, buf, ld, 64)]))
+    rotary_check(buf[:, :64].reshape(rows, 1, 64), x.reshape(rows, 1, 64), range(rows), freqs, 64, "half", amp, 0,
+                 "bf16", "y")
+    for V in (100, 40001):
+        n = rows if V == 100 else 4100
+        x, t = ce_inputs(n, V, V + 7 & ~7, "bf16", 2)
+        buf[:n, :x.shape[1]] = x.cuda()
+        pick = [0, 1, n - 2, n - 1]
+        loss, lse, _ = run_ce(L.cross_entropy(V), n, buf, ld, t.cuda(), "bf16", in_place=True)
+        sub, tt = to_np(x)[pick][:, :V], t.numpy()[pick]
+        ref = O.cross_entropy(sub, tt)
+        tol = ce_tol(sub, tt, V, ref, 0.0, 0.0, 1.0, "bf16")
+        within(loss[pick], ref[0], tol[0], "loss")
+        within(buf[pick][:, :V], ref[2], tol[2], "dx")
+        buf[:n, :x.shape[1]] = x.cuda()
+        L.sppo_cross_entropy_bwd(L.cross_entropy(V), n, buf, ld, t.cuda(), lse, None, buf, ld)
+        within(buf[pick][:, :V], ref[2], tol[2] + 8 * U * np.abs(ref[1])[:, None], "dx from lse")
+
+
+def test_calls_past_a_launch():
+    """More rows than one launch takes (2^25 waves): rows at both sides of the
+    border and at the end."""
+    rows = (1 << 25) + 5
+    announce("calls past a launch")
+    pick = torch.tensor([0, 1, 2 ** 25 - 1, 2 ** 25, 2 ** 25 + 1, rows - 1])
+    x = torch.randn(rows, 8, device="cuda").to(BF)
+    freqs, dev, amp = table(8)
+    y = torch.empty_like(x)
+    L.sppo_rotary_apply(L.rotary(8, dev, "half", amp, 3), rows,
+                        L.rotary_tensors([L.rotary_tensor(1, 8, x, 8, 8, y, 8, 8)]))
+    rotary_check(y[pick].reshape(-1, 1, 8), x[pick].reshape(-1, 1, 8), (pick + 3).tolist(), freqs, 8, "half", amp, 0,
+                 "bf16", "y")
+    t = torch.randint(0, 7, (rows,), device="cuda", dtype=torch.int32)
+    ce = L.cross_entropy(7, id_type="i32")
+    loss, lse, dx = run_ce(ce, rows, x, 8, t, "bf16")
+    sub, tt = to_np(x[pick])[:, :7], t[pick].cpu().numpy()
+    ref = O.cross_entropy(sub, tt)
+    tol = ce_tol(sub, tt, 7, ref, 0.0, 0.0, 1.0, "bf16")
+    within(loss[pick], ref[0], tol[0], "loss")
+    within(dx[pick][:, :7], ref[2], tol[2], "dx")
+    L.sppo_cross_entropy_bwd(ce, rows, x, 8, t, lse, None, dx, 8)
+    within(dx[pick][:, :7], ref[2], tol[2] + 8 * U * np.abs(ref[1])[:, None], "dx from lse")
+
+
 def test_cross_entropy_gradient_matches_differences():
     """Central differences of the fp32 loss: steps of 2^-4 have a third-order
     error of h^2/6 max|loss'''| (below 1, with z's 2 (3 z) added), and the two losses' roundings over
@@ -515,6 +586,28 @@ def test_adamw_counts_and_schedules_on_the_device():
     L.sppo_adamw_step(a.list, L.adamw(1e-2, step=1))
     for n in a.buf:
         assert torch.equal(a.buf[n], b.buf[n]), n
+
+
+def test_an_update_past_32_bit_offsets():
+    """One tensor of 2^32 + 37 elements: the norm of gradients at its ends, and the
+    update there."""
+    announce("update past 2^32 elements")
+    n = 2 ** 32 + 37
+    g = torch.zeros(n, dtype=BF, device="cuda")
+    w = torch.ones(n, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ms, vs = (torch.zeros(n // 32 + 1, dtype=torch.uint8, device="cuda") for _ in range(2))
+    ends = torch.tensor([0, 5, 2 ** 32 - 1, 2 ** 32, n - 3, n - 1], device="cuda")
+    g[ends] = torch.tensor([1.0, -2.0, 3.0, -4.0, 5.0, -6.0], device="cuda", dtype=BF)
+    lst = L.opt_list([L.opt_tensor(n, g, "bf16", w, "f32", None, m, v, ms, vs)], "e4m3")
+    out, ws = torch.empty(2, device="cuda"), torch.empty(L.sppo_grad_norm_workspace(lst), dtype=torch.uint8, device="cuda")
+    L.sppo_grad_norm(lst, INF, out, ws, ws.numel())
+    assert abs(out[0].item() - 91 ** 0.5) <= U * 91 ** 0.5 * 1.01
+    L.sppo_adamw_step(lst, L.adamw(0.5, 0.9, 0.99, 1e-8, 1))
+    # The first step goes lr against the gradient's sign: 16 roundings of one, and eps / |g|.
+    assert torch.all((w[ends] - 1.0 + 0.5 * torch.sign(g[ends].float())).abs() <= 16 * U + 1e-8)
+    w[ends] = 1.0
+    assert torch.all(w == 1.0) and int((m != 0).sum()) == len(ends) and int((v != 0).sum()) == len(ends)
 
 
 @pytest.mark.parametrize("state", ["f32", "e4m3"])

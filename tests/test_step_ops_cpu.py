@@ -199,7 +199,7 @@ def change(ts, i, **kw):
     (lambda: (lambda t: change(t, 0, m=t[1].param))(tensors([8, 8])), BAD),
     (lambda: (lambda t: change(t, 0, v=t[0].m + 16))(tensors([8])), BAD),  # v inside m
     (lambda: (lambda t: change(t, 0, grad=t[1].master))(tensors([8, 8])), BAD),
-    (lambda: change(tensors([8, 8]), 1, n=2 ** 43), UNS),
+    (lambda: change(tensors([8, 8]), 1, n=2 ** 36), UNS),
 ])
 def test_opt_list_refuses(build, status):
     with pytest.raises(L.SppoError) as e:
@@ -242,6 +242,7 @@ def rot_call(spec=None, t=None, rows=4, inverse=0, n=1, **over):
     (dict(spec=dict(layout=2)), BAD), (dict(spec=dict(freqs=None)), BAD), (dict(spec=dict(freqs=P + 4)), BAD),
     (dict(spec=dict(amp=float("nan"))), BAD), (dict(spec=dict(positions=P + 4)), BAD),
     (dict(spec=dict(id_type=4)), BAD), (dict(rows=-1), BAD), (dict(inverse=2), BAD), (dict(n=5), BAD),
+    (dict(n=2), BAD),                            # the same tensor twice
     (dict(t=dict(dtype=3)), BAD), (dict(t=dict(heads=0)), BAD), (dict(t=dict(head_dim=20)), BAD),
     (dict(t=dict(head_dim=1032, hsx=1032, hsy=1032, ldx=4096, ldy=4096)), UNS),
     (dict(t=dict(heads=65536, ldx=2 ** 30, ldy=2 ** 30)), UNS),
@@ -307,7 +308,7 @@ def test_update_refuses():
         L.sppo_adamw_step(lst, L.adamw(1e-3), stream=0)
     lst.table = P
     for kw in (dict(lr=float("nan")), dict(lr=1e300), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=-1.0),
-               dict(eps=float("inf")), dict(step=0), dict(step_dev=P + 4), dict(norm=P + 2), dict(lr_dev=P + 2)):
+               dict(eps=0.0), dict(eps=1e-40), dict(eps=float("inf")), dict(step=0), dict(step_dev=P + 4), dict(norm=P + 2), dict(lr_dev=P + 2)):
         with pytest.raises(L.SppoError) as e:
             L.sppo_adamw_step(lst, L.adamw(**{"lr": 1e-3, **kw}), stream=0)
         assert e.value.status == BAD, kw
@@ -347,11 +348,12 @@ def test_layer_refuses_before_the_device():
         Rotary(rot=20).table(64, "cpu")
     rot, table, amp = Rotary(base=500000.0).table(64, "cpu")
     assert rot == 64 and table.shape == (32,) and amp == 1.0
-    for a in ((0,), (100,), (2 ** 31,), (256, -0.1), (256, 0.0, -1.0), (256, 0.0, float("nan"))):
+    for a in ((0,), (100,), (2 ** 31,), (256, -0.1), (256, 0.0, -1.0), (256, 0.0, float("nan")), (256, 0.0, 1e39)):
         with pytest.raises(ValueError):
             Loss(*a)
     w = torch.zeros(4)
     for params, grads, kw in (({}, {}, {}), ({"a": w}, {"b": w}, {}), ({"a": w}, {"a": w}, {}),
-                              ({"a": w}, {"a": w}, dict(state="f16")), ({"a": w}, {"a": w}, dict(max_norm=0.0))):
+                              ({"a": w}, {"a": w}, dict(state="f16")), ({"a": w}, {"a": w}, dict(max_norm=0.0)),
+                              ({"a": w}, {"a": w}, dict(betas=(0.9, 1.0))), ({"a": w}, {"a": w}, dict(eps=0.0))):
         with pytest.raises(ValueError):
             AdamW(params, grads, 1e-3, **kw)
