@@ -26,6 +26,9 @@ def _f64(x):
 
 
 # ------------------------------------------------------------------- rotary
+PI = np.longdouble("3.14159265358979323846264338327950288")
+
+
 def rope_freqs(rot, base=10000.0, kind="none", factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0):
     """Angles per position [rot / 2] (long double) and the amplitude."""
     ld = np.longdouble
@@ -35,7 +38,7 @@ def rope_freqs(rot, base=10000.0, kind="none", factor=1.0, original_len=0.0, bet
     if kind == "linear":
         f = f / s
     if kind == "yarn":
-        turns = original_len * f / (2 * ld("3.14159265358979323846264338327950288"))
+        turns = original_len * f / (2 * PI)
         c = np.clip((turns - beta_slow) / ld(beta_fast - beta_slow), 0, 1)
         f = c * f + (1 - c) * f / s
     return f, 0.1 * math.log(factor) + 1.0 if kind == "yarn" else 1.0
@@ -48,7 +51,7 @@ def rotary(x, pos, freqs, rot, layout, amp=1.0, inverse=False):
     if isinstance(freqs[0], (int, np.uint64)):
         turns = np.array([[(int(p) * int(f)) % 2 ** 64 / 2.0 ** 64 for f in freqs] for p in pos])
     else:
-        t = np.asarray(pos).astype(np.longdouble)[:, None] * (freqs / (2 * np.longdouble("3.14159265358979323846264338327950288")))
+        t = np.asarray(pos).astype(np.longdouble)[:, None] * (freqs / (2 * PI))
         turns = (t - np.floor(t)).astype(np.float64)
     w = 2 * math.pi * turns * (-1.0 if inverse else 1.0)
     c, s = amp * np.cos(w)[:, None, :], amp * np.sin(w)[:, None, :]
@@ -170,7 +173,8 @@ def layer_step(x, p, hq, hkv, d, rope, targets, smooth=0.0, z=0.0, scale=1.0, en
                 pre_gamma=w["g2"], pre_beta=w["b2"]) for n in (1, 2)]
     keep = [np.ones(x.shape) * k for k in keep]
     pos = np.arange(S) + rope["position0"]
-    turn = lambda t, inv: rotary(t[0], pos, rope["freqs"], rope["rot"], rope["layout"], rope["amp"], inv)[None]  # noqa: E731
+    how = (rope["freqs"], rope["rot"], rope["layout"], rope["amp"])
+    turn = lambda t, inv: rotary(t[0], pos, *how, inv)[None]  # noqa: E731
     u, m1, r1 = layer_norm(x, w["g1"], w["b1"], eps)
     split = np.split(u @ w["w_qkv"], [hq * d, (hq + hkv) * d], axis=1)
     q, k, v = (t.reshape(1, S, n, d) for t, n in zip(split, (hq, hkv, hkv)))

@@ -1,6 +1,13 @@
 // Rotary positions: the pairs of a head turned by an angle that grows with the
 // row's position, for the queries and keys of a chunk in one launch; turned
 // the other way it is the gradient.
+//
+// HBM-bound: 8192 rows of 32 + 32 heads of 128 bf16, on new data every time, in
+// 47.5 us, 5.65 TB/s (16384 rows 89 us, 6.0); with 3001 rows of 32 bf16 and 8
+// fp32 heads, half of each turned, 12.8 us.  A wave makes its row's angles once
+// (a pair a lane) and turns one item a lane with them: with four items a lane the
+// angles cost a quarter, but fewer waves' loads are on their way (52 us), and
+// with the loads behind the table 48.
 #include "row_common.h"
 
 namespace sppo {
@@ -205,7 +212,10 @@ hipError_t launch(RotaryArgs a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
-  // Pieces of 16 bytes where bf16 tensors divide into pairs of them.
+  // Pieces of 16 bytes where bf16 tensors divide into pairs of them, else of 8
+  // (24 of 128 turned: 55 us where the whole head takes 47.5).  Large tensors are
+  // read past the caches, but written through them, as the attention reads them
+  // next.
   bool wide = true, past = false;
   for (int k = 0; k < a.n; ++k) {
     const RotaryTensor& t = a.t[k];

@@ -185,7 +185,8 @@ sppo_status sppo_rotary_apply(const sppo_rotary* spec, int64_t rows, int32_t inv
   for (int i = 0; i < n_tensors; ++i) {
     const sppo_rotary_tensor& t = tensors[i];
     if (!dtype_ok(t.dtype) || t.heads < 1 || t.head_dim < 8 || t.head_dim % 8 || t.head_dim < spec->rot)
-      return fail(SPPO_ERR_INVALID_ARG, "rotary: unknown dtype, no heads, or head_dim not a multiple of 8 of at least rot");
+      return fail(SPPO_ERR_INVALID_ARG,
+                  "rotary: unknown dtype, no heads, or head_dim not a multiple of 8 of at least rot");
     if (t.head_dim > sppo::kRotaryMaxDim || t.heads > 65535)
       return fail(SPPO_ERR_UNSUPPORTED, "rotary: head_dim above 1024 or more than 65535 heads");
     if (!t.x || !t.y || !aligned(t.x, 16) || !aligned(t.y, 16))

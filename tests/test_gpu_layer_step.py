@@ -158,7 +158,8 @@ def test_layer_step_refuses():
     for bad in (t[:255], t.to(torch.int16), t.repeat(2)[::2], inp["targets"]):
         with pytest.raises(ValueError):
             lay.step({"x": x, "targets": bad}, dp, out)
-    for bad in (float("inf"), float("nan"), torch.ones(2, device="cuda"), torch.ones(1), torch.ones(1, device="cuda").double()):
+    for bad in (float("inf"), float("nan"), torch.ones(2, device="cuda"), torch.ones(1),
+                torch.ones(1, device="cuda").double()):
         with pytest.raises(ValueError):
             lay.step({"x": x, "targets": t}, dp, out, loss_scale=bad)
     lay.close()
