@@ -747,7 +747,7 @@ typedef struct {
  * caller to device memory (16-byte aligned) whose address it writes into
  * `table`; list and table live as long as their calls run.  INVALID_ARG where
  * a buffer that is written overlaps another of the list (a tensor listed twice;
- * gradients may be shared).  At most 2^20 tensors and 2^24 - 1 tiles of 4096
+ * gradients may be shared).  At most 2^20 tensors and 2^24 - 1 tiles of 2048
  * elements (UNSUPPORTED above). */
 typedef struct {
   const void* table;

@@ -90,47 +90,75 @@ __device__ __forceinline__ double block_sum64(double v, double* lds) {
   return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// Of n <= kOptTile elements.  Squares of fp32 numbers are exact in fp64, and
-// their sum neither overflows nor loses small gradients.
-template <typename T, bool PAST>
-__device__ __forceinline__ double tile_squares(const T* g, int n) {
-  constexpr int N = 16 / (int)sizeof(T), K = kOptTile / (N * kThreads);
+// A tile's n <= kOptTile gradients.  Squares of fp32 numbers are exact in fp64,
+// and their sum neither overflows nor loses small gradients.
+template <typename T>
+struct TileSquares {
+  static constexpr int N = 16 / (int)sizeof(T), K = kOptTile / (N * kThreads);
   Vec<T, N> x[K];
+  T rest;
+  template <bool PAST>
+  __device__ __forceinline__ void load(const T* g, int n) {
 #pragma unroll
-  for (int u = 0; u < K; ++u) {
-    const int e = N * (kThreads * u + threadIdx.x);
-    if (e + N <= n) load_vec<PAST>(x[u], g + e);
+    for (int u = 0; u < K; ++u) {
+      const int e = N * (kThreads * u + threadIdx.x);
+      if (e + N <= n) load_vec<PAST>(x[u], g + e);
+    }
+    const int e = n / N * N + threadIdx.x;
+    if (e < n) rest = g[e];
   }
-  double s[2] = {0.0, 0.0};
+  __device__ __forceinline__ double sum(int n) const {
+    double s[2] = {0.0, 0.0};
 #pragma unroll
-  for (int u = 0; u < K; ++u) {
-    const int e = N * (kThreads * u + threadIdx.x);
-    if (e + N > n) continue;
-    float f[N];
-    x[u].get(f);
+    for (int u = 0; u < K; ++u) {
+      const int e = N * (kThreads * u + threadIdx.x);
+      if (e + N > n) continue;
+      float f[N];
+      x[u].get(f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) s[i & 1] += (double)f[i] * f[i];
+      for (int i = 0; i < N; ++i) s[i & 1] += (double)f[i] * f[i];
+    }
+    if (n / N * N + (int)threadIdx.x < n) {
+      const double f = load1(&rest);
+      s[0] += f * f;
+    }
+    return s[0] + s[1];
   }
-  const int e = n / N * N + threadIdx.x;
-  if (e < n) {
-    const double f = load1(g + e);
-    s[0] += f * f;
-  }
-  return s[0] + s[1];
-}
+};
 
-// Workgroup b adds tiles b, b + gridDim, ... in order.
+// Workgroup b adds tiles b, b + gridDim, ... in order; where the next one lies is
+// looked up while this one's gradients are on their way.
 template <bool PAST>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(OptTable t, double* part) {
   __shared__ double lds[4];
-  double s = 0.0;
-  for (int64_t i = blockIdx.x; i < t.tiles; i += gridDim.x) {
-    const OptTile at = t.tile[i];
+  struct Place {
+    const void* g;
+    int n;
+    bool bf16;
+  };
+  const auto place = [&](int64_t i) {
+    const OptTile at = t.tile[min(i, t.tiles - 1)];
     const OptDesc& d = t.desc[at.tensor];
     const int64_t e0 = (int64_t)at.tile * kOptTile;
-    const int n = (int)min((int64_t)kOptTile, d.n - e0);
-    s += d.flags & kOptGradBf16 ? tile_squares<uint16_t, PAST>(static_cast<const uint16_t*>(d.grad) + e0, n)
-                                : tile_squares<float, PAST>(static_cast<const float*>(d.grad) + e0, n);
+    const bool bf = d.flags & kOptGradBf16;
+    return Place{static_cast<const char*>(d.grad) + e0 * (bf ? 2 : 4), (int)min((int64_t)kOptTile, d.n - e0), bf};
+  };
+  double s = 0.0;
+  Place p = place(blockIdx.x);
+  for (int64_t i = blockIdx.x; i < t.tiles; i += gridDim.x) {
+    Place next;
+    if (p.bf16) {
+      TileSquares<uint16_t> x;
+      x.template load<PAST>(static_cast<const uint16_t*>(p.g), p.n);
+      next = place(i + gridDim.x);
+      s += x.sum(p.n);
+    } else {
+      TileSquares<float> x;
+      x.template load<PAST>(static_cast<const float*>(p.g), p.n);
+      next = place(i + gridDim.x);
+      s += x.sum(p.n);
+    }
+    p = next;
   }
   s = block_sum64(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;

@@ -376,7 +376,7 @@ hipError_t launch_cross_entropy_bwd(const CeArgs& a, hipStream_t stream);
 
 // The table of a parameter list, in device memory: n descriptions, then `tiles`
 // entries (tensor, tile of kOptTile elements in it).
-constexpr int kOptTile = 4096;
+constexpr int kOptTile = 2048;
 enum { kOptVector = 1, kOptParamBf16 = 2, kOptGradBf16 = 4 };
 struct OptDesc {
   void* param;

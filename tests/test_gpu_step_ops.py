@@ -392,7 +392,7 @@ def flat_views(sizes, dtype, shift=0, align=32, fill=0.0):
     return buf, [buf[shift + a:shift + a + n] for a, n in zip(places, sizes)]
 
 
-RAGGED = [1, 7, 8, 9, 31, 32, 33, 0, 255, 2047, 4095, 4096, 4097, 12345]
+RAGGED = [1, 7, 8, 9, 31, 32, 33, 0, 255, 2047, 2048, 2049, 4095, 4096, 4097, 12345]
 
 
 @pytest.mark.parametrize("sizes,dtype,shift", [

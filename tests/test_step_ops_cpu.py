@@ -169,9 +169,9 @@ def make(ts, state="f32", short=0):
 def test_opt_list(state):
     ts = tensors([1, 0, 4096, 4097, 70000], state)
     got, host = make(ts, state)
-    assert (got.tiles, got.n_tensors, got.state) == (1 + 0 + 1 + 2 + 18, 5, L.OPT_STATES[state])
+    assert (got.tiles, got.n_tensors, got.state) == (1 + 0 + 2 + 3 + 35, 5, L.OPT_STATES[state])
     tiles = np.frombuffer(host, dtype=np.uint32)[5 * 96 // 4:][:2 * got.tiles].reshape(-1, 2)
-    assert tiles[:4].tolist() == [[0, 0], [2, 0], [3, 0], [3, 1]] and tiles[-1].tolist() == [4, 17]
+    assert tiles[:5].tolist() == [[0, 0], [2, 0], [2, 1], [3, 0], [3, 1]] and tiles[-1].tolist() == [4, 34]
     block0 = [int.from_bytes(bytes(host)[96 * i + 64:96 * i + 72], "little") for i in range(5)]
     assert block0 == [0, 1, 1, 129, 129 + 129]
 
