@@ -377,7 +377,7 @@ hipError_t launch_cross_entropy_bwd(const CeArgs& a, hipStream_t stream);
 // The table of a parameter list, in device memory: n descriptions, then `tiles`
 // entries (tensor, tile of kOptTile elements in it).
 constexpr int kOptTile = 2048;
-enum { kOptVector = 1, kOptParamBf16 = 2, kOptGradBf16 = 4 };
+enum { kOptParamBf16 = 1, kOptGradBf16 = 2 };
 struct OptDesc {
   void* param;
   const void* grad;

@@ -321,10 +321,7 @@ sppo_status sppo_opt_list_make(int32_t n_tensors, const sppo_opt_tensor* tensors
     d.grad = t.grad;
     d.n = t.n;
     d.block0 = block0;
-    const void* all[] = {t.grad, t.param, t.master, t.m, t.v};
-    bool vec = true;
-    for (int k = 0; k < (state == SPPO_STATE_NONE ? 1 : 5); ++k) vec = vec && aligned(all[k], 16);
-    d.flags = (vec ? sppo::kOptVector : 0) | (t.grad_dtype == SPPO_BF16 ? sppo::kOptGradBf16 : 0);
+    d.flags = t.grad_dtype == SPPO_BF16 ? sppo::kOptGradBf16 : 0;
     if (state != SPPO_STATE_NONE) {
       d.param = t.param; d.master = t.master;
       d.m = t.m; d.v = t.v;
