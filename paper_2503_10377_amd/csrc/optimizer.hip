@@ -4,7 +4,7 @@
 // launch.  HBM-bound: 201M fp32 gradients' norm 125 us (6.4 TB/s), their AdamW
 // step with fp32 states, masters and bf16 parameters (30 bytes an element) 1055 us
 // (5.7 TB/s); 50M parameters with 8-bit states and bf16 gradients (16.1 bytes) 139
-// us (5.8 TB/s) with the vector units busy for 70%: ten rounds of the generator
+// us (5.8 TB/s) with the vector units busy for 77%: ten rounds of the generator
 // are a third of their work.  Tiles of 2048 elements leave registers for eight
 // waves a SIMD: with 4096 the 8-bit step took 145 us and 300 ragged tensors 8.5
 // instead of 7.5 (the norm 122), with 8192 242 and 10.4.
@@ -84,12 +84,17 @@ __device__ __forceinline__ double wave_sum64(double v) {
   for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
   return v;
 }
-// Over the workgroup, in every thread of the first wave.
-__device__ __forceinline__ double block_sum64(double v, double* lds) {
+// Over a workgroup of WAVES waves, in every thread.
+template <int WAVES>
+__device__ __forceinline__ double block_sum64(double v) {
+  __shared__ double lds[WAVES];
   v = wave_sum64(v);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  double s = lds[0];
+#pragma unroll
+  for (int k = 1; k < WAVES; ++k) s += lds[k];
+  return s;
 }
 
 // A tile's n <= kOptTile gradients.  Squares of fp32 numbers are exact in fp64,
@@ -132,7 +137,6 @@ struct TileSquares {
 // looked up while this one's gradients are on their way.
 template <bool PAST>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(OptTable t, double* part) {
-  __shared__ double lds[4];
   struct Place {
     const void* g;
     int n;
@@ -162,16 +166,18 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(OptTable t, double* par
     }
     p = next;
   }
-  s = block_sum64(s, lds);
+  s = block_sum64<kThreads / 64>(s);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_kernel(const double* part, int n, float max_norm, float* out,
-                                                        int64_t* steps) {
-  __shared__ double lds[4];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += kThreads) s += part[i];
-  s = block_sum64(s, lds);
+// The partial sums, all loads at once.
+constexpr int kNormThreads = 1024;
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(const double* part, int n, float max_norm, float* out,
+                                                            int64_t* steps) {
+  static_assert(kNormBlocks == 2 * kNormThreads, "");
+  const int i = threadIdx.x, k = i + kNormThreads;
+  const double a = i < n ? part[i] : 0.0, b = k < n ? part[k] : 0.0;
+  const double s = block_sum64<kNormThreads / 64>(a + b);
   if (threadIdx.x != 0) return;
   const double norm = sqrt(s);
   const bool ok = (float)norm < __builtin_inff();
@@ -451,7 +457,7 @@ hipError_t launch_grad_norm(const OptTable& t, float max_norm, float* out, int64
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, stream, part, n, max_norm, out, steps);
+  hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kNormThreads), 0, stream, part, n, max_norm, out, steps);
   return hipGetLastError();
 }
 

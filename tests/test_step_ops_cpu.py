@@ -161,8 +161,10 @@ def tensors(sizes, state="f32", param="bf16", grad="f32"):
 
 def make(ts, state="f32", short=0):
     nbytes = max(16, L.sppo_opt_list_bytes(ts) - short)
-    host = (ctypes.c_uint64 * (nbytes // 8 + 2))()
-    return L.sppo_opt_list_make(ts, state, ctypes.addressof(host), nbytes), host
+    host = (ctypes.c_uint64 * (nbytes // 8 + 2))(*[0xABABABABABABABAB] * (nbytes // 8 + 2))
+    out = L.sppo_opt_list_make(ts, state, ctypes.addressof(host), nbytes)
+    assert bytes(host)[max(nbytes, 16):] == b"\xab" * (len(bytes(host)) - max(nbytes, 16)), "written past the table"
+    return out, host
 
 
 @pytest.mark.parametrize("state", ["f32", "e4m3"])
