@@ -113,7 +113,8 @@ class Rotary:
     """Positions in the attention: ``rot`` elements of a head are turned (all
     where None), pairs (j, j + rot/2) ("half") or (2j, 2j + 1) ("interleaved");
     the first row's position; the frequencies as sppo_rotary_freqs takes them
-    (base, scaling, factor, original_len, beta_fast, beta_slow, inv_freq)."""
+    (base, or inv_freq, or scaling with factor, original_len, beta_fast,
+    beta_slow)."""
 
     def __init__(self, rot=None, layout="half", position0=0, **freqs):
         if layout not in L.ROTARY_LAYOUTS:

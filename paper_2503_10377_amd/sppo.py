@@ -713,10 +713,21 @@ ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "given": 4}
 OPT_STATES = {"none": 0, "f32": 1, "e4m3": 2}
 
 
-def sppo_rotary_freqs(rot, base=10000.0, scaling="none", factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0,
+def sppo_rotary_freqs(rot, base=10000.0, scaling=None, factor=1.0, original_len=0.0, beta_fast=32.0, beta_slow=1.0,
                       inv_freq=None):
     """([rot / 2] integers of a rotary spec's table, to be put on the device as
-    64-bit numbers, and its amplitude)."""
+    64-bit numbers, and its amplitude).  Without a scaling: "given" with inv_freq,
+    else "none"; the other settings then need one that is named (ValueError).  A
+    named scaling leaves unread what it does not use, but inv_freq is for "given"
+    alone."""
+    if scaling is None:
+        if (factor, original_len, beta_fast, beta_slow) != (1.0, 0.0, 32.0, 1.0):
+            raise ValueError("factor, original_len, beta_fast and beta_slow need a scaling")
+        if inv_freq is not None and base != 10000.0:
+            raise ValueError("either base or inv_freq")
+        scaling = "none" if inv_freq is None else "given"
+    if inv_freq is not None and ROPE_SCALINGS.get(scaling, scaling) != ROPE_SCALINGS["given"]:
+        raise ValueError(f"scaling {scaling!r} does not read inv_freq")
     n = min(max(int(rot) // 2, 1), 512)  # more is refused
     given = None
     if inv_freq is not None:

@@ -127,6 +127,28 @@ def test_rotary_freqs_given():
         L.sppo_rotary_freqs(8, scaling="given", inv_freq=given)
 
 
+def test_rotary_freqs_drop_nothing_that_is_given():
+    """inv_freq alone is the table; settings that nothing would read are refused,
+    by the layer's description too."""
+    from paper_2503_10377_amd.chunked_layer import Rotary
+
+    given = [0.5, 0.25, -0.125, 3.0]
+    want = L.sppo_rotary_freqs(8, scaling="given", inv_freq=given)
+    assert want != L.sppo_rotary_freqs(8)
+    assert L.sppo_rotary_freqs(8, inv_freq=given) == want
+    rot, table, amp = Rotary(inv_freq=given).table(8, "cpu")
+    assert table.numpy().view(np.uint64).tolist() == want[0] and amp == 1.0
+    for kw in (dict(scaling="none", inv_freq=given), dict(scaling="yarn", factor=2.0, original_len=64, inv_freq=given),
+               dict(inv_freq=given, factor=2.0), dict(inv_freq=given, base=500000.0), dict(factor=8.0),
+               dict(original_len=4096.0), dict(beta_fast=16.0), dict(beta_slow=2.0)):
+        with pytest.raises(ValueError):
+            L.sppo_rotary_freqs(8, **kw)
+        with pytest.raises(ValueError):
+            Rotary(**kw).table(8, "cpu")
+    # A scaling that is named says which settings count.
+    assert L.sppo_rotary_freqs(8, 10000.0, "none", factor=8.0, original_len=4096.0) == L.sppo_rotary_freqs(8)
+
+
 @pytest.mark.parametrize("kw", [
     dict(rot=0), dict(rot=12), dict(rot=1032), dict(rot=-8), dict(base=1.0), dict(base=float("inf")),
     dict(base=float("nan")), dict(scaling=9), dict(scaling="linear", factor=0.5),
