@@ -782,7 +782,9 @@ sppo_status sppo_grad_norm(const sppo_opt_list* list, float max_norm, float* out
  * element e of a tensor whose blocks of 32 start at the list's block B takes
  * word e % 4 of Philox4x32-10 (as the dropout's) with counter (8 B + e / 4 low,
  * high, t low, high) and key seed, its low half for m, its high half for r.
- * Values that are infinite or NaN are kept as NaN, a v below 2^-126 as zero. */
+ * Values that are infinite or NaN are kept as NaN, a v below 2^-126 as zero.
+ * Squares past fp32's range: with F32 v is infinite from then on, and the
+ * parameter only decays; with E4M3 r is finite where g' and the old r are. */
 typedef struct {
   double lr, beta1, beta2, eps;  /* lr finite; 0 <= beta < 1; eps > 0, a
                                     normal fp32 number                      */

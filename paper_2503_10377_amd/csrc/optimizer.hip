@@ -331,6 +331,27 @@ __device__ __forceinline__ float root(float v) {
   return v < 1.17549435e-38f ? 0.f : s;
 }
 
+// Roots and steps of a quad some of whose v may be infinite, though r and g are
+// not: gradients from 1.8e19 on.  Those elements are computed from 2^-96 g, m, r
+// and eps, whose squares lie in [2^-64, 2^64] (or are too small beside the other
+// one's to count), and r is scaled back: it fits wherever g and the old r did.
+// The others are what the plain path makes of them, times one.
+__device__ __forceinline__ void far_steps(const Coef& c, const float (&fg)[4], const float (&fm)[4],
+                                          const float (&v2)[4], float (&fr)[4], float (&fw)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool far = v2[i] == __builtin_inff();
+    const float s = far ? 0x1p-96f : 1.f;
+    float unused = 0.f, v = (fr[i] * s) * (fr[i] * s);
+    moments(c, fg[i] * s, unused, v);
+    Coef d = c;
+    d.eps = c.eps * s;
+    const float r = root(v);
+    fw[i] = stepped(d, fw[i], fm[i] * s, r);
+    fr[i] = far ? r * 0x1p96f : r;
+  }
+}
+
 // A tile with 8-bit states: elements from n on count as zeros and are not
 // written, so that every lane takes part in its block's exponent.
 template <typename G, bool PBF, bool PAST>
@@ -383,12 +404,21 @@ __device__ __forceinline__ void adam8_tile(const Coef& c, const OptDesc& d, int6
     }
     decode8(cm[u], __uint_as_float(sm[u] << 23), fm);
     decode8(cv[u], __uint_as_float(sv[u] << 23), fr);
+    float v2[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float v2 = fr[i] * fr[i];
-      moments(c, fg[i], fm[i], v2);
-      fr[i] = root(v2);
-      fw[i] = stepped(c, fw[i], fm[i], fr[i]);
+      v2[i] = fr[i] * fr[i];
+      moments(c, fg[i], fm[i], v2[i]);
+    }
+    const float top = fmaxf(fmaxf(v2[0], v2[1]), fmaxf(v2[2], v2[3]));  // of what is no NaN
+    if (__builtin_amdgcn_ballot_w64(top == __builtin_inff())) {  // some square of the wave: rare
+      far_steps(c, fg, fm, v2, fr, fw);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        fr[i] = root(v2[i]);
+        fw[i] = stepped(c, fw[i], fm[i], fr[i]);
+      }
     }
     const int km = block_exponent(fm), kr = block_exponent(fr);
     const float im = pow2(-km), ir = pow2(-kr);

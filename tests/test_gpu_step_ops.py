@@ -648,6 +648,52 @@ def test_adamw_of_extreme_gradients():
             assert not m[rest].any() and not v[rest].any()
 
 
+@pytest.mark.parametrize("param", ["f32", "bf16"])
+@pytest.mark.parametrize("f", [1.0, 0.5])
+def test_adamw_of_gradients_whose_squares_are_infinite(param, f):
+    """Finite gradients from 1.8e19 on, whose squares leave fp32's range, beside
+    small ones.  With 8-bit states three steps against the oracle, each from what
+    the one before left: parameters as check_step counts them, states to a step
+    of their codes (2^-3 of a value, 2^-9 of the block's unit at least).  With
+    fp32 states v is infinite and the parameter only decays."""
+    announce(f"adamw of gradients with infinite squares param={param} f={f}")
+    lr, b1, b2, eps = 1e-2, 0.9, 0.99, 1e-8
+    norm = torch.tensor([3.0, f], device="cuda")
+    big = [1.7e19, 1.9e19, -2e19, 1e25, -3e30, 1e38, -3.3e38]
+    k = Setting([133, 96], "e4m3", param, "f32")
+    for t in (1, 2, 3):
+        k.gradients(t)
+        for i, v in enumerate(big):
+            k.v["g"][0][3 + 7 * i + 40 * (i % 2)] = v if t != 2 else 1e-3
+            k.v["g"][1][95 - i] = v
+        before = {n: k.np(n) for n in ("w", "g", "m", "v", "ms", "vs")}
+        L.sppo_adamw_step(k.list, L.adamw(lr, b1, b2, eps, t, norm=norm, seed=11))
+        for i, n in enumerate(k.sizes):
+            w, g = before["w"][i], before["g"][i]
+            m, r = (O.value8(before[a][i], before[a + "s"][i]) for a in ("m", "v"))
+            rp, rm, rv = O.adamw(w, g, m, r * r, t, lr * k.lrs[i], b1, b2, eps, k.decay[i], f)
+            rr = np.sqrt(rv)
+            tm = 4 * U * (np.abs(b1 * m) + (1 - b1) * np.abs(f * g)) + 2.0 ** -148
+            den = rr / np.sqrt(1 - b2 ** t) + eps
+            q = rm / (1 - b1 ** t) / den
+            tq = tm / (1 - b1 ** t) / den + 12 * U * np.abs(q)
+            tp = lr * k.lrs[i] * (tq + 4 * U * (np.abs(q) + np.abs(k.decay[i] * w))) + 2 * U * np.abs(w)
+            within(k.v["w"][i], rp, tp, ("w", t, i))
+            for a, x in (("m", rm), ("v", rr)):
+                scales = k.v[a + "s"][i].cpu().numpy()
+                assert np.array_equal(scales, O.block_bytes(x)), (a, t, i)
+                unit = 2.0 ** (np.repeat(scales.astype(np.float64), 32)[:n] - 127)
+                got = torch.from_numpy(O.value8(k.v[a][i].cpu().numpy(), scales))
+                within(got, x, 2.0 ** -3 * np.abs(x) + 2.0 ** -9 * unit, (a, t, i))
+    k = Setting([96], "f32", param, "f32")
+    k.gradients(1)
+    k.v["g"][0][5], k.v["g"][0][64] = 1e25, -3.3e38
+    w0 = k.np("w")[0]
+    L.sppo_adamw_step(k.list, L.adamw(lr, b1, b2, eps, 1, norm=norm))
+    assert torch.isinf(k.v["v"][0][[5, 64]]).all() and torch.isfinite(k.v["w"][0]).all()
+    within(k.v["w"][0][[5, 64]], w0[[5, 64]], 0.0, "w under an infinite v")
+
+
 # --------------------------------------------------------------------- together
 def test_a_step_in_graphs():
     """Rotary, loss, norm and update captured twice with their own buffers and
