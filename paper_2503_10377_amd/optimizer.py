@@ -34,8 +34,8 @@ class AdamW:
             raise ValueError(f"unknown state {state!r}")
         if max_norm is not None and not max_norm > 0:
             raise ValueError("max_norm must be positive")
-        if not all(0.0 <= b < 1.0 for b in betas) or not eps > 0.0:
-            raise ValueError("betas must be in [0, 1), eps positive")
+        if len(betas) != 2 or not all(0.0 <= b < 1.0 for b in betas) or not eps > 0.0:
+            raise ValueError("betas must be two in [0, 1), eps positive")
         device = next(iter(params.values())).device
         for name, p in params.items():
             g = grads[name]

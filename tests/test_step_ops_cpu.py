@@ -383,3 +383,13 @@ def test_layer_refuses_before_the_device():
                               ({"a": w}, {"a": w}, dict(betas=(0.9, 1.0))), ({"a": w}, {"a": w}, dict(eps=0.0))):
         with pytest.raises(ValueError):
             AdamW(params, grads, 1e-3, **kw)
+
+
+def test_optimizer_needs_two_betas():
+    from paper_2503_10377_amd.optimizer import AdamW
+    import torch
+
+    w = torch.zeros(4)
+    for betas in ((), (0.9,), (0.9, 0.95, 0.99)):
+        with pytest.raises(ValueError, match="betas"):
+            AdamW({"a": w}, {"a": w}, 1e-3, betas=betas)
