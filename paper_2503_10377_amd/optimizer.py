@@ -34,8 +34,8 @@ class AdamW:
             raise ValueError(f"unknown state {state!r}")
         if max_norm is not None and not max_norm > 0:
             raise ValueError("max_norm must be positive")
-        if len(betas) != 2 or not all(0.0 <= b < 1.0 for b in betas) or not eps > 0.0:
-            raise ValueError("betas must be two in [0, 1), eps positive")
+        self.betas, self.eps = betas, eps
+        self._check()
         device = next(iter(params.values())).device
         for name, p in params.items():
             g = grads[name]
@@ -49,7 +49,7 @@ class AdamW:
                 raise ValueError(f"lr_scale names {name!r}, which is no parameter")
         self.params, self.grads, self.device, self.state = dict(params), dict(grads), device, state
         self.lr, self.max_norm = lr, max_norm
-        self.betas, self.eps, self.seed = betas, eps, seed
+        self.seed = seed
         zeros = lambda n, dt: torch.zeros(n, dtype=dt, device=device)  # noqa: E731
         self.master = {k: p.detach().float() for k, p in self.params.items() if p.dtype == torch.bfloat16}
         sdt = torch.float32 if state == "f32" else torch.uint8
@@ -77,13 +77,22 @@ class AdamW:
         dev = isinstance(lr, torch.Tensor)
         if dev and (lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self.device):
             raise ValueError("an lr tensor must be one fp32 on the parameters' device")
+        # What the update's call refuses is refused before the norm's call counts the update.
         if not dev and not L.scale_ok(lr, float("inf")):
-            raise ValueError("lr must be finite")  # before the norm's call counts the step
+            raise ValueError("lr must be finite")
+        self._check()
+        spec = L.adamw(1.0 if dev else lr, *self.betas, self.eps, 0, self.steps, self.norm, lr if dev else None,
+                       self.seed)
         with torch.cuda.device(self.device):
             L.sppo_grad_norm(self.list, float("inf") if self.max_norm is None else self.max_norm, self.norm, self.ws,
                              self.ws_bytes, self.steps, stream)
-            L.sppo_adamw_step(self.list, L.adamw(1.0 if dev else lr, *self.betas, self.eps, 0, self.steps, self.norm,
-                                                 lr if dev else None, self.seed), stream)
+            L.sppo_adamw_step(self.list, spec, stream)
+
+    def _check(self):
+        if len(self.betas) != 2 or not all(0.0 <= b < 1.0 for b in self.betas):
+            raise ValueError("betas must be two in [0, 1)")
+        if not self.eps > 0.0 or not L.scale_ok(self.eps, float("inf")) or L.scale_ok(self.eps, 2.0 ** -126):
+            raise ValueError("eps must be positive and a normal fp32 number")
 
     def state_tensors(self):
         """The tensors that make up the optimizer's state beside the parameters,

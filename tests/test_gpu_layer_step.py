@@ -18,6 +18,7 @@ import torch
 from oracle import step_ops as O
 from oracle import train_ops as T
 from paper_2503_10377_amd import chunked_layer as C
+from paper_2503_10377_amd import sppo as L
 from paper_2503_10377_amd.chunked_layer import BlockEnds, ChunkedLayer, Loss, Rotary
 from paper_2503_10377_amd.inputs import make_layer_inputs
 from paper_2503_10377_amd.optimizer import AdamW
@@ -307,3 +308,24 @@ def test_optimizer_refuses():
         with pytest.raises(ValueError):
             o.step(lr)
     assert o.steps.item() == 0
+
+
+def test_optimizer_counts_no_update_that_is_refused():
+    """Settings that are changed between steps to what the update's call refuses:
+    nothing is enqueued and nothing counted."""
+    announce("optimizer with settings that are refused")
+    p, g = {"w": torch.ones(8, 8, device="cuda")}, {"w": torch.ones(8, 8, device="cuda")}
+    o = AdamW(p, g, 1e-3)
+    o.step()
+    kept = {n: t.clone() for n, t in o.state_tensors().items()}
+    for name, bad in (("eps", 1e-40), ("eps", INF), ("eps", 0.0), ("betas", (0.9, 1.0)), ("betas", (0.9,)),
+                      ("seed", 0.5), ("lr", INF), ("lr", torch.ones(1)), ("max_norm", 0.0)):
+        good = getattr(o, name)
+        setattr(o, name, bad)
+        with pytest.raises((ValueError, TypeError, L.SppoError)):
+            o.step()
+        setattr(o, name, good)
+        for n, t in o.state_tensors().items():
+            assert torch.equal(t, kept[n]), (name, bad, n)
+    o.step()
+    assert o.steps.item() == 2

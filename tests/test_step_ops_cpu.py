@@ -393,3 +393,17 @@ def test_optimizer_needs_two_betas():
     for betas in ((), (0.9,), (0.9, 0.95, 0.99)):
         with pytest.raises(ValueError, match="betas"):
             AdamW({"a": w}, {"a": w}, 1e-3, betas=betas)
+
+
+def test_optimizer_refuses_an_eps_that_the_update_refuses():
+    """eps as the update's call takes it: a normal fp32 number."""
+    from paper_2503_10377_amd.optimizer import AdamW
+    import torch
+
+    w = torch.zeros(4)
+    for eps in (1e-46, 1e-40, 2.0 ** -126 * (1 - 2.0 ** -20), 1e39, float("inf"), float("nan"), 0.0, -1e-8):
+        with pytest.raises(ValueError, match="eps"):
+            AdamW({"a": w}, {"a": w}, 1e-3, eps=eps)
+    for eps in (2.0 ** -126, 1e-8, 1.0):  # refused for their tensors, which are in host memory
+        with pytest.raises(ValueError, match="device"):
+            AdamW({"a": w}, {"a": w}, 1e-3, eps=eps)
