@@ -155,6 +155,10 @@ class ChunkedLayer:
             raise ValueError("vocab must be in [1, 2^31)")
         if vocab is not None and not L.scale_ok(embed_scale):
             raise ValueError("embed_scale must be finite and below 2^112")
+        # What the products over the classes refuse: an output of 2^31 elements,
+        # and 256 rows of either operand from 2^31 bytes on.
+        if loss is not None and (H * loss.classes >= 2 ** 31 or loss.classes >= 2 ** 22):
+            raise ValueError("Hq*D times the loss's classes must be below 2^31, the classes below 2^22")
         self.S, self.N, self.Hq, self.Hkv, self.D, self.H, self.Wt = S, n_chunks, Hq, Hkv, D, H, wt
         self.eps = eps
         self.device = device

@@ -407,3 +407,22 @@ def test_optimizer_refuses_an_eps_that_the_update_refuses():
     for eps in (2.0 ** -126, 1e-8, 1.0):  # refused for their tensors, which are in host memory
         with pytest.raises(ValueError, match="device"):
             AdamW({"a": w}, {"a": w}, 1e-3, eps=eps)
+
+
+@pytest.mark.parametrize("heads,classes", [(64, 2 ** 18), (32, 2 ** 19), (2, 2 ** 22), (2, 2 ** 30)])
+def test_layer_refuses_classes_that_its_products_refuse(heads, classes):
+    """The gradient of [H, classes] weights counts its elements in 31 bits, and a
+    product over the classes takes fewer than 2^22: refused with the layer, not in
+    the last chunk of its first step.  The products' calls refuse the same sizes."""
+    from paper_2503_10377_amd.chunked_layer import ChunkedLayer, Loss
+
+    H = 128 * heads
+    with pytest.raises(ValueError, match="classes"):
+        ChunkedLayer(512, 4, heads, heads, 128, device="cpu", loss=Loss(classes))
+
+    call = ("tn", H, classes, 128, P, H, P, classes, P, classes)
+    if H * classes < 2 ** 31:
+        call = ("nt", 128, H, classes, P, classes, P, classes, P, H)
+    with pytest.raises(L.SppoError) as e:
+        L.sppo_gemm_bf16(*call, stream=0)
+    assert e.value.status == UNS
