@@ -705,8 +705,10 @@ typedef struct {
  * [rows], loss and lse fp32 [rows] (lse may be NULL), dlogits as logits, or
  * NULL for the loss alone; it may be logits (with the same stride).  Columns
  * from V on are neither used nor written.  rows 0: nothing is done; rows <
- * 2^31.  workspace: sppo_cross_entropy_workspace bytes (0, and NULL, where rows
- * are many or short; also 0 for an invalid ce), 16-byte aligned. */
+ * 2^31.  workspace: sppo_cross_entropy_workspace bytes, 16-byte aligned: enough
+ * for any call of up to that many rows (0 up to V = 32768, for no rows and for an
+ * invalid ce).  Calls of V up to 131072 bf16 or 65536 fp32 logits and more than
+ * 127 rows use none and take NULL, like those of V up to 32768. */
 size_t sppo_cross_entropy_workspace(const sppo_ce* ce, int64_t rows);
 sppo_status sppo_cross_entropy(const sppo_ce* ce, int64_t rows, const void* logits, int64_t ld, const void* targets,
                                float* loss, float* lse, void* dlogits, int64_t lddl, void* workspace,

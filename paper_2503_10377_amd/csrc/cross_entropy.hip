@@ -492,11 +492,14 @@ hipError_t launch_bwd(const CeArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t cross_entropy_workspace(int64_t rows, int64_t V, bool f32) {
-  // Not less for more rows than for fewer.
-  if (rows > kFewRows && !in_parts(rows, V, f32)) rows = kFewRows;
+size_t cross_entropy_uses(int64_t rows, int64_t V, bool f32) {
   if (rows <= 0 || !in_parts(rows, V, f32)) return 0;
   return (size_t)(rows_at_once(rows, V, f32) * parts_of(V, f32)) * sizeof(f32x4);
+}
+
+size_t cross_entropy_workspace(int64_t rows, int64_t V, bool f32) {
+  // Not less for more rows than for fewer.
+  return cross_entropy_uses(rows > kFewRows && !in_parts(rows, V, f32) ? kFewRows : rows, V, f32);
 }
 
 hipError_t launch_cross_entropy(const CeArgs& a, hipStream_t stream) {

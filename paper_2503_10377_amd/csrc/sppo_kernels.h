@@ -370,6 +370,9 @@ struct CeArgs {
   void* workspace;
   int f32;
 };
+// Bytes of workspace that a call uses, and the most that one of up to so many
+// rows does.
+size_t cross_entropy_uses(int64_t rows, int64_t V, bool f32);
 size_t cross_entropy_workspace(int64_t rows, int64_t V, bool f32);
 hipError_t launch_cross_entropy(const CeArgs& a, hipStream_t stream);
 hipError_t launch_cross_entropy_bwd(const CeArgs& a, hipStream_t stream);

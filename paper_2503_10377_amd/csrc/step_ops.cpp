@@ -262,7 +262,7 @@ sppo_status sppo_cross_entropy(const sppo_ce* ce, int64_t rows, const void* logi
   if (st != SPPO_OK) return st;
   if (!loss || !aligned(loss, 4) || !aligned(lse, 4))
     return fail(SPPO_ERR_INVALID_ARG, "cross entropy: null or misaligned loss, or misaligned lse");
-  const size_t need = sppo::cross_entropy_workspace(rows, ce->V, a.f32);
+  const size_t need = sppo::cross_entropy_uses(rows, ce->V, a.f32);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
     return fail(SPPO_ERR_INVALID_ARG, "cross entropy: workspace null, misaligned or too small");
   if (rows == 0) return SPPO_OK;

@@ -149,6 +149,20 @@ def test_cross_entropy_around_the_borders(V, dtype, rows):
     assert torch.equal(x[:, :V], dx[:, :V])
 
 
+@pytest.mark.parametrize("rows,V,dtype", [(128, 40001, "bf16"), (200, 65536, "f32"), (5, 32768, "bf16")])
+def test_cross_entropy_without_the_workspace_that_it_does_not_use(rows, V, dtype):
+    """NULL where rows are kept in registers: the bits of a call that has one."""
+    announce(f"cross entropy without a workspace rows={rows} V={V} {dtype}")
+    ld = (V + 7) // 8 * 8
+    x, t = ce_case(rows, V, ld, dtype)
+    ce = L.cross_entropy(V, dtype)
+    want = run_ce(ce, rows, x, ld, t, dtype)
+    loss, lse, dx = torch.empty_like(want[0]), torch.empty_like(want[1]), torch.full_like(want[2], 7.0)
+    L.sppo_cross_entropy(ce, rows, x, ld, t, loss, lse, dx, ld)
+    for a, b in zip((loss, lse, dx), want):
+        assert torch.equal(a, b)
+
+
 def test_cross_entropy_in_parts_past_32_bit_offsets():
     """Rows in parts whose offsets pass 2^32 elements, in place, in a buffer that
     is touched at few places."""

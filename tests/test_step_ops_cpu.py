@@ -426,3 +426,21 @@ def test_layer_refuses_classes_that_its_products_refuse(heads, classes):
     with pytest.raises(L.SppoError) as e:
         L.sppo_gemm_bf16(*call, stream=0)
     assert e.value.status == UNS
+
+
+def test_cross_entropy_workspace_is_asked_for_where_it_is_used():
+    """Few long rows and rows past 131072 bf16 (65536 fp32) logits need it; the
+    size never shrinks with more rows, so one for the largest call serves all."""
+    for V, dtype, first in ((32768, "bf16", None), (32769, "bf16", 1), (131072, "bf16", 1), (65536, "f32", 1),
+                            (131073, "bf16", 1), (65537, "f32", 1)):
+        ce = L.cross_entropy(V, dtype)
+        sizes = [L.sppo_cross_entropy_workspace(ce, r) for r in (0, 1, 2, 126, 127, 128, 129, 5000)]
+        assert sizes == sorted(sizes) and sizes[0] == 0 and (sizes[1] > 0) == (first == 1)
+    c = dict(logits=P, ld=131080, targets=2 * P, loss=3 * P, lse=None, dlogits=None, lddl=0)
+    for V, rows in ((40001, 1), (40001, 127), (131073, 128), (131073, 5000)):
+        ce = L.cross_entropy(V)
+        need = L.sppo_cross_entropy_workspace(ce, rows)
+        for ws, n in ((None, 0), (None, need), (P, need - 1), (P + 8, need)):
+            with pytest.raises(L.SppoError) as e:
+                L.sppo_cross_entropy(ce, rows, *c.values(), ws, n, stream=0)
+            assert e.value.status == BAD
