@@ -63,9 +63,10 @@ class AdamW:
             tensors.append(L.opt_tensor(p.numel(), self.grads[k], _DTYPES[self.grads[k].dtype], p, _DTYPES[p.dtype],
                                         self.master.get(k), self.m[k], self.v[k], self.m_scale.get(k),
                                         self.v_scale.get(k), (lr_scale or {}).get(k, 1.0), wd))
-        self.list = L.opt_list(tensors, state, device)
         self.norm = torch.zeros(2, dtype=torch.float32, device=device)  # of the last step: the norm, the factor
         self.steps = torch.zeros(1, dtype=torch.int64, device=device)   # updates made
+        # The table's copy waits for all that was filled before it, so the first step() may be on any stream.
+        self.list = L.opt_list(tensors, state, device)
         self.ws_bytes = L.sppo_grad_norm_workspace(self.list)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
 

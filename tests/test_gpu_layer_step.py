@@ -329,3 +329,37 @@ def test_optimizer_counts_no_update_that_is_refused():
             assert torch.equal(t, kept[n]), (name, bad, n)
     o.step()
     assert o.steps.item() == 2
+
+
+def test_optimizer_steps_at_once_on_another_stream(monkeypatch):
+    """The first step() on a stream that waits for nothing, while the
+    constructor's stream is still busy with what was enqueued after the list's
+    table: state, norm and count are ready by then."""
+    announce("optimizer at once on another stream")
+    real = L.opt_list
+
+    def busy(*a):
+        out = real(*a)
+        torch.cuda._sleep(10 ** 8)  # some 40 ms before whatever the constructor fills after this
+        return out
+
+    monkeypatch.setattr(L, "opt_list", busy)
+    g = torch.Generator().manual_seed(1)
+    p0 = torch.randn(300, 7, generator=g).cuda()
+    grad = {"w": torch.randn(300, 7, generator=g).cuda()}
+    torch.cuda.synchronize()
+    for state in ("f32", "e4m3"):
+        params = [{"w": p0.clone()} for _ in range(2)]
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        a = AdamW(params[0], grad, lr=1e-2, max_norm=1.0, state=state)
+        a.step(stream=s)
+        torch.cuda.synchronize()
+        b = AdamW(params[1], grad, lr=1e-2, max_norm=1.0, state=state)
+        torch.cuda.synchronize()
+        b.step()
+        torch.cuda.synchronize()
+        assert a.steps.item() == 1 and torch.equal(a.norm, b.norm)
+        for n, t in a.state_tensors().items():
+            assert torch.equal(t, b.state_tensors()[n]), n
+        assert torch.equal(params[0]["w"], params[1]["w"])
