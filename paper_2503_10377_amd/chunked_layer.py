@@ -231,6 +231,8 @@ class ChunkedLayer:
             ce = self._ce("i64", 1.0)
             self.ce_ws_bytes = max(L.sppo_cross_entropy_workspace(ce, self.chunk_len(i)) for i in range(self.N))
             self.ce_ws = torch.empty(max(self.ce_ws_bytes, 16) // 4, dtype=f32, device=dev)
+            # The one buffer here whose content a step reads: it may be on any stream.
+            torch.cuda.current_stream(dev).synchronize()
         if self.vocab is not None:
             self.x, self.dx = e(sm, H), e(sm, H)
             self.emb_ws_bytes = L.sppo_embedding_bwd_workspace(sm, H)

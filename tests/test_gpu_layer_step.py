@@ -363,3 +363,31 @@ def test_optimizer_steps_at_once_on_another_stream(monkeypatch):
         for n, t in a.state_tensors().items():
             assert torch.equal(t, b.state_tensors()[n]), n
         assert torch.equal(params[0]["w"], params[1]["w"])
+
+
+def test_layer_with_a_loss_steps_at_once_on_another_stream():
+    """A first step on a stream that waits for nothing, while the stream that the
+    layer was made on was busy: the bits of a step that waited."""
+    announce("layer at once on another stream")
+    inp, p = setup(256, 2, 2, 128, 256, None, 1)
+    inp, p = ({k: v.cuda() for k, v in d.items()} for d in (inp, p))
+    outs = []
+    for busy in (True, False):
+        made, s = torch.cuda.Stream(), torch.cuda.Stream()
+        with torch.cuda.stream(made):
+            # What the layer's buffers may be made of holds no zeros.
+            old = [torch.full((256, 256), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(64)]
+            made.synchronize()
+            del old
+            if busy:
+                torch.cuda._sleep(10 ** 8)  # some 40 ms
+            lay = ChunkedLayer(256, 2, 2, 2, 128, offsets=[0, 100, 256], loss=Loss(256), rotary=Rotary())
+            out = lay.alloc_outputs()
+        if not busy:
+            torch.cuda.synchronize()
+        lay.step(inp, p, out, stream=s)
+        torch.cuda.synchronize()
+        outs.append({k: v.clone() for k, v in out.items()})
+        lay.close()
+    for k in outs[0]:
+        assert torch.isfinite(outs[0][k].float()).all() and torch.equal(outs[0][k], outs[1][k]), k
