@@ -114,14 +114,16 @@ class Rotary:
     where None), pairs (j, j + rot/2) ("half") or (2j, 2j + 1) ("interleaved");
     the first row's position; the frequencies as sppo_rotary_freqs takes them
     (base, or inv_freq, or scaling with factor, original_len, beta_fast,
-    beta_slow)."""
+    beta_slow), and the amplitude where it is not theirs (1 with inv_freq)."""
 
-    def __init__(self, rot=None, layout="half", position0=0, **freqs):
+    def __init__(self, rot=None, layout="half", position0=0, amp=None, **freqs):
         if layout not in L.ROTARY_LAYOUTS:
             raise ValueError(f"unknown layout {layout!r}")
         if not 0 <= position0 < 2 ** 62:
             raise ValueError("position0 must be in [0, 2^62)")
-        self.rot, self.layout, self.position0, self.freqs = rot, layout, position0, freqs
+        if amp is not None and not L.scale_ok(amp, float("inf")):
+            raise ValueError("amp must be finite")
+        self.rot, self.layout, self.position0, self.amp, self.freqs = rot, layout, position0, amp, freqs
 
     def table(self, head_dim, device):
         """The device table of a head's frequencies and their amplitude."""
@@ -129,6 +131,7 @@ class Rotary:
         if rot > head_dim:
             raise ValueError("rot is more than a head has")
         freqs, amp = L.sppo_rotary_freqs(rot, **self.freqs)
+        amp = amp if self.amp is None else self.amp
         return rot, torch.from_numpy(np.array(freqs, dtype=np.uint64).view(np.int64)).to(device), amp
 
 

@@ -140,6 +140,21 @@ def test_layer_rotary_depends_on_differences_only():
     assert np.linalg.norm(c["dw_qkv"] - a["dw_qkv"]) > 0.1 * np.linalg.norm(a["dw_qkv"])
 
 
+def test_layer_rotary_with_given_frequencies():
+    """A stretched context's frequencies and amplitude, given: what the scaling by
+    name makes of them within the gates (the table's roundings differ); plain
+    positions move the outputs by O(1)."""
+    offsets = [0, 130, 256]
+    named = Rotary(scaling="yarn", factor=8.0, original_len=32, beta_fast=4.0)
+    rope = rope_of(named, 128)
+    given = Rotary(inv_freq=[float(f) for f in rope["freqs"]], amp=rope["amp"])
+    a, _, _ = run(256, 2, 2, 128, offsets, named, Loss(256), seed=3)
+    b, _, _ = run(256, 2, 2, 128, offsets, given, Loss(256), seed=3)
+    check(b, a)
+    c, _, _ = run(256, 2, 2, 128, offsets, Rotary(), Loss(256), seed=3)
+    assert np.linalg.norm(c["dw_qkv"] - a["dw_qkv"]) > 0.05 * np.linalg.norm(a["dw_qkv"])
+
+
 def test_layer_loss_scale_on_the_device():
     offsets = [0, 130, 256]
     a, _, _ = run(256, 2, 2, 128, offsets, None, Loss(256), seed=4, loss_scale=0.125)

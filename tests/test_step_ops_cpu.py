@@ -444,3 +444,15 @@ def test_cross_entropy_workspace_is_asked_for_where_it_is_used():
             with pytest.raises(L.SppoError) as e:
                 L.sppo_cross_entropy(ce, rows, *c.values(), ws, n, stream=0)
             assert e.value.status == BAD
+
+
+def test_rotary_amplitude_of_given_frequencies():
+    """Given frequencies have the amplitude that is given with them."""
+    from paper_2503_10377_amd.chunked_layer import Rotary
+
+    given = [0.5, 0.25, -0.125, 3.0]
+    assert Rotary(inv_freq=given, amp=1.25).table(8, "cpu")[2] == 1.25
+    assert Rotary(scaling="yarn", factor=4.0, original_len=64, amp=1.0).table(8, "cpu")[2] == 1.0
+    for amp in (float("inf"), float("nan"), 1e39):
+        with pytest.raises(ValueError):
+            Rotary(inv_freq=given, amp=amp)
