@@ -137,7 +137,9 @@ class Rotary:
 
 class Loss:
     """The loss behind the layer: cross-entropy over ``classes`` (a multiple of
-    256, as the projection's gradient needs)."""
+    256, as the projection's gradient needs, below 2^22, and below 2^31 / (Hq D)
+    with a layer's heads).  All of them take part in the softmax, also those that
+    only pad a vocabulary."""
 
     def __init__(self, classes, label_smoothing=0.0, z_loss=0.0):
         if not 0 < classes < 2 ** 31 or classes % 256:

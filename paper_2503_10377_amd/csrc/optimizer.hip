@@ -2,12 +2,13 @@
 // step with states in 32 or in 8 bits.  A workgroup takes a tile of kOptTile
 // elements of one tensor, whichever it belongs to, so a list of any tensors is one
 // launch.  HBM-bound: 201M fp32 gradients' norm 125 us (6.4 TB/s), their AdamW
-// step with fp32 states, masters and bf16 parameters (30 bytes an element) 1055 us
-// (5.7 TB/s); 50M parameters with 8-bit states and bf16 gradients (16.1 bytes) 139
-// us (5.8 TB/s) with the vector units busy for 77%: ten rounds of the generator
-// are a third of their work.  Tiles of 2048 elements leave registers for eight
-// waves a SIMD: with 4096 the 8-bit step took 145 us and 300 ragged tensors 8.5
-// instead of 7.5 (the norm 122), with 8192 242 and 10.4.
+// step with fp32 states, masters and bf16 parameters (30 bytes an element) 1054 to
+// 1085 us by the machine (5.6-5.7 TB/s); 50M parameters with 8-bit states and bf16
+// gradients (16.1 bytes) 138 to 141 us (5.8 TB/s) with the vector units busy for
+// 79%: ten rounds of the generator are a third of their work.  Tiles of 2048
+// elements leave registers for eight waves a SIMD: with 4096 the 8-bit step took
+// 145 us and 300 ragged tensors 8.5 instead of 7.5 (the norm 122), with 8192 242
+// and 10.4.
 //
 // Four neighbouring elements a thread in one access: eight (two accesses of fp32,
 // each of half the cache lines) took 1122 us, and 137 for the norm.  Accesses are

@@ -8,8 +8,10 @@ the AdamW update of the parameters, over libsppo's calls.
 bf16 parameters get fp32 masters; the states are fp32 or 8-bit (e4m3 codes under
 a power of two for 32 elements).  The update's number counts on the device, and
 an update whose gradients hold an infinity or a NaN changes nothing and does not
-count, so a step() may be captured into a graph and replayed.  Only C-ABI calls
-and torch allocations happen here.
+count, so a step() may be captured into a graph and replayed.  The list of
+tensors holds their addresses: gradients are to be written where they were, as a
+layer's outputs are, and ones that are allocated anew need another list.  Only
+C-ABI calls and torch allocations happen here.
 """
 from __future__ import annotations
 
