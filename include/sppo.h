@@ -786,7 +786,8 @@ sppo_status sppo_grad_norm(const sppo_opt_list* list, float max_norm, float* out
  * high, t low, high) and key seed, its low half for m, its high half for r.
  * Values that are infinite or NaN are kept as NaN, a v below 2^-126 as zero.
  * Squares past fp32's range: with F32 v is infinite from then on, and the
- * parameter only decays; with E4M3 r is finite where g' and the old r are. */
+ * parameter only decays (is NaN from the next step on with beta2 0); with E4M3 m
+ * and r are finite where they and g' were, kept to 240 2^120 (3.19e38). */
 typedef struct {
   double lr, beta1, beta2, eps;  /* lr finite; 0 <= beta < 1; eps > 0, a
                                     normal fp32 number                      */

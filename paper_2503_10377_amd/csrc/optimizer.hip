@@ -332,24 +332,34 @@ __device__ __forceinline__ float root(float v) {
   return v < 1.17549435e-38f ? 0.f : s;
 }
 
-// Roots and steps of a quad some of whose v may be infinite, though r and g are
-// not: gradients from 1.8e19 on.  Those elements are computed from 2^-96 g, m, r
-// and eps, whose squares lie in [2^-64, 2^64] (or are too small beside the other
-// one's to count), and r is scaled back: it fits wherever g and the old r did.
-// The others are what the plain path makes of them, times one.
-__device__ __forceinline__ void far_steps(const Coef& c, const float (&fg)[4], const float (&fm)[4],
-                                          const float (&v2)[4], float (&fr)[4], float (&fw)[4]) {
+// Roots and steps of a quad some of whose v may be infinite (or NaN, by a beta2 of
+// zero), though r and g are not: gradients from 1.8e19 on.  Those elements are
+// computed from 2^-72 g, m, r and eps where one of g and r is above 2^60: squares
+// below 2^112 and, where they count, normal numbers.  A beta2 below 2^-100 counts as
+// zero there.  The others are what the plain path makes of them, times one.  States
+// are kept to 240 2^120, the largest code's value that fp32 holds there: above it a
+// code of 256 2^120 would be infinite.  (Without such an element no state grows
+// that far.)
+__device__ __forceinline__ void far_steps(const Coef& c, const float (&fg)[4], float (&fm)[4], const float (&v2)[4],
+                                          float (&fr)[4], float (&fw)[4]) {
+  const auto kept = [](float x) {
+    constexpr float top = 0x1.ep127f;
+    return fabsf(x) > top && fabsf(x) < __builtin_inff() ? copysignf(top, x) : x;
+  };
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool far = v2[i] == __builtin_inff();
-    const float s = far ? 0x1p-96f : 1.f;
-    float unused = 0.f, v = (fr[i] * s) * (fr[i] * s);
+    const bool far = !(v2[i] < __builtin_inff());
+    const float r0 = far && c.b2 < 0x1p-100f && fr[i] < __builtin_inff() ? 0.f : fr[i];
+    const bool scaled = far && (r0 > 0x1p60f || fabsf(fg[i] * c.f) > 0x1p60f);
+    const float s = scaled ? 0x1p-72f : 1.f;
+    float unused = 0.f, v = (r0 * s) * (r0 * s);
     moments(c, fg[i] * s, unused, v);
     Coef d = c;
     d.eps = c.eps * s;
     const float r = root(v);
     fw[i] = stepped(d, fw[i], fm[i] * s, r);
-    fr[i] = far ? r * 0x1p96f : r;
+    fr[i] = kept(scaled ? r * 0x1p72f : r);
+    fm[i] = kept(fm[i]);
   }
 }
 
@@ -411,8 +421,8 @@ __device__ __forceinline__ void adam8_tile(const Coef& c, const OptDesc& d, int6
       v2[i] = fr[i] * fr[i];
       moments(c, fg[i], fm[i], v2[i]);
     }
-    const float top = fmaxf(fmaxf(v2[0], v2[1]), fmaxf(v2[2], v2[3]));  // of what is no NaN
-    if (__builtin_amdgcn_ballot_w64(top == __builtin_inff())) {  // some square of the wave: rare
+    const float top = max_nc(max3_nc(v2[0], v2[1], v2[2]), v2[3]);  // NaN where one is
+    if (__builtin_amdgcn_ballot_w64(!(top < __builtin_inff()))) {    // some square of the wave: rare
       far_steps(c, fg, fm, v2, fr, fw);
     } else {
 #pragma unroll

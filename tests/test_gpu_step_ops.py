@@ -694,6 +694,38 @@ def test_adamw_of_gradients_whose_squares_are_infinite(param, f):
     within(k.v["w"][0][[5, 64]], w0[[5, 64]], 0.0, "w under an infinite v")
 
 
+@pytest.mark.parametrize("b1,b2", [(0.0, 0.99), (0.9, 0.0), (0.0, 0.0)])
+def test_adamw_states_at_the_end_of_the_range(b1, b2):
+    """With a beta of zero a state is as large as its gradient: rounding up must
+    not make 256 2^120, which is past fp32's range, of 8-bit states.  Three steps
+    under large gradients, and with beta1 zero one under small ones (else m over a
+    small r is itself past the range), leave finite parameters, each step within
+    check_step's count of roundings, and states to a step of their codes (2^-3)."""
+    announce(f"adamw states at the end of the range betas={b1},{b2}")
+    lr, eps = 1e-2, 1e-8
+    k = Setting([256], "e4m3", "f32", "f32")
+    for t in (1, 2, 3, 4) if b1 == 0.0 else (1, 2, 3):
+        k.gradients(t)
+        if t < 4:
+            big = torch.linspace(3.1e38, 3.4e38, 200, device="cuda")
+            k.v["g"][0][20:220] = torch.where(torch.arange(200, device="cuda") % 3 == t % 3, -big, big)
+        w, g = k.np("w")[0], k.np("g")[0]
+        m, r = (O.value8(k.np(a)[0], k.np(a + "s")[0]) for a in ("m", "v"))
+        assert np.abs(m).max() < 2.0 ** 128 and r.max() < 2.0 ** 128
+        L.sppo_adamw_step(k.list, L.adamw(lr, b1, b2, eps, t, seed=t))
+        rp, rm, rv = O.adamw(w, g, m, r * r, t, lr * k.lrs[0], b1, b2, eps, k.decay[0])
+        tm = 4 * U * (np.abs(b1 * m) + (1 - b1) * np.abs(g)) + 2.0 ** -148
+        den = np.sqrt(rv / (1 - b2 ** t)) + eps
+        q = rm / (1 - b1 ** t) / den
+        tp = lr * k.lrs[0] * (tm / (1 - b1 ** t) / den + 16 * U * np.abs(q)) + 2 * U * np.abs(w)
+        within(k.v["w"][0], rp, tp, ("w", t))
+        for a, x in (("m", rm), ("v", np.sqrt(rv))):
+            scales = k.v[a + "s"][0].cpu().numpy()
+            unit = 2.0 ** (np.repeat(scales.astype(np.float64), 32)[:256] - 127)
+            got = O.value8(k.v[a][0].cpu().numpy(), scales)
+            assert np.all(np.abs(got - x) <= 2.0 ** -3 * np.abs(x) + 2.0 ** -9 * unit), (a, t)
+
+
 # --------------------------------------------------------------------- together
 def test_a_step_in_graphs():
     """Rotary, loss, norm and update captured twice with their own buffers and
